@@ -1,4 +1,5 @@
-"""Python binding of the GB300 PackServe scheduler library (include/packserve.h).
+"""Python binding of the GB300 PackServe scheduler library (include/packserve.h; the serving operators of
+include/packserve_kv.h are wrapped for torch in ``kvcache``).
 
 Argument marshalling only: every step of the hot path (hit lengths, latency model, filters,
 argmin, greedy assignment) runs in the CUDA kernels of ``libpackserve.so``.  The raw entry points
@@ -27,7 +28,9 @@ ABI_FUNCTIONS = ("ps_create", "ps_load_instances", "ps_get_instances", "ps_get_p
                  "ps_insert_blocks", "ps_insert_chains", "ps_cached_blocks", "ps_score_window",
                  "ps_schedule_window", "ps_commit_window", "ps_last_timings", "ps_last_probe_stats", "ps_last_error",
                  "ps_destroy", "ps_score_window_noalloc", "ps_load_requests", "ps_advance_window",
-                 "ps_shard_wmin", "ps_shard_pick")
+                 "ps_shard_wmin", "ps_shard_pick",
+                 "ps_kv_create", "ps_kv_write", "ps_kv_read", "ps_kv_check", "ps_kv_plan_create", "ps_kv_plan_set",
+                 "ps_kv_plan_workspace", "ps_kv_attend", "ps_kv_last_error", "ps_kv_plan_destroy", "ps_kv_destroy")
 
 
 class PsModel(ctypes.Structure):
@@ -95,6 +98,16 @@ class PsStateArrays(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("b", "qr", "q_tokens", "S_tokens", "M_KV_tokens", "B_max")]
 
 
+class PsKvConfig(ctypes.Structure):
+    _fields_ = [("device", ctypes.c_int32), ("kv_heads", ctypes.c_uint32), ("num_blocks", ctypes.c_uint64),
+                ("head_dim", ctypes.c_uint32), ("format", ctypes.c_int32)]
+
+
+class PsKvRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("type", ctypes.c_int32)]
+
+
 PS_NOALLOC_MAX_PAIRS = 2097152
 
 STATE_DTYPE = np.dtype([("b", np.int32), ("qr", np.int32), ("q_tokens", np.int64), ("S_tokens", np.int64),
@@ -137,6 +150,15 @@ def lib() -> ctypes.CDLL:
             "ps_shard_pick": [vp, vp, u32, vp, vp, i32, ctypes.POINTER(PsScores)],
             "ps_score_window_noalloc": [vp, vp, vp, u32, ctypes.POINTER(PsStateArrays), ctypes.POINTER(PsWindow),
                                         ctypes.POINTER(PsModel), i32, ctypes.POINTER(PsScores), vp],
+            "ps_kv_create": [ctypes.POINTER(PsKvConfig), ctypes.POINTER(vp)],
+            "ps_kv_write": [vp, ctypes.POINTER(PsKvRows), ctypes.POINTER(PsKvRows), vp, u64, vp],
+            "ps_kv_read": [vp, vp, u64, ctypes.POINTER(PsKvRows), ctypes.POINTER(PsKvRows), vp],
+            "ps_kv_check": [vp, vp],
+            "ps_kv_plan_create": [vp, u32, u32, u32, u64, ctypes.POINTER(vp)],
+            "ps_kv_plan_set": [vp, u32, vp, u32, vp, u64],
+            "ps_kv_plan_workspace": [vp, ctypes.POINTER(u64)],
+            "ps_kv_attend": [vp, vp, ctypes.POINTER(PsKvRows), ctypes.POINTER(PsKvRows), vp, ctypes.c_float, vp, u64,
+                             vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -144,8 +166,11 @@ def lib() -> ctypes.CDLL:
             fn.restype = st
         L.ps_last_error.argtypes = [vp]
         L.ps_last_error.restype = ctypes.c_char_p
-        L.ps_destroy.argtypes = [vp]
-        L.ps_destroy.restype = None
+        L.ps_kv_last_error.argtypes = [vp]
+        L.ps_kv_last_error.restype = ctypes.c_char_p
+        for name in ("ps_destroy", "ps_kv_plan_destroy", "ps_kv_destroy"):
+            getattr(L, name).argtypes = [vp]
+            getattr(L, name).restype = None
         _lib = L
     return _lib
 

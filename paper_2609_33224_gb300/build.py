@@ -16,7 +16,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libpackserve.so")
-SOURCES = ["api.cu", "probe.cu", "score.cu", "greedy.cu", "relations.cu", "table.cu", "noalloc.cu", "window.cu"]
+SOURCES = ["api.cu", "probe.cu", "score.cu", "greedy.cu", "relations.cu", "table.cu", "noalloc.cu", "window.cu",
+           "kv.cu", "kv_store.cu", "kv_rows.cu", "kv_join.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 # host code is compiled without floating-point contraction (calibrate.h is exact fp32, op by op)
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
@@ -44,11 +45,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
     headers = [os.path.join(CSRC, "ps_internal.cuh"), os.path.join(CSRC, "calibrate.h"),
                os.path.join(CSRC, "greedy_grid.h"),
                os.path.join(ROOT, "include", "packserve.h")]
+    kv_headers = [os.path.join(CSRC, "kv_internal.cuh"), os.path.join(ROOT, "include", "packserve_kv.h"), headers[-1]]
     jobs = []
     for src in SOURCES:
         s = os.path.join(CSRC, src)
         o = os.path.join(BUILD, src.replace(".cu", ".o"))
-        if force or _stale(o, [s] + headers):
+        if force or _stale(o, [s] + (kv_headers if src.startswith("kv") else headers)):
             cmd = [nvcc, *ARCH, *FLAGS, "-I", os.path.join(ROOT, "include"), "-c", s, "-o", o]
             if verbose:
                 cmd.insert(1, "-Xptxas=-v")

@@ -1,0 +1,211 @@
+// Shared by the serving operators (kv*.cu): the layout of a cache block, the descriptors that a plan hands
+// to the attention kernels, and the PTX wrappers they use.
+//
+// A cache is an array of records, one per (block, key/value head), the heads of a block next to each other.
+// A record holds 16 tokens:
+//   16-bit formats: K then V, each 16 * D * 2 bytes as two groups of 8 tokens, a group as D / 64 panels of
+//     8 rows x 128 bytes, 16-byte chunk c of row r at chunk c ^ r.  That is the 128-byte-swizzled order that
+//     the tensor cores read from shared memory (keys: K-major, 8-row groups 16 * D bytes apart; values:
+//     MN-major, panels 1024 bytes apart), so a plain bulk copy of a record's half lands ready for use,
+//     and ldmatrix reads it without bank conflicts.
+//   fp8: K codes, V codes (16 rows of D bytes, 16-byte chunk c of row r at c ^ swz(r)), then the 16 scale
+//     exponents of K and the 16 of V (biased by 127; 255: the row holds a NaN), which fill one 32-byte
+//     sector: one copy brings a record with its scales.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "packserve_kv.h"
+
+namespace pskv {
+
+constexpr int kBlock = PS_BLOCK_TOKENS;
+constexpr int kSmallRows = 16;   // rows of a tile of the row kernel (one m16 of mma.sync)
+constexpr int kTileRows = 256;   // rows of a tile of the tile kernel (two tcgen05 accumulators of 128)
+constexpr int kTileKeys = 128;   // keys of one step of the tile kernel
+constexpr int kExpBias = 127;
+constexpr int kExpMin = -110, kExpMax = 119, kExpNan = 255;
+
+enum : uint32_t { kErrSlot = 1u, kErrWait = 2u };
+
+__host__ __device__ constexpr int record_bytes(int D, int fmt) {
+  return fmt == PS_KV_FP8 ? 2 * kBlock * D + 2 * kBlock : 2 * kBlock * D * 2;
+}
+__host__ __device__ constexpr int half_bytes(int D, int fmt) { return kBlock * D * (fmt == PS_KV_FP8 ? 1 : 2); }
+
+// byte offset of 16-byte chunk c of token t inside the K (or V) part of a record
+template <int D, bool FP8>
+__device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t c) {
+  if (FP8) {
+    const uint32_t swz = D == 128 ? (t & 7u) : ((t >> 1) & 3u);
+    return t * D + ((c ^ swz) << 4);
+  }
+  return (t >> 3) * (8 * D * 2) + (c >> 3) * 1024 + (t & 7u) * 128 + (((c & 7u) ^ (t & 7u)) << 4);
+}
+
+// A piece of work of either attention kernel: a run of key blocks for the rows of one tile and one
+// key/value head.  A span's rows are its queries' heads of the group, row r = (r / g)-th query, head r % g.
+struct alignas(16) Piece {
+  uint32_t block;     // where the piece's block ids start
+  uint32_t nblocks;   // blocks (row kernel) or key tiles of 8 blocks (tile kernel; the last may be partial)
+  uint32_t key0;      // index in the span of the first key
+  uint32_t end;       // keys end before this index
+  int32_t climit;     // the span's i-th query sees keys j <= climit + i
+  uint32_t query0;    // the span's first query
+  uint32_t row0;      // the tile's first row
+  uint32_t part_row;  // first row of the partial result, or kDirect: the only piece of its rows
+  uint16_t nrows;
+  uint16_t head;
+  uint32_t pad[3];
+};
+static_assert(sizeof(Piece) == 48, "Piece layout");
+constexpr uint32_t kDirect = 0xFFFFFFFFu;
+constexpr int32_t kNoLimit = 0x3FFFFFFF;
+
+// The rows of a span, tiled one way; tile t and head h have the parts groups[group0 + t * kv_heads + h].
+struct Layer {
+  uint32_t query0;
+  uint32_t tile_rows;
+  uint32_t group0;
+  uint32_t pad;
+};
+struct Group {
+  uint32_t part_row;  // kDirect: already in the output
+  uint32_t nparts;
+};
+
+struct PlanDev {
+  const Piece* row_pieces;
+  const uint32_t* row_off;  // pieces of worker w: row_off[w] .. row_off[w + 1]
+  uint32_t row_workers, row_ctas;
+  const Piece* tile_pieces;
+  const uint32_t* tile_off;
+  uint32_t tile_ctas;
+  const Layer* layers;
+  const Group* groups;
+  const uint32_t* tok_off;  // layers of query t: tok_layer[tok_off[t]] ..
+  const uint32_t* tok_layer;
+  const uint32_t* join;  // (query * kv_heads + head) that have parts to join, or nothing
+  uint32_t njoin;
+  uint32_t max_parts;
+  const uint32_t* blocks;
+};
+
+struct AttnArgs {
+  const uint8_t* pool;
+  const uint16_t* q;
+  int64_t q_tok, q_head;  // in elements
+  uint16_t* out;
+  int64_t o_tok, o_head;
+  float* lse;       // [query][q head] or null
+  float* part;      // [part row][D], not yet divided by the sum
+  float2* part_ml;  // [part row] maximum (of the scores times log2 e) and sum
+  uint32_t kv_heads, group;
+  float scale_log2;
+  uint32_t* err;  // mapped host word
+};
+
+struct StoreArgs {
+  uint8_t* pool;
+  const int64_t* slots;
+  uint64_t n;
+  uint64_t num_slots;
+  uint32_t kv_heads;
+  void* k;
+  void* v;
+  int64_t k_tok, k_head, v_tok, v_head;
+  uint32_t* err;
+};
+
+cudaError_t launch_write(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
+cudaError_t launch_read(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
+cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
+cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
+cudaError_t prepare_rows(int D, int fmt);
+constexpr int kRowWarps = 8;  // workers (warps) of a CTA of the row kernel
+
+// ---- PTX ----------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// Waits for a phase, one second at most (the limit of the scheduler's waits); false: it gave up.
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+  const uint64_t t0 = now_ns();
+  for (;;) {
+    for (int i = 0; i < 256; ++i)
+      if (mbar_try(bar, parity)) return true;
+    if (now_ns() - t0 > 1000000000ull) return false;
+  }
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
+  for (int i = 0; i < 16; ++i)
+    if (mbar_try(bar, parity)) return true;
+  return mbar_wait_slow(bar, parity);
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <bool FP16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if (FP16) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// The scale of an fp8 row as a float; the mark of a row with a NaN gives a NaN.
+__device__ __forceinline__ float exp_value(uint32_t e) {
+  return __uint_as_float(e == kExpNan ? 0x7FC00000u : e << 23);
+}
+
+// Two e4m3 codes in the high bytes of the halves of x -> bf16x2, without their scale.  A code's magnitude
+// bits, moved down by 4, are a bf16 whose exponent bias is 127 instead of 7 (subnormal codes become bf16
+// subnormals), so a product with 2^120 gives the value, exactly.  Code 0x7F (NaN) becomes 480: the caches
+// mark rows with a NaN by their scale.
+__device__ __forceinline__ uint32_t e4m3_to_bf16x2(uint32_t x) {
+  const uint32_t y = ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u);
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(y), "r"(0x7B807B80u));
+  return r;
+}
+
+}  // namespace pskv

@@ -1,0 +1,459 @@
+// Attention of few rows over many keys (single-token queries, the ends of causal spans): the row kernel.
+//
+// A worker is one warp.  It holds 16 rows of one span and key/value head (queries x heads of the group) and
+// streams the records of its run of blocks through a private ring in shared memory, one bulk copy per
+// record (16 keys and values), several in flight, with no barrier between warps: per block, scores by
+// mma.sync (16 rows x 16 keys), the running maximum and sum of the softmax, and the product with the
+// values, all in registers.  The plan cuts the batch's (rows, head, keys) space into equal shares, one per
+// worker, so that long and short spans fill the GPU alike; a share's rows leave as partial results (maximum,
+// sum, unnormalised values) for join_kernel, or as the final output where nothing is to be joined.
+//
+// Bound by the bytes of the cache: 2 * D elements per key and head for 4 * D * 16 multiply-adds.  mma.sync
+// has the smallest tile (16 rows) and takes operands and results in registers; tcgen05's 128 rows would be
+// 1/8 or less filled here.
+#include "kv_internal.cuh"
+
+namespace pskv {
+namespace {
+
+constexpr int kRingBytes = 28 * 1024;  // ring of one warp; 8 warps fill the 227 KB of an SM
+
+template <int D, int FMT>
+constexpr int ring_stages() {
+  return kRingBytes / record_bytes(D, FMT);
+}
+
+template <bool FP16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (FP16)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <bool TRANS>
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  if (TRANS)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t addr) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128_zero(uint32_t addr) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(addr), "r"(0) : "memory");
+}
+
+// Whether one of the two 16-bit floats in w is an infinity or a NaN.
+template <bool FP16>
+__device__ __forceinline__ bool not_finite2(uint32_t w) {
+  constexpr uint32_t m = FP16 ? 0x7C00u : 0x7F80u;
+  return (w & m) == m || ((w >> 16) & m) == m;
+}
+template <bool FP16>
+__device__ __forceinline__ float value16(uint16_t b) {
+  if (FP16) return __half2float(__ushort_as_half(b));
+  return __uint_as_float((uint32_t)b << 16);
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
+  constexpr bool kFp8 = FMT == PS_KV_FP8, kFp16 = FMT == PS_KV_FP16;
+  constexpr int kRec = record_bytes(D, FMT), kHalf = half_bytes(D, FMT);
+  constexpr int kStages = ring_stages<D, FMT>();
+  constexpr int kTiles = D / 8;  // n8 tiles of the output
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[kRowWarps * kStages];
+
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t worker = warp * p.row_ctas + blockIdx.x;  // neighbours in the plan go to different SMs
+  if (worker >= p.row_workers) return;                     // no barrier of the CTA is used
+  const uint32_t ring = smem_u32(smem) + warp * kStages * kRec;
+  const uint32_t bar = smem_u32(bars) + warp * kStages * 8;
+  if (lane < kStages) mbar_init(bar + lane * 8, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
+
+  const uint32_t piece_end = p.row_off[worker + 1];
+  // what is loaded next: block `ahead_i` of piece `ahead`, into stage `ahead_st`
+  uint32_t ahead = p.row_off[worker], ahead_i = 0, ahead_st = 0;
+  uint32_t ahead_n = 0, ahead_block = 0, ahead_head = 0, ids = 0;
+  uint32_t in_flight = 0;
+  auto issue = [&]() {
+    if (ahead >= piece_end) return;
+    if (ahead_i == 0) {
+      const Piece* q = p.row_pieces + ahead;
+      ahead_n = q->nblocks;
+      ahead_block = q->block;
+      ahead_head = q->head;
+    }
+    if ((ahead_i & 31u) == 0) ids = p.blocks[ahead_block + min(ahead_i + lane, ahead_n - 1)];
+    const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, ahead_i & 31u);
+    if (lane == 0) {
+      mbar_expect(bar + ahead_st * 8, kRec);
+      bulk_load(ring + ahead_st * kRec, a.pool + ((uint64_t)id * a.kv_heads + ahead_head) * kRec, kRec,
+                bar + ahead_st * 8);
+    }
+    ++in_flight;
+    ahead_st = ahead_st + 1 == kStages ? 0 : ahead_st + 1;
+    if (++ahead_i == ahead_n) {
+      ahead_i = 0;
+      ++ahead;
+    }
+  };
+#pragma unroll 1
+  for (int i = 0; i < kStages; ++i) issue();
+
+  const uint32_t quad = lane / 4, t4 = lane % 4;  // row (or key, or column) of a fragment, place in the quad
+  const uint32_t mi = lane / 8, mr = lane % 8;    // ldmatrix: matrix and row whose address this lane gives
+  uint32_t st = 0, phase = 0;
+
+  for (uint32_t pi = p.row_off[worker]; pi < piece_end; ++pi) {
+    const Piece pc = p.row_pieces[pi];
+    // ---- the rows of the tile
+    const uint32_t ra = pc.row0 + quad, rb = ra + 8;
+    const bool va = quad < pc.nrows, vb = quad + 8 < pc.nrows;
+    const uint32_t ta = ra / a.group, tb = rb / a.group;
+    const uint32_t ha = pc.head * a.group + ra % a.group, hb = pc.head * a.group + rb % a.group;
+    uint32_t qf[D / 16][4];
+    {
+      const uint16_t* qa = a.q + (int64_t)(pc.query0 + ta) * a.q_tok + (int64_t)ha * a.q_head;
+      const uint16_t* qb = a.q + (int64_t)(pc.query0 + tb) * a.q_tok + (int64_t)hb * a.q_head;
+#pragma unroll
+      for (int kc = 0; kc < D / 16; ++kc) {
+        // fp8: the key fragment of a 16-byte chunk has this lane's four neighbouring elements
+        const int lo = kFp8 ? kc * 16 + t4 * 4 : kc * 16 + t4 * 2, hi = kFp8 ? lo + 2 : lo + 8;
+        qf[kc][0] = va ? *reinterpret_cast<const uint32_t*>(qa + lo) : 0u;
+        qf[kc][1] = vb ? *reinterpret_cast<const uint32_t*>(qb + lo) : 0u;
+        qf[kc][2] = va ? *reinterpret_cast<const uint32_t*>(qa + hi) : 0u;
+        qf[kc][3] = vb ? *reinterpret_cast<const uint32_t*>(qb + hi) : 0u;
+      }
+    }
+    // the last key each of the two rows sees, and the last that all rows of the tile see
+    const int32_t last = (int32_t)pc.end - 1;
+    const int32_t lim_a = min(last, pc.climit + (int32_t)ta), lim_b = min(last, pc.climit + (int32_t)tb);
+    const int32_t lim_all = min(last, pc.climit + (int32_t)(pc.row0 / a.group));
+
+    float acc[kTiles][4];
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+    float ma = -INFINITY, mb = -INFINITY, la = 0.0f, lb = 0.0f;
+
+    for (uint32_t bi = 0; bi < pc.nblocks; ++bi) {
+      const uint32_t rec = ring + st * kRec;
+      if (!mbar_wait(bar + st * 8, phase)) {
+        if (lane == 0) atomicOr_system(a.err, kErrWait);
+        while (--in_flight) {  // the copies behind it write this warp's memory: they are waited for too
+          if (++st == kStages) {
+            st = 0;
+            phase ^= 1u;
+          }
+          mbar_wait(bar + st * 8, phase);
+        }
+        return;
+      }
+      // ---- scores
+      float s[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+      if constexpr (kFp8) {
+        const uint32_t tok = (mi & 1) * 8 + mr;
+#pragma unroll
+        for (int c = 0; c < D / 16; c += 2) {
+          uint32_t r[4];  // keys 0-7 and 8-15 of chunk c, then of chunk c + 1
+          ldsm4<false>(r, rec + chunk_offset<D, true>(tok, c + (mi >> 1)));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            mma16816<false>(s[i & 1], qf[c + (i >> 1)], e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x1404)),
+                            e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x3424)));
+        }
+      } else {
+        const uint32_t tok = (mi >> 1) * 8 + mr;
+#pragma unroll
+        for (int kc = 0; kc < D / 16; ++kc) {
+          uint32_t r[4];  // keys 0-7: elements 0-7 and 8-15 of the step; keys 8-15: the same
+          ldsm4<false>(r, rec + chunk_offset<D, false>(tok, 2 * kc + (mi & 1)));
+          mma16816<kFp16>(s[0], qf[kc], r[0], r[1]);
+          mma16816<kFp16>(s[1], qf[kc], r[2], r[3]);
+        }
+      }
+      float vs[4];  // fp8: the value rows' scales of this lane's keys
+      if constexpr (kFp8) {
+        const uint32_t e0 = lds16(rec + 2 * kHalf + t4 * 2), e1 = lds16(rec + 2 * kHalf + 8 + t4 * 2);
+        const uint32_t f0 = lds16(rec + 2 * kHalf + 16 + t4 * 2), f1 = lds16(rec + 2 * kHalf + 24 + t4 * 2);
+        const float k0 = exp_value(e0 & 255u) * a.scale_log2, k1 = exp_value(e0 >> 8) * a.scale_log2;
+        const float k2 = exp_value(e1 & 255u) * a.scale_log2, k3 = exp_value(e1 >> 8) * a.scale_log2;
+        s[0][0] *= k0; s[0][1] *= k1; s[0][2] *= k0; s[0][3] *= k1;
+        s[1][0] *= k2; s[1][1] *= k3; s[1][2] *= k2; s[1][3] *= k3;
+        vs[0] = exp_value(f0 & 255u); vs[1] = exp_value(f0 >> 8);
+        vs[2] = exp_value(f1 & 255u); vs[3] = exp_value(f1 >> 8);
+      } else {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[n][i] *= a.scale_log2;
+      }
+      // ---- masks: only blocks past what every row sees
+      const int32_t key0 = (int32_t)(pc.key0 + bi * kBlock);
+      const bool edge = key0 + kBlock - 1 > lim_all;  // the same for the whole warp
+      uint32_t bad = 0;                               // 16-bit formats: keys whose values are not all finite
+      if (edge) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int32_t j = key0 + n * 8 + (int32_t)t4 * 2 + i;
+            if (j > lim_a) s[n][i] = -INFINITY;
+            if (j > lim_b) s[n][2 + i] = -INFINITY;
+          }
+        if constexpr (!kFp8) {
+          // A masked key's probability is 0, but 0 times an infinity or a NaN is not: value rows past the
+          // end (left there by other tokens) and rows with such a value are taken out of the product.  Of
+          // the latter, those that some row sees are added below one by one.
+          const uint32_t tok = lane >> 1;
+          const bool past = key0 + (int32_t)tok > last;
+          bool odd = false;
+#pragma unroll 4
+          for (int c = 0; c < D / 16; ++c) {
+            const uint4 w = lds128(rec + kHalf + chunk_offset<D, false>(tok, 2 * c + (lane & 1)));
+            odd |= not_finite2<kFp16>(w.x) | not_finite2<kFp16>(w.y) | not_finite2<kFp16>(w.z) | not_finite2<kFp16>(w.w);
+          }
+          const uint32_t odds = __ballot_sync(0xFFFFFFFFu, odd && !past);
+          const bool out = past || ((odds >> (lane & ~1u)) & 3u) != 0;
+          if (out) {
+#pragma unroll 4
+            for (int c = 0; c < D / 16; ++c) sts128_zero(rec + kHalf + chunk_offset<D, false>(tok, 2 * c + (lane & 1)));
+          }
+          bad = odds | (odds >> 1);  // bit 2 * key
+          __syncwarp();
+        }
+      }
+      // ---- running maximum and sum.  The maximum that the exponents refer to follows only when a new one
+      // is more than 2^8 larger: up to there the probabilities and their sum are far from 32-bit overflow.
+      float xa = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
+      float xb = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
+      xa = fmaxf(xa, __shfl_xor_sync(0xFFFFFFFFu, xa, 1));
+      xb = fmaxf(xb, __shfl_xor_sync(0xFFFFFFFFu, xb, 1));
+      xa = fmaxf(xa, __shfl_xor_sync(0xFFFFFFFFu, xa, 2));
+      xb = fmaxf(xb, __shfl_xor_sync(0xFFFFFFFFu, xb, 2));
+      if (__any_sync(0xFFFFFFFFu, xa > ma + 8.0f || xb > mb + 8.0f)) {
+        const float na = fmaxf(ma, xa), nb = fmaxf(mb, xb);
+        const float fa = na == ma ? 1.0f : ex2(ma - na), fb = nb == mb ? 1.0f : ex2(mb - nb);
+        ma = na;
+        mb = nb;
+        la *= fa;
+        lb *= fb;
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          acc[j][0] *= fa;
+          acc[j][1] *= fa;
+          acc[j][2] *= fb;
+          acc[j][3] *= fb;
+        }
+      }
+      const float ua = ma == -INFINITY ? 0.0f : ma, ub = mb == -INFINITY ? 0.0f : mb;
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        s[n][0] = ex2(s[n][0] - ua);
+        s[n][1] = ex2(s[n][1] - ua);
+        s[n][2] = ex2(s[n][2] - ub);
+        s[n][3] = ex2(s[n][3] - ub);
+        la += s[n][0] + s[n][1];
+        lb += s[n][2] + s[n][3];
+      }
+      if constexpr (kFp8) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float fa = vs[2 * n + i], fb = fa;
+            if (edge) {  // the scale of a masked row may be the mark of a NaN
+              const int32_t j = key0 + n * 8 + (int32_t)t4 * 2 + i;
+              if (j > lim_a) fa = 0.0f;
+              if (j > lim_b) fb = 0.0f;
+            }
+            s[n][i] *= fa;
+            s[n][2 + i] *= fb;
+          }
+      }
+      // ---- product with the values
+      const uint32_t pf[4] = {pack2<kFp16>(s[0][0], s[0][1]), pack2<kFp16>(s[0][2], s[0][3]),
+                              pack2<kFp16>(s[1][0], s[1][1]), pack2<kFp16>(s[1][2], s[1][3])};
+      if constexpr (kFp8) {
+        const uint32_t tok = (mi & 1) * 8 + mr;
+#pragma unroll
+        for (int c = 0; c < D / 16; c += 2) {
+          uint32_t r[4];
+          ldsm4<true>(r, rec + kHalf + chunk_offset<D, true>(tok, c + (mi >> 1)));
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            // a chunk's 16 columns: tile 2c has the even ones, tile 2c + 1 the odd ones
+            mma16816<false>(acc[2 * c + i], pf, e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x2404)),
+                            e4m3_to_bf16x2(__byte_perm(r[i + 1], 0, 0x2404)));
+            mma16816<false>(acc[2 * c + i + 1], pf, e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x3414)),
+                            e4m3_to_bf16x2(__byte_perm(r[i + 1], 0, 0x3414)));
+          }
+        }
+      } else {
+        const uint32_t tok = (mi & 1) * 8 + mr;
+#pragma unroll
+        for (int j = 0; j < kTiles; j += 2) {
+          uint32_t r[4];
+          ldsm4<true>(r, rec + kHalf + chunk_offset<D, false>(tok, j + (mi >> 1)));
+          mma16816<kFp16>(acc[j], pf, r[0], r[1]);
+          mma16816<kFp16>(acc[j + 1], pf, r[2], r[3]);
+        }
+        if (edge) {
+          if (bad & 0x55555555u) {
+            const uint32_t id = p.blocks[pc.block + bi];
+            const uint8_t* vals = a.pool + ((uint64_t)id * a.kv_heads + pc.head) * kRec + kHalf;
+            for (uint32_t kk = 0; kk < kBlock; ++kk) {
+              if (!((bad >> (2 * kk)) & 1u)) continue;
+              const uint32_t from = (lane & ~3u) | ((kk % 8) / 2);
+              const float c0 = kk < 8 ? ((kk & 1) ? s[0][1] : s[0][0]) : ((kk & 1) ? s[1][1] : s[1][0]);
+              const float c1 = kk < 8 ? ((kk & 1) ? s[0][3] : s[0][2]) : ((kk & 1) ? s[1][3] : s[1][2]);
+              const float pa = __shfl_sync(0xFFFFFFFFu, c0, from), pb = __shfl_sync(0xFFFFFFFFu, c1, from);
+              const bool sa = key0 + (int32_t)kk <= lim_a, sb = key0 + (int32_t)kk <= lim_b;
+#pragma unroll
+              for (int j = 0; j < kTiles; ++j) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vals + chunk_offset<D, false>(kk, j) + t4 * 4);
+                const float v0 = value16<kFp16>((uint16_t)w), v1 = value16<kFp16>((uint16_t)(w >> 16));
+                if (sa) {
+                  acc[j][0] += pa * v0;
+                  acc[j][1] += pa * v1;
+                }
+                if (sb) {
+                  acc[j][2] += pb * v0;
+                  acc[j][3] += pb * v1;
+                }
+              }
+            }
+          }
+          fence_async_shared();  // the zeros above before the next copy into this stage
+        }
+      }
+      __syncwarp();
+      --in_flight;
+      if (++st == kStages) {
+        st = 0;
+        phase ^= 1u;
+      }
+      issue();
+    }
+
+    // ---- the piece's result
+    la += __shfl_xor_sync(0xFFFFFFFFu, la, 1);
+    lb += __shfl_xor_sync(0xFFFFFFFFu, lb, 1);
+    la += __shfl_xor_sync(0xFFFFFFFFu, la, 2);
+    lb += __shfl_xor_sync(0xFFFFFFFFu, lb, 2);
+    if (pc.part_row != kDirect) {
+      float* oa = a.part + (uint64_t)(pc.part_row + quad) * D;
+      float* ob = oa + 8 * D;
+      if (va) {
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          if (kFp8) {
+            if (j & 1) continue;
+            *reinterpret_cast<float4*>(oa + 8 * j + 4 * t4) = make_float4(acc[j][0], acc[j + 1][0], acc[j][1], acc[j + 1][1]);
+          } else {
+            *reinterpret_cast<float2*>(oa + 8 * j + 2 * t4) = make_float2(acc[j][0], acc[j][1]);
+          }
+        }
+        if (t4 == 0) a.part_ml[pc.part_row + quad] = make_float2(ma, la);
+      }
+      if (vb) {
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          if (kFp8) {
+            if (j & 1) continue;
+            *reinterpret_cast<float4*>(ob + 8 * j + 4 * t4) = make_float4(acc[j][2], acc[j + 1][2], acc[j][3], acc[j + 1][3]);
+          } else {
+            *reinterpret_cast<float2*>(ob + 8 * j + 2 * t4) = make_float2(acc[j][2], acc[j][3]);
+          }
+        }
+        if (t4 == 0) a.part_ml[pc.part_row + 8 + quad] = make_float2(mb, lb);
+      }
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (half ? !vb : !va) continue;
+        const float l = half ? lb : la, m = half ? mb : ma;
+        const uint32_t query = pc.query0 + (half ? tb : ta), head = half ? hb : ha;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no key: zeros (a NaN stays one)
+        uint16_t* o = a.out + (int64_t)query * a.o_tok + (int64_t)head * a.o_head;
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          const float x0 = acc[j][2 * half] * inv, x1 = acc[j][2 * half + 1] * inv;
+          if (kFp8) {
+            if (j & 1) continue;
+            const float y0 = acc[j + 1][2 * half] * inv, y1 = acc[j + 1][2 * half + 1] * inv;
+            *reinterpret_cast<uint2*>(o + 8 * j + 4 * t4) = make_uint2(pack2<kFp16>(x0, y0), pack2<kFp16>(x1, y1));
+          } else {
+            *reinterpret_cast<uint32_t*>(o + 8 * j + 2 * t4) = pack2<kFp16>(x0, x1);
+          }
+        }
+        if (a.lse && t4 == 0)
+          a.lse[(uint64_t)query * a.kv_heads * a.group + head] =
+              l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      }
+    }
+  }
+}
+
+template <int D, int FMT>
+constexpr int smem_bytes() {
+  return kRowWarps * ring_stages<D, FMT>() * record_bytes(D, FMT);
+}
+
+template <int D, int FMT>
+cudaError_t prepare_one() {
+  return cudaFuncSetAttribute(rows_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FMT>());
+}
+template <int D, int FMT>
+cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+  rows_kernel<D, FMT><<<p.row_ctas, kRowWarps * 32, smem_bytes<D, FMT>(), s>>>(a, p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t prepare_rows(int D, int fmt) {
+  if (D == 128)
+    return fmt == PS_KV_BF16   ? prepare_one<128, PS_KV_BF16>()
+           : fmt == PS_KV_FP16 ? prepare_one<128, PS_KV_FP16>()
+                               : prepare_one<128, PS_KV_FP8>();
+  return fmt == PS_KV_BF16   ? prepare_one<64, PS_KV_BF16>()
+         : fmt == PS_KV_FP16 ? prepare_one<64, PS_KV_FP16>()
+                             : prepare_one<64, PS_KV_FP8>();
+}
+
+cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+  if (D == 128)
+    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, s)
+           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, s)
+                               : launch_one<128, PS_KV_FP8>(a, p, s);
+  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, s)
+         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, s)
+                             : launch_one<64, PS_KV_FP8>(a, p, s);
+}
+
+}  // namespace pskv

@@ -1,0 +1,207 @@
+"""The serving operators (include/packserve_kv.h) for torch: the paged key/value cache in the scheduler's
+16-token blocks, and attention of a batch over it.
+
+``KVCache`` holds the keys and values of one layer: ``write`` stores new tokens (rounding them to the
+cache's format), ``read`` gives back what the cache holds, ``attend`` computes attention of a batch that an
+``AttentionPlan`` describes.  All three run on torch's current stream of the cache's device and return
+without waiting for it; what a kernel finds wrong raises ``PSError`` from the next call, or from ``check``.
+"""
+from __future__ import annotations
+
+import ctypes
+import weakref
+
+import numpy as np
+import torch
+
+from . import PS_OK, PSError, PsKvConfig, PsKvRows, lib
+
+FORMATS = {"bf16": 0, "fp16": 1, "fp8": 2}
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 3}
+BLOCK_TOKENS = 16
+# ps_kv_span: a run of cached tokens (their blocks start at first_block of the plan's block array) and the
+# queries that see it; causal: the last num_queries tokens are the queries' own
+SPAN_DTYPE = np.dtype([("first_query", np.uint32), ("num_queries", np.uint32), ("length", np.uint64),
+                       ("causal", np.uint32), ("first_block", np.uint64)], align=True)
+
+
+class KVCache:
+    """``num_blocks`` blocks of 16 tokens x ``kv_heads`` x ``head_dim`` (64 or 128) keys and values.
+
+    ``fmt``: "bf16", "fp16", or "fp8" (e4m3 with a power-of-two scale per token and head).  Token t of block b
+    has slot ``16 * b + t``.  Without ``device``, torch's current one.
+    """
+
+    def __init__(self, num_blocks: int, kv_heads: int, head_dim: int, fmt: str = "bf16", device: int | None = None):
+        if fmt not in FORMATS:
+            raise ValueError(f"fmt must be one of {', '.join(FORMATS)}")
+        self.device = torch.cuda.current_device() if device is None else int(device)
+        self.num_blocks, self.kv_heads, self.head_dim, self.fmt = int(num_blocks), int(kv_heads), int(head_dim), fmt
+        self.dtype = torch.float16 if fmt == "fp16" else torch.bfloat16  # of the queries and the output
+        if not (0 < self.num_blocks < 1 << 32 and 0 < self.kv_heads <= 1024 and self.head_dim in (64, 128)):
+            raise ValueError("num_blocks must be in 1..2^32-1, kv_heads in 1..1024, head_dim 64 or 128")
+        cfg = PsKvConfig(self.device, self.kv_heads, self.num_blocks, self.head_dim, FORMATS[fmt])
+        h = ctypes.c_void_p()
+        s = lib().ps_kv_create(ctypes.byref(cfg), ctypes.byref(h))
+        if s != PS_OK:
+            raise PSError(s, "ps_kv_create failed (invalid configuration or device allocation)")
+        self._h = h
+        self._lib = lib()
+        self._plans = weakref.WeakSet()
+
+    def _check(self, s: int):
+        if s != PS_OK:
+            raise PSError(s, self._lib.ps_kv_last_error(self._h).decode())
+
+    def close(self):
+        """Release the cache's memory, and the plans made for it."""
+        if getattr(self, "_h", None):
+            for p in list(self._plans):
+                p.close()
+            self._lib.ps_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def _open(self):
+        if not self._h:
+            raise ValueError("the cache is closed")
+        return self._h
+
+    def _stream(self):
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _rows(self, x, name: str, n: int, heads: int) -> PsKvRows:
+        if x.device.type != "cuda" or x.device.index != self.device:
+            raise ValueError(f"{name} must be a tensor on cuda:{self.device}")
+        t = _TYPES.get(x.dtype)
+        if t is None:
+            raise ValueError(f"{name} must be bfloat16, float16 or float32, not {x.dtype}")
+        if x.dim() != 3 or x.shape[0] != n or x.shape[1] != heads or x.shape[2] != self.head_dim:
+            raise ValueError(f"{name} must have shape {(n, heads, self.head_dim)}, not {tuple(x.shape)}")
+        st = x.stride()
+        if st[2] != 1:
+            raise ValueError(f"{name}'s head_dim elements must lie next to each other")
+        return PsKvRows(x.data_ptr(), st[0], st[1], t)
+
+    def _slots(self, slots) -> int:
+        if slots.dtype != torch.int64 or slots.dim() != 1 or slots.device.type != "cuda" or \
+                slots.device.index != self.device or not slots.is_contiguous():
+            raise ValueError(f"slots must be a contiguous int64 vector on cuda:{self.device}")
+        return slots.shape[0]
+
+    def write(self, k, v, slots):
+        """Store row t of k and v ([T, kv_heads, head_dim]) at slot ``slots[t]`` (int64; negative: skipped)."""
+        h, n = self._open(), self._slots(slots)
+        rk, rv = self._rows(k, "k", n, self.kv_heads), self._rows(v, "v", n, self.kv_heads)
+        self._check(self._lib.ps_kv_write(h, rk, rv, slots.data_ptr(), n, self._stream()))
+
+    def read(self, slots, dtype=None, k=None, v=None):
+        """The cached keys and values at ``slots``, as (k, v) of ``dtype`` (default: ``self.dtype``) or in the
+        tensors given; a negative slot gives zeros."""
+        h, n = self._open(), self._slots(slots)
+        shape = (n, self.kv_heads, self.head_dim)
+        if k is None:
+            k = torch.empty(shape, dtype=dtype or self.dtype, device=slots.device)
+        if v is None:
+            v = torch.empty(shape, dtype=dtype or self.dtype, device=slots.device)
+        if dtype is not None and (k.dtype != dtype or v.dtype != dtype):
+            raise ValueError("k and v are not of the dtype asked for")
+        rk, rv = self._rows(k, "k", n, self.kv_heads), self._rows(v, "v", n, self.kv_heads)
+        self._check(self._lib.ps_kv_read(h, slots.data_ptr(), n, rk, rv, self._stream()))
+        return k, v
+
+    def attend(self, q, plan: "AttentionPlan", scale: float | None = None, out=None, lse=None):
+        """Attention of the plan's batch: q [queries, q_heads, head_dim] of ``self.dtype`` -> out of the same shape.
+
+        ``scale`` defaults to head_dim ** -0.5; ``lse``, a contiguous float32 [queries, q_heads] tensor, receives
+        the logarithms of the softmax sums (-inf where a query sees no key; its output is zero).
+        """
+        h, p = self._open(), plan._open()
+        n, heads = plan.num_queries, plan.q_heads
+        if out is None:
+            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=q.device)
+        rq, ro = self._rows(q, "q", n, heads), self._rows(out, "out", n, heads)
+        if lse is not None and (lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or
+                                tuple(lse.shape) != (n, heads)):
+            raise ValueError(f"lse must be a contiguous float32 tensor of shape {(n, heads)} on q's device")
+        nb = plan.workspace_bytes
+        ws = torch.empty(nb, dtype=torch.uint8, device=q.device) if nb else None
+        self._check(self._lib.ps_kv_attend(h, p, rq, ro, None if lse is None else lse.data_ptr(),
+                                           self.head_dim ** -0.5 if scale is None else scale,
+                                           None if ws is None else ws.data_ptr(), nb, self._stream()))
+        return out
+
+    def check(self):
+        """Wait for the current stream and raise what kernels have reported since the last report."""
+        self._check(self._lib.ps_kv_check(self._open(), self._stream()))
+
+
+class AttentionPlan:
+    """The spans of a batch for ``KVCache.attend``: set once per step, used by every layer's call of it.
+
+    ``set(num_queries, spans, blocks)``: ``spans`` is an array of ``SPAN_DTYPE`` (or rows of its five fields),
+    ``blocks`` the uint32 block ids that they index.  A prefix shared by a range of queries is one span over
+    all of them, a request's own tokens a (causal) span of its own.
+    """
+
+    def __init__(self, cache: KVCache, q_heads: int, max_queries: int, max_spans: int, max_blocks: int):
+        h = ctypes.c_void_p()
+        limits = [int(x) for x in (q_heads, max_queries, max_spans, max_blocks)]
+        if min(limits) < 0 or max(limits) >= 1 << 32:
+            raise ValueError("q_heads and the limits must be in 0..2^32-1")
+        self.cache, self.q_heads, self.num_queries, self.workspace_bytes = cache, limits[0], 0, 0
+        cache._check(cache._lib.ps_kv_plan_create(cache._open(), *limits, ctypes.byref(h)))
+        self._h = h
+        cache._plans.add(self)
+
+    def _open(self):
+        if not self._h:
+            raise ValueError("the plan is closed")
+        return self._h
+
+    def set(self, num_queries: int, spans, blocks):
+        L, h = self.cache._lib, self._open()
+        if not (isinstance(spans, np.ndarray) and spans.dtype == SPAN_DTYPE):
+            rows = [tuple(int(x) for x in r) for r in spans]
+            if any(len(r) != 5 or min(r) < 0 or max(r[0], r[1], r[3]) >= 1 << 32 for r in rows):
+                raise ValueError("a span is (first_query, num_queries, length, causal, first_block), none negative")
+            spans = np.array(rows, SPAN_DTYPE)
+        spans = np.ascontiguousarray(spans)
+        b = np.asarray(blocks)
+        if b.ndim != 1 or spans.ndim != 1:
+            raise ValueError("spans and blocks are one-dimensional")
+        if b.dtype != np.uint32:
+            if b.size and (b.dtype.kind not in "iu" or int(b.min()) < 0 or int(b.max()) >= 1 << 32):
+                raise ValueError("block ids must be whole numbers in 0..2^32-1")
+            b = b.astype(np.uint32)
+        b = np.ascontiguousarray(b)
+        if not 0 <= int(num_queries) < 1 << 32:
+            raise ValueError("num_queries must be in 0..2^32-1")
+        self.num_queries = self.workspace_bytes = 0
+        self.cache._check(L.ps_kv_plan_set(h, int(num_queries), spans.ctypes.data if spans.size else None, spans.size,
+                                           b.ctypes.data if b.size else None, b.size))
+        n = ctypes.c_uint64()
+        self.cache._check(L.ps_kv_plan_workspace(h, ctypes.byref(n)))
+        self.num_queries, self.workspace_bytes = int(num_queries), n.value
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self.cache._lib.ps_kv_plan_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
