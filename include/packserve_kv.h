@@ -82,8 +82,8 @@ PS_API ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v
                              void* stream);
 
 /* Read n tokens back: k and v (of one type, rounded to it) receive the values that the cache holds at
- * slots[t]; a negative slot gives zeros, a slot past the cache zeros and a report.  The paper has no
- * counterpart.  Errors: as ps_kv_write. */
+ * slots[t]; a negative slot gives zeros, a slot past the cache zeros and a report.
+ * The paper has no counterpart.  Errors: as ps_kv_write. */
 PS_API ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_rows* k, const ps_kv_rows* v,
                             void* stream);
 
@@ -109,8 +109,8 @@ PS_API ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_que
 PS_API ps_status ps_kv_plan_set(ps_kv_plan* plan, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
                                 const uint32_t* blocks, uint64_t num_blocks);
 
-/* Bytes of workspace that ps_kv_attend needs for the batch that is set (0 possible).  The paper has no
- * counterpart. */
+/* Bytes of workspace that ps_kv_attend needs for the batch that is set (0 possible).
+ * The paper has no counterpart. */
 PS_API ps_status ps_kv_plan_workspace(ps_kv_plan* plan, uint64_t* bytes);
 
 /* Attention of the plan's batch over the cache.  With z_ij = scale * q_i . k_j over the keys j of all spans
@@ -125,8 +125,8 @@ PS_API ps_status ps_kv_plan_workspace(ps_kv_plan* plan, uint64_t* bytes);
 PS_API ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,
                               float scale, void* workspace, uint64_t workspace_bytes, void* stream);
 
-/* Text of the last error of this cache's calls, its plans' among them ("" if none).  The paper has no
- * counterpart. */
+/* Text of the last error of this cache's calls, its plans' among them ("" if none).
+ * The paper has no counterpart. */
 PS_API const char* ps_kv_last_error(const ps_kv* kv);
 
 /* Release a plan: waits for the calls that read it.  NULL is accepted.  The paper has no counterpart. */
