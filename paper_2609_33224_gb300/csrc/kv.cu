@@ -124,11 +124,38 @@ ps_status store_args(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const 
 
 // ---- planning -----------------------------------------------------------------------------------------
 
+using pskv::kBlock;
+using pskv::kSmallRows;
+using pskv::kTileKeys;
+using pskv::kTileRows;
+
+// Where the tile kernel takes a span: from this many rows and keys on.
+constexpr uint32_t kTileLeastRows = 33;
+constexpr int64_t kTileLeastKeys = 256;
+
 // Rows of one tile and one head over a range of key blocks, before it is cut into pieces.
 struct Unit {
-  Piece p;         // block, key0: of the whole range
-  uint32_t group;  // its entry of the groups
+  Piece p;             // block, key0: of the whole range
+  uint32_t group;      // its entry of the groups
+  uint32_t tile_rows;  // rows of its partial results
 };
+
+Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t from, int64_t end, int step, int32_t climit,
+          uint32_t tile_rows, uint32_t group) {
+  Unit u{};
+  u.p.block = (uint32_t)(s.first_block + (uint64_t)from / kBlock);
+  u.p.nblocks = (uint32_t)((end - from + step - 1) / step);
+  u.p.key0 = (uint32_t)from;
+  u.p.end = (uint32_t)end;
+  u.p.climit = climit;
+  u.p.query0 = s.first_query;
+  u.p.row0 = r0;
+  u.p.nrows = (uint16_t)nr;
+  u.p.head = (uint16_t)h;
+  u.group = group;
+  u.tile_rows = tile_rows;
+  return u;
+}
 
 struct Layout {
   std::vector<Layer> layers;
@@ -188,34 +215,37 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     if (s.num_queries == 0 || s.length == 0) continue;
     const uint32_t rows = s.num_queries * g;
     const int64_t len = (int64_t)s.length;
-    Layer ly{s.first_query, (uint32_t)pskv::kSmallRows, (uint32_t)o.groups.size(), 0};
-    const uint32_t tiles = (rows + pskv::kSmallRows - 1) / pskv::kSmallRows;
-    o.layers.push_back(ly);
-    o.layer_queries.push_back(s.num_queries);
-    for (uint32_t t = 0; t < tiles; ++t) {
-      const uint32_t r0 = t * pskv::kSmallRows, nr = std::min<uint32_t>(rows - r0, pskv::kSmallRows);
-      int64_t end = len;
-      int32_t climit = pskv::kNoLimit;
-      if (s.causal) {
-        climit = (int32_t)(len - (int64_t)s.num_queries);
-        end = std::min<int64_t>(len, (int64_t)climit + (r0 + nr - 1) / g + 1);
+    const int32_t climit = s.causal ? (int32_t)(len - (int64_t)s.num_queries) : pskv::kNoLimit;
+
+    // Tiles take the keys that all their rows see; cut[t]: how many those are for tile t.
+    std::vector<int64_t> cut;
+    const uint32_t tile_rows = rows <= kTileRows / 2 ? kTileRows / 2 : kTileRows;
+    if (rows >= kTileLeastRows && len >= kTileLeastKeys) {
+      const uint32_t tiles = (rows + tile_rows - 1) / tile_rows;
+      o.layers.push_back(Layer{s.first_query, tile_rows, (uint32_t)o.groups.size(), 0});
+      o.layer_queries.push_back(s.num_queries);
+      for (uint32_t t = 0; t < tiles; ++t) {
+        const uint32_t r0 = t * tile_rows, nr = std::min(rows - r0, tile_rows);
+        int64_t c = len;
+        if (s.causal) c = std::max<int64_t>(0, (int64_t)climit + r0 / g + 1) / kBlock * kBlock;
+        if (c < kTileLeastKeys) c = 0;
+        cut.push_back(c);
+        for (uint32_t h = 0; h < H; ++h) {
+          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, (uint32_t)o.groups.size()));
+          o.groups.push_back(Group{0, 0});
+        }
       }
+      if (!s.causal) continue;
+    }
+    o.layers.push_back(Layer{s.first_query, (uint32_t)kSmallRows, (uint32_t)o.groups.size(), 0});
+    o.layer_queries.push_back(s.num_queries);
+    for (uint32_t r0 = 0; r0 < rows; r0 += kSmallRows) {
+      const uint32_t nr = std::min<uint32_t>(rows - r0, kSmallRows);
+      const int64_t from = cut.empty() ? 0 : cut[r0 / tile_rows];
+      const int64_t end = s.causal ? std::min<int64_t>(len, (int64_t)climit + (r0 + nr - 1) / g + 1) : len;
       for (uint32_t h = 0; h < H; ++h) {
-        const uint32_t gi = (uint32_t)o.groups.size();
+        if (end > from) o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, (uint32_t)o.groups.size()));
         o.groups.push_back(Group{0, 0});
-        if (end <= 0) continue;
-        Unit u{};
-        u.p.block = (uint32_t)s.first_block;
-        u.p.nblocks = (uint32_t)((end + pskv::kBlock - 1) / pskv::kBlock);
-        u.p.key0 = 0;
-        u.p.end = (uint32_t)end;
-        u.p.climit = climit;
-        u.p.query0 = s.first_query;
-        u.p.row0 = r0;
-        u.p.nrows = (uint16_t)nr;
-        u.p.head = (uint16_t)h;
-        u.group = gi;
-        o.row_units.push_back(u);
       }
     }
   }
@@ -237,7 +267,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
   }
 
   // pieces, and where their partial results go
-  auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, uint32_t tile_rows) {
+  auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
       const Piece& p = units[i].p;
@@ -253,14 +283,18 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
       o.max_parts = std::max(o.max_parts, b - a);
       for (uint32_t k = a; k < b; ++k) {
         pieces[k].part_row = (uint32_t)o.part_rows;
-        o.part_rows += tile_rows;
+        o.part_rows += units[i].tile_rows;
       }
     }
   };
   std::vector<uint32_t> first;
   if (!o.row_units.empty()) {
     share_out(o.row_units, (uint32_t)pl.kv->sms * pskv::kRowWarps, 2, 2, 1, &o.row_pieces, &o.row_off, &first);
-    finish(o.row_units, o.row_pieces, first, pskv::kSmallRows);
+    finish(o.row_units, o.row_pieces, first);
+  }
+  if (!o.tile_units.empty()) {
+    share_out(o.tile_units, (uint32_t)pl.kv->sms, 2, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
+    finish(o.tile_units, o.tile_pieces, first);
   }
 
   // (query, head) pairs whose rows have something to join, or no key at all
@@ -430,6 +464,7 @@ ps_status ps_kv_create(const ps_kv_config* cfg, ps_kv** out) {
     e = cudaHostGetDevicePointer(&dev, kv->err_host, 0);
   }
   if (e == cudaSuccess) e = pskv::prepare_rows((int)kv->D, kv->fmt);
+  if (e == cudaSuccess) e = pskv::prepare_tiles((int)kv->D, kv->fmt);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   kv->err_dev = static_cast<uint32_t*>(dev);
   if (e != cudaSuccess) {
@@ -574,6 +609,7 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   const int D = (int)kv->D;
   cudaError_t e = cudaSuccess;
   if (pl->dev.row_workers) e = pskv::launch_rows(D, kv->fmt, a, pl->dev, s);
+  if (e == cudaSuccess && pl->dev.tile_ctas) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, s);
   if (e == cudaSuccess && pl->dev.njoin) e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev, s);
   if (!capturing) {  // also after a failed launch: the ones before it read the buffer
     const cudaError_t r = cudaEventRecord(b.used, s);

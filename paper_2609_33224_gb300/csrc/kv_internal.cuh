@@ -24,7 +24,7 @@ namespace pskv {
 
 constexpr int kBlock = PS_BLOCK_TOKENS;
 constexpr int kSmallRows = 16;   // rows of a tile of the row kernel (one m16 of mma.sync)
-constexpr int kTileRows = 256;   // rows of a tile of the tile kernel (two tcgen05 accumulators of 128)
+constexpr int kTileRows = 256;   // most rows of a tile of the tile kernel (two tcgen05 accumulators of 128)
 constexpr int kTileKeys = 128;   // keys of one step of the tile kernel
 constexpr int kExpBias = 127;
 constexpr int kExpMin = -110, kExpMax = 119, kExpNan = 255;
@@ -124,7 +124,9 @@ cudaError_t launch_write(int D, int fmt, int type, const StoreArgs& a, int sms, 
 cudaError_t launch_read(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
 cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
+cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
+cudaError_t prepare_tiles(int D, int fmt);
 constexpr int kRowWarps = 8;  // workers (warps) of a CTA of the row kernel
 
 // ---- PTX ----------------------------------------------------------------------------------------------
@@ -156,19 +158,20 @@ __device__ __forceinline__ uint64_t now_ns() {
   return t;
 }
 // Waits for a phase, one second at most (the limit of the scheduler's waits); false: it gave up.
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+  if (mbar_try(bar, parity)) return true;
   const uint64_t t0 = now_ns();
+#pragma unroll 1
   for (;;) {
-    for (int i = 0; i < 256; ++i)
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
       if (mbar_try(bar, parity)) return true;
     if (now_ns() - t0 > 1000000000ull) return false;
   }
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-#pragma unroll 1
-  for (int i = 0; i < 16; ++i)
-    if (mbar_try(bar, parity)) return true;
-  return mbar_wait_slow(bar, parity);
+// The same for a whole warp, which goes on or gives up together.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+  return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity)) != 0;
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),

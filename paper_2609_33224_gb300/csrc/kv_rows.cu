@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 
     for (uint32_t bi = 0; bi < pc.nblocks; ++bi) {
       const uint32_t rec = ring + st * kRec;
-      if (!mbar_wait(bar + st * 8, phase)) {
+      if (!mbar_wait_warp(bar + st * 8, phase)) {
         if (lane == 0) atomicOr_system(a.err, kErrWait);
         while (--in_flight) {  // the copies behind it write this warp's memory: they are waited for too
           if (++st == kStages) {

@@ -1,0 +1,527 @@
+// Attention of many rows over the same keys (a prefix that a batch shares, new tokens over a cached prefix):
+// the tile kernel, on the 5th-generation tensor cores.
+//
+// A CTA holds 256 rows of one span and key/value head as two tiles of 128 and walks its keys in steps of 128.
+// Per step and tile: S = Q K^T into tensor memory (one thread issues tcgen05.mma, operands in shared memory),
+// a warpgroup, one thread per row, reads S, keeps the row's running maximum and sum, and writes the
+// probabilities back over S in 16 bits, and O += P V with P read from tensor memory.  The tiles take turns:
+// while one tile's softmax runs, the tensor cores work on the other's products.  O is rescaled in tensor
+// memory, by the threads that own its rows, only when a row's maximum has grown by more than 2^8.
+// Tensor memory (512 columns): S/P of tile 0 and 1, O of tile 0 and 1.
+//
+// The cache's 16-bit records lie in memory in the swizzled order that the tensor cores read, so keys and
+// values arrive by plain bulk copies into a ring.  fp8 records land in a ring of their own and a fourth
+// warpgroup turns them into bf16 (exactly, scales included) in the operands' ring.
+//
+// Keys here are seen by all rows: the plan gives the ends of causal spans to the row kernel.  Only a span's
+// last step can be partial; its scores past the end are masked, and its value rows past the end zeroed.
+//
+// Bound by the tensor cores for full tiles: 4 * D multiply-adds a row and key, and, near that, the
+// exponentials: one per row and key.  Work is cut into equal shares per SM; each share walks its pieces.
+#include "kv_internal.cuh"
+
+namespace pskv {
+namespace {
+
+constexpr int kRowsPerTile = 128;
+
+template <int D, int FMT>
+struct Cfg {
+  static constexpr bool kFp8 = FMT == PS_KV_FP8, kFp16 = FMT == PS_KV_FP16;
+  static constexpr int kSlot = kTileKeys * D * 2;               // keys or values of a step as operands
+  static constexpr int kQ = kRowsPerTile * D * 2;               // one tile's queries
+  static constexpr int kRec = record_bytes(D, FMT), kHalf = half_bytes(D, FMT);
+  static constexpr int kRaw = kFp8 ? 8 * kRec : 0;              // a step's fp8 records
+  static constexpr int kRaws = kFp8 ? (D == 128 ? 2 : 4) : 0;
+  static constexpr int kSlots = kFp8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 11);
+  static constexpr int kWarps = kFp8 ? 16 : 12;
+  static constexpr int kRegSoft = kFp8 ? 192 : 208, kRegRest = kFp8 ? 64 : 88;
+  static constexpr int kSmem = 2 * kQ + kSlots * kSlot + kRaws * kRaw + 1024;  // 1024: alignment
+};
+static_assert(192 * 256 + 64 * 256 <= 65536 && 208 * 256 + 88 * 128 <= 384 * 168, "register split");
+
+struct Bars {
+  uint64_t full[12], empty[12];  // operand ring
+  uint64_t raw_full[4], raw_empty[4];
+  uint64_t q_ready[2], s_full[2], p_ready[2], o_done[2], drain;
+  uint32_t tmem;
+};
+
+// ---- tcgen05
+__device__ __forceinline__ void tc_alloc(uint32_t dst, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tc_relinquish() {
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_dealloc(uint32_t addr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// D[tmem] (+)= A[smem] B[smem]
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] B[smem]
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+
+#define TC_R8(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
+#define TC_I8(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3]), "r"(a[i + 4]), "r"(a[i + 5]), "r"(a[i + 6]), "r"(a[i + 7])
+
+// 32 columns of the calling warp's 32 lanes, one lane a thread
+__device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : TC_R8(r, 0), TC_R8(r, 8), TC_R8(r, 16), TC_R8(r, 24)
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : TC_R8(r, 0), TC_R8(r, 8)
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TC_I8(r, 0),
+      TC_I8(r, 8), "r"(addr)
+      : "memory");
+}
+
+// Shared-memory operand descriptor, 128-byte swizzle.  Keys and queries (K-major): sbo = bytes between groups of
+// 8 rows.  Values (MN-major): lbo = bytes between panels of 64 columns, sbo = bytes between groups of 8 keys.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+// f32 accumulator, M = 128, N, A and B of one 16-bit type; mn_b: B is MN-major
+__device__ __forceinline__ constexpr uint32_t instruction(bool fp16, int n, bool mn_b) {
+  return (1u << 4) | (fp16 ? 0u : (1u << 7) | (1u << 10)) | (mn_b ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) |
+         ((128u >> 4) << 24);
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(const AttnArgs a, const PlanDev p) {
+  using C = Cfg<D, FMT>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) Bars bars;
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_smem = smem, ring = smem + 2 * C::kQ, raw_ring = ring + C::kSlots * C::kSlot;
+  auto full = [&](uint32_t i) { return smem_u32(&bars.full[i]); };
+  auto empty = [&](uint32_t i) { return smem_u32(&bars.empty[i]); };
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kSlots; ++i) {
+      mbar_init(full(i), C::kFp8 ? 128 : 1);
+      mbar_init(empty(i), 1);
+    }
+    for (int i = 0; i < C::kRaws; ++i) {
+      mbar_init(smem_u32(&bars.raw_full[i]), 1);
+      mbar_init(smem_u32(&bars.raw_empty[i]), 128);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&bars.q_ready[t]), 128);
+      mbar_init(smem_u32(&bars.s_full[t]), 1);
+      mbar_init(smem_u32(&bars.p_ready[t]), 128);
+      mbar_init(smem_u32(&bars.o_done[t]), 1);
+    }
+    mbar_init(smem_u32(&bars.drain), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    tc_alloc(smem_u32(&bars.tmem), 512);
+    tc_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars.tmem;
+  const uint32_t first = p.tile_off[blockIdx.x], last = p.tile_off[blockIdx.x + 1];
+
+  if (warp < 8) {
+    // ================= softmax: warpgroup t owns tile t, thread r its row r =================
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegSoft));
+    const uint32_t t = warp / 4, r = threadIdx.x % 128;
+    const uint32_t s_addr = tmem + t * 128 + ((warp % 4) * 32 << 16);
+    const uint32_t o_addr = tmem + 256 + t * 128 + ((warp % 4) * 32 << 16);
+    const float sc = fmaxf(fabsf(a.scale_log2), 1.2e-38f);  // a scale of 0 still sends masked scores to -inf
+    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    uint32_t steps = 0, done = 0;  // phases of s_full; of o_done
+    bool alive = true;
+    for (uint32_t pi = first; alive && pi < last; ++pi) {
+      const Piece pc = p.tile_pieces[pi];
+      if (t * kRowsPerTile >= pc.nrows) continue;
+      const uint32_t row = pc.row0 + t * kRowsPerTile + r;
+      const bool valid = t * kRowsPerTile + r < pc.nrows;
+      const uint32_t query = pc.query0 + row / a.group, head = pc.head * a.group + row % a.group;
+      {
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)query * a.q_tok + (int64_t)head * a.q_head);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          uint4 w = valid ? src[c] : make_uint4(0, 0, 0, 0);
+          w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_smem + t * C::kQ + chunk_offset<D, false>(r, c)),
+                       "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
+                       : "memory");
+        }
+      }
+      fence_async_shared();
+      mbar_arrive(smem_u32(&bars.q_ready[t]));
+
+      float m = -INFINITY, l = 0.0f;
+      for (uint32_t j = 0; j < pc.nblocks; ++j) {
+        if (!mbar_wait_warp(smem_u32(&bars.s_full[t]), steps & 1)) {
+          alive = false;
+          break;
+        }
+        ++steps;
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tc_ld32(s[c], s_addr + 32 * c);
+        tc_wait_ld();
+        const uint32_t left = pc.end - (pc.key0 + j * kTileKeys);
+        if (left < (uint32_t)kTileKeys) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if ((uint32_t)(32 * c + i) >= left) s[c][i] = 0xFF800000u;
+        }
+        float x0 = -INFINITY, x1 = -INFINITY, x2 = -INFINITY, x3 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          x0 = fmaxf(x0, __uint_as_float(s[0][i]));
+          x1 = fmaxf(x1, __uint_as_float(s[1][i]));
+          x2 = fmaxf(x2, __uint_as_float(s[2][i]));
+          x3 = fmaxf(x3, __uint_as_float(s[3][i]));
+        }
+        const float x = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)) * sc;
+        const bool grow = x > m + 8.0f;
+        if (__any_sync(0xFFFFFFFFu, grow)) {
+          const float n = fmaxf(m, x), f = n == m ? 1.0f : ex2(m - n);
+          m = n;
+          l *= f;
+          if (j > 0) {  // the product before this step's scores is done: it was issued, and so finished, first
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t o[16];
+              tc_ld16(o, o_addr + 16 * c);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tc_st16(o_addr + 16 * c, o);
+            }
+          }
+        }
+        const float u = m == -INFINITY ? 0.0f : m;
+        float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float p0 = ex2(fmaf(__uint_as_float(s[c][i]), sc, -u));
+            const float p1 = ex2(fmaf(__uint_as_float(s[c][i + 1]), sc, -u));
+            l0 += p0;
+            l1 += p1;
+            pk[i / 2] = pack2<C::kFp16>(p0, p1);
+          }
+          tc_st16(s_addr + 16 * c, pk);
+        }
+        l += l0 + l1;
+        tc_wait_st();
+        tc_fence_before();
+        mbar_arrive(smem_u32(&bars.p_ready[t]));
+      }
+      if (!alive || !mbar_wait_warp(smem_u32(&bars.o_done[t]), done & 1)) {
+        alive = false;
+        break;
+      }
+      ++done;
+      tc_fence_after();
+      const bool direct = pc.part_row == kDirect;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      const uint64_t at = (uint64_t)pc.part_row + t * kRowsPerTile + r;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        tc_ld32(o, o_addr + 32 * c);
+        tc_wait_ld();
+        if (!valid) continue;
+        if (direct) {
+          uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)query * a.o_tok + (int64_t)head * a.o_head + 32 * c);
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              w[k] = pack2<C::kFp16>(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
+            dst[i / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>(a.part + at * D + 32 * c);
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) dst[i / 4] = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+      }
+      if (valid) {
+        if (!direct)
+          a.part_ml[at] = make_float2(m, l);
+        else if (a.lse)
+          a.lse[(uint64_t)query * a.kv_heads * a.group + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      }
+      tc_fence_before();  // the reads of O before the next piece's products, which p_ready orders
+    }
+    if (!alive && r == 0) atomicOr_system(a.err, kErrWait);
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
+    if (warp == 8) {
+      // ================= copies: a step's keys, then its values (fp8: its records) =================
+      uint32_t n = 0, ids = 0;  // slots (fp8: raw stages) filled
+      constexpr uint32_t kN = C::kFp8 ? (C::kRaws ? C::kRaws : 1) : C::kSlots;
+      bool alive = true;
+      for (uint32_t pi = first; alive && pi < last; ++pi) {
+        const Piece* pp = p.tile_pieces + pi;
+        const uint32_t steps = pp->nblocks, block = pp->block, head = pp->head, key0 = pp->key0, end = pp->end;
+        const uint32_t nb = (end - key0 + kBlock - 1) / kBlock;  // blocks from here to the span's end
+        for (uint32_t j = 0; alive && j < steps; ++j) {
+          if ((j & 3u) == 0) ids = p.blocks[block + min(j * 8 + lane, nb - 1)];
+          const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, (j & 3u) * 8 + (lane & 7u));
+          const uint32_t live = min(nb - j * 8, 8u);
+          const uint8_t* rec = a.pool + ((uint64_t)id * a.kv_heads + head) * C::kRec;
+          for (uint32_t part = 0; part < (C::kFp8 ? 1u : 2u); ++part, ++n) {
+            const uint32_t at = n % kN;
+            const uint32_t fb = C::kFp8 ? smem_u32(&bars.raw_full[at % 4]) : full(at);
+            const uint32_t eb = C::kFp8 ? smem_u32(&bars.raw_empty[at % 4]) : empty(at);
+            if (n >= kN && !mbar_wait_warp(eb, (n / kN - 1) & 1)) {
+              alive = false;
+              break;
+            }
+            constexpr uint32_t bytes = C::kFp8 ? C::kRec : C::kHalf;
+            if (lane == 0) mbar_expect(fb, live * bytes);
+            __syncwarp();
+            if (lane < live)
+              bulk_load((C::kFp8 ? raw_ring + at * C::kRaw : ring + at * C::kSlot) + lane * bytes, rec + part * C::kHalf, bytes, fb);
+          }
+        }
+      }
+      for (uint32_t i = n > kN ? n - kN : 0; i < n; ++i)  // no copy is left in flight
+        alive &= mbar_wait_warp(C::kFp8 ? smem_u32(&bars.raw_full[i % kN % 4]) : full(i % kN), (i / kN) & 1);
+      if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
+    } else if (warp == 9) {
+      // ================= products: the whole warp follows, one lane issues =================
+      constexpr uint32_t id_s = instruction(C::kFp16, kTileKeys, false), id_o = instruction(C::kFp16, D, true);
+      uint32_t n = 0;          // slots taken
+      uint32_t p_seen[2] = {0, 0}, q_seen[2] = {0, 0};
+      bool alive = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (alive && !mbar_wait_warp(bar, parity)) alive = false;
+        return alive;
+      };
+      auto scores = [&](uint32_t t, uint32_t slot) {
+        const uint64_t qd = operand(q_smem + t * C::kQ, 16, 16 * D), kd = operand(ring + slot * C::kSlot, 16, 16 * D);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t off = ((k / 4) * 1024 + (k % 4) * 32) >> 4;
+          tc_mma_ss(tmem + t * 128, qd + off, kd + off, id_s, k > 0);
+        }
+      };
+      auto values = [&](uint32_t t, uint32_t slot, bool acc) {
+        const uint64_t vd = operand(ring + slot * C::kSlot, 1024, 16 * D);
+#pragma unroll
+        for (int k = 0; k < kTileKeys / 16; ++k)
+          tc_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + ((k * 32 * D) >> 4), id_o, acc || k > 0);
+      };
+      for (uint32_t pi = first; alive && pi < last; ++pi) {
+        const Piece* pp = p.tile_pieces + pi;
+        const uint32_t steps = pp->nblocks, key0 = pp->key0, end = pp->end;
+        const uint32_t tiles = pp->nrows > kRowsPerTile ? 2 : 1;
+        // ring order: keys 0, values 0, keys 1, values 1, ...: step j's keys are slot n0 + 2j, values n0 + 2j + 1
+        const uint32_t n0 = n;
+        auto slot = [&](uint32_t i) { return (n0 + i) % C::kSlots; };
+        auto parity = [&](uint32_t i) { return ((n0 + i) / C::kSlots) & 1u; };
+        wait(full(slot(0)), parity(0));
+        for (uint32_t t = 0; alive && t < tiles; ++t) {
+          if (!wait(smem_u32(&bars.q_ready[t]), q_seen[t] & 1)) break;
+          ++q_seen[t];
+          tc_fence_after();
+          if (lane == 0) {
+            scores(t, slot(0));
+            if (t == tiles - 1) tc_commit(empty(slot(0)));
+            tc_commit(smem_u32(&bars.s_full[t]));
+          }
+          __syncwarp();
+        }
+        for (uint32_t j = 0; alive && j < steps; ++j) {
+          const bool more = j + 1 < steps;
+          if (!wait(full(slot(2 * j + 1)), parity(2 * j + 1))) break;
+          const uint32_t left = end - (key0 + j * kTileKeys);
+          if (!C::kFp8 && left < (uint32_t)kTileKeys) {
+            // value rows past the end: what other tokens or earlier steps left there
+            const uint32_t v = ring + slot(2 * j + 1) * C::kSlot;
+            for (uint32_t i = left * (D / 8) + lane; i < kTileKeys * (D / 8); i += 32) {
+              const uint32_t tok = i / (D / 8), c = i % (D / 8);
+              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + chunk_offset<D, false>(tok, c)), "r"(0) : "memory");
+            }
+            fence_async_shared();
+            __syncwarp();
+          }
+          if (more && !wait(full(slot(2 * j + 2)), parity(2 * j + 2))) break;
+          for (uint32_t t = 0; alive && t < tiles; ++t) {
+            if (!wait(smem_u32(&bars.p_ready[t]), p_seen[t] & 1)) break;
+            ++p_seen[t];
+            tc_fence_after();
+            if (lane == 0) {
+              values(t, slot(2 * j + 1), j > 0);
+              if (t == tiles - 1) tc_commit(empty(slot(2 * j + 1)));
+              if (more) {
+                scores(t, slot(2 * j + 2));
+                if (t == tiles - 1) tc_commit(empty(slot(2 * j + 2)));
+                tc_commit(smem_u32(&bars.s_full[t]));
+              } else {
+                tc_commit(smem_u32(&bars.o_done[t]));
+              }
+            }
+            __syncwarp();
+          }
+        }
+        n = n0 + 2 * steps;
+      }
+      if (lane == 0) tc_commit(smem_u32(&bars.drain));
+      __syncwarp();
+      alive &= mbar_wait_warp(smem_u32(&bars.drain), 0);  // nothing is left in flight when tensor memory is freed
+      if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
+    }
+  } else {
+    // ================= fp8: records to operands, a thread a token =================
+    if constexpr (C::kFp8) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
+      const uint32_t tok = threadIdx.x % 128;
+      uint32_t n = 0, raws = 0;
+      bool alive = true;
+      for (uint32_t pi = first; alive && pi < last; ++pi) {
+        const Piece* pp = p.tile_pieces + pi;
+        const uint32_t steps = pp->nblocks, key0 = pp->key0, end = pp->end;
+        for (uint32_t j = 0; alive && j < steps; ++j, ++raws) {
+          const uint32_t rs = raws % C::kRaws;
+          if (!mbar_wait_warp(smem_u32(&bars.raw_full[rs]), (raws / C::kRaws) & 1)) {
+            alive = false;
+            break;
+          }
+          const bool live = key0 + j * kTileKeys + tok < end;
+          const uint32_t rec = raw_ring + rs * C::kRaw + (tok / kBlock) * C::kRec;
+          for (uint32_t part = 0; part < 2; ++part, ++n) {
+            const uint32_t at = n % C::kSlots;
+            if (n >= (uint32_t)C::kSlots && !mbar_wait_warp(empty(at), (n / C::kSlots - 1) & 1)) {
+              alive = false;
+              break;
+            }
+            uint32_t e = kExpBias;
+            if (live) {
+              uint16_t b;
+              asm volatile("ld.shared.u8 %0, [%1];" : "=h"(b) : "r"(rec + 2 * C::kHalf + part * kBlock + tok % kBlock) : "memory");
+              e = b;
+            }
+            // value = code * 2^120 * 2^(e - 127); the second factor as a bf16, a NaN for a row with a NaN
+            const uint32_t f1 = e == (uint32_t)kExpNan ? 0x7FC0u : e << 7;
+            const uint32_t f = f1 | (f1 << 16);
+            const uint32_t dst = ring + at * C::kSlot;
+#pragma unroll 2
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t w[4] = {0, 0, 0, 0}, o[8];
+              if (live)
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                             : "r"(rec + part * C::kHalf + chunk_offset<D, true>(tok % kBlock, c))
+                             : "memory");
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                o[2 * i] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x1404));
+                o[2 * i + 1] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x3424));
+              }
+#pragma unroll
+              for (int i = 0; i < 8; ++i) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(o[i]), "r"(f));
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + chunk_offset<D, false>(tok, 2 * c + i)),
+                             "r"(o[4 * i]), "r"(o[4 * i + 1]), "r"(o[4 * i + 2]), "r"(o[4 * i + 3])
+                             : "memory");
+            }
+            fence_async_shared();
+            mbar_arrive(full(at));
+          }
+          if (alive) mbar_arrive(smem_u32(&bars.raw_empty[rs]));
+        }
+      }
+      if (!alive && tok == 0) atomicOr_system(a.err, kErrWait);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) tc_dealloc(tmem, 512);
+}
+
+template <int D, int FMT>
+cudaError_t prepare_one() {
+  // setmaxnreg hands out what the launch was given: fewer registers than the split adds up to would wait for ever
+  cudaFuncAttributes at{};
+  cudaError_t e = cudaFuncGetAttributes(&at, tiles_kernel<D, FMT>);
+  if (e != cudaSuccess) return e;
+  const int threads = Cfg<D, FMT>::kWarps * 32;
+  if (at.numRegs * threads < 256 * Cfg<D, FMT>::kRegSoft + (threads - 256) * Cfg<D, FMT>::kRegRest)
+    return cudaErrorInvalidKernelImage;
+  return cudaFuncSetAttribute(tiles_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, FMT>::kSmem);
+}
+template <int D, int FMT>
+cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+  tiles_kernel<D, FMT><<<p.tile_ctas, Cfg<D, FMT>::kWarps * 32, Cfg<D, FMT>::kSmem, s>>>(a, p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t prepare_tiles(int D, int fmt) {
+  if (D == 128)
+    return fmt == PS_KV_BF16   ? prepare_one<128, PS_KV_BF16>()
+           : fmt == PS_KV_FP16 ? prepare_one<128, PS_KV_FP16>()
+                               : prepare_one<128, PS_KV_FP8>();
+  return fmt == PS_KV_BF16   ? prepare_one<64, PS_KV_BF16>()
+         : fmt == PS_KV_FP16 ? prepare_one<64, PS_KV_FP16>()
+                             : prepare_one<64, PS_KV_FP8>();
+}
+
+cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+  if (D == 128)
+    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, s)
+           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, s)
+                               : launch_one<128, PS_KV_FP8>(a, p, s);
+  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, s)
+         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, s)
+                             : launch_one<64, PS_KV_FP8>(a, p, s);
+}
+
+}  // namespace pskv
