@@ -293,7 +293,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     finish(o.row_units, o.row_pieces, first);
   }
   if (!o.tile_units.empty()) {
-    share_out(o.tile_units, (uint32_t)pl.kv->sms, 2, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
+    share_out(o.tile_units, (uint32_t)pl.kv->sms, 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
     finish(o.tile_units, o.tile_pieces, first);
   }
 

@@ -43,7 +43,7 @@ static_assert(192 * 256 + 64 * 256 <= 65536 && 208 * 256 + 88 * 128 <= 384 * 168
 struct Bars {
   uint64_t full[12], empty[12];  // operand ring
   uint64_t raw_full[4], raw_empty[4];
-  uint64_t q_ready[2], s_full[2], p_ready[2], o_done[2], drain;
+  uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], drain;
   uint32_t tmem;
 };
 
@@ -108,6 +108,34 @@ __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16]) 
       : "memory");
 }
 
+// Two floats in a register pair
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float& lo, float& hi) {
+  uint32_t a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(x));
+  lo = __uint_as_float(a);
+  hi = __uint_as_float(b);
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // Shared-memory operand descriptor, 128-byte swizzle.  Keys and queries (K-major): sbo = bytes between groups of
 // 8 rows.  Values (MN-major): lbo = bytes between panels of 64 columns, sbo = bytes between groups of 8 keys.
 __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_t sbo) {
@@ -143,7 +171,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&bars.q_ready[t]), 128);
       mbar_init(smem_u32(&bars.s_full[t]), 1);
-      mbar_init(smem_u32(&bars.p_ready[t]), 128);
+      mbar_init(smem_u32(&bars.p_ready[t][0]), 128);
+      mbar_init(smem_u32(&bars.p_ready[t][1]), 128);
       mbar_init(smem_u32(&bars.o_done[t]), 1);
     }
     mbar_init(smem_u32(&bars.drain), 1);
@@ -176,13 +205,23 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       const bool valid = t * kRowsPerTile + r < pc.nrows;
       const uint32_t query = pc.query0 + row / a.group, head = pc.head * a.group + row % a.group;
       {
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + (int64_t)query * a.q_tok + (int64_t)head * a.q_head);
+        // a warp's 32 rows, each row's chunks by neighbouring lanes
+        const int64_t mine = (int64_t)query * a.q_tok + (int64_t)head * a.q_head;
+        constexpr int kLanes = D / 8, kAt = 32 / kLanes;
+        const uint32_t c = lane % kLanes;
+        uint4 w[32 / kAt];
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          uint4 w = valid ? src[c] : make_uint4(0, 0, 0, 0);
-          w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
-          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_smem + t * C::kQ + chunk_offset<D, false>(r, c)),
-                       "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
+        for (int i = 0; i < 32 / kAt; ++i) {
+          const int from = i * kAt + lane / kLanes;
+          const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, from);
+          const bool ok = __shfl_sync(0xFFFFFFFFu, (int)valid, from) != 0;
+          w[i] = ok ? *reinterpret_cast<const uint4*>(a.q + at + 8 * c) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 32 / kAt; ++i) {
+          const uint32_t to = (r & ~31u) + i * kAt + lane / kLanes;
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_smem + t * C::kQ + chunk_offset<D, false>(to, c)),
+                       "r"(w[i].x ^ flip), "r"(w[i].y ^ flip), "r"(w[i].z ^ flip), "r"(w[i].w ^ flip)
                        : "memory");
         }
       }
@@ -209,15 +248,15 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             for (int i = 0; i < 32; ++i)
               if ((uint32_t)(32 * c + i) >= left) s[c][i] = 0xFF800000u;
         }
-        float x0 = -INFINITY, x1 = -INFINITY, x2 = -INFINITY, x3 = -INFINITY;
+        float x4[4];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          x0 = fmaxf(x0, __uint_as_float(s[0][i]));
-          x1 = fmaxf(x1, __uint_as_float(s[1][i]));
-          x2 = fmaxf(x2, __uint_as_float(s[2][i]));
-          x3 = fmaxf(x3, __uint_as_float(s[3][i]));
+        for (int c = 0; c < 4; ++c) {
+          x4[c] = max3(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]), __uint_as_float(s[c][2]));
+#pragma unroll
+          for (int i = 3; i < 31; i += 2) x4[c] = max3(x4[c], __uint_as_float(s[c][i]), __uint_as_float(s[c][i + 1]));
+          x4[c] = fmaxf(x4[c], __uint_as_float(s[c][31]));
         }
-        const float x = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3)) * sc;
+        const float x = max3(fmaxf(x4[0], x4[1]), x4[2], x4[3]) * sc;
         const bool grow = x > m + 8.0f;
         if (__any_sync(0xFFFFFFFFu, grow)) {
           const float n = fmaxf(m, x), f = n == m ? 1.0f : ex2(m - n);
@@ -236,24 +275,33 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           }
         }
         const float u = m == -INFINITY ? 0.0f : m;
-        float l0 = 0.0f, l1 = 0.0f;
+        const uint64_t sc2 = pair(__float_as_uint(sc), __float_as_uint(sc));
+        const uint64_t u2 = pair(__float_as_uint(-u), __float_as_uint(-u));
+        uint64_t sum2 = 0;
+        // by halves, so that the product of the first half runs beside the exponentials of the second
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t pk[16];
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const float p0 = ex2(fmaf(__uint_as_float(s[c][i]), sc, -u));
-            const float p1 = ex2(fmaf(__uint_as_float(s[c][i + 1]), sc, -u));
-            l0 += p0;
-            l1 += p1;
-            pk[i / 2] = pack2<C::kFp16>(p0, p1);
+          for (int c = 2 * h; c < 2 * h + 2; ++c) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float p0, p1;
+              unpair(fma2(pair(s[c][i], s[c][i + 1]), sc2, u2), p0, p1);
+              p0 = ex2(p0);
+              p1 = ex2(p1);
+              sum2 = add2(sum2, pair(__float_as_uint(p0), __float_as_uint(p1)));
+              pk[i / 2] = pack2<C::kFp16>(p0, p1);
+            }
+            tc_st16(s_addr + 16 * c, pk);
           }
-          tc_st16(s_addr + 16 * c, pk);
+          tc_wait_st();
+          tc_fence_before();
+          mbar_arrive(smem_u32(&bars.p_ready[t][h]));
         }
+        float l0, l1;
+        unpair(sum2, l0, l1);
         l += l0 + l1;
-        tc_wait_st();
-        tc_fence_before();
-        mbar_arrive(smem_u32(&bars.p_ready[t]));
       }
       if (!alive || !mbar_wait_warp(smem_u32(&bars.o_done[t]), done & 1)) {
         alive = false;
@@ -264,27 +312,47 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       const bool direct = pc.part_row == kDirect;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const uint64_t at = (uint64_t)pc.part_row + t * kRowsPerTile + r;
+      // The queries are used up: their rows' shared memory takes the warp's 32 rows, half of their columns at a
+      // time, from which whole rows are stored by neighbouring lanes.
+      const uint32_t stage = q_smem + t * C::kQ + (warp % 4) * (32 * D * 2);
+      constexpr int kCols = D / 2, kChunks = kCols / 4;  // floats and 16-byte chunks of a row in one round
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tc_ld32(o, o_addr + 32 * c);
-        tc_wait_ld();
-        if (!valid) continue;
-        if (direct) {
-          uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)query * a.o_tok + (int64_t)head * a.o_head + 32 * c);
+      for (int half = 0; half < 2; ++half) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) {
-            uint32_t w[4];
+        for (int c = 0; c < kCols / 16; ++c) {
+          uint32_t o[16];
+          tc_ld16(o, o_addr + half * kCols + 16 * c);
+          tc_wait_ld();
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              w[k] = pack2<C::kFp16>(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
-            dst[i / 8] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        } else {
-          uint4* dst = reinterpret_cast<uint4*>(a.part + at * D + 32 * c);
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) dst[i / 4] = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          for (int i = 0; i < 4; ++i)
+            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * (kCols * 4) + (((4 * c + i) ^ (lane & 7u)) << 4)),
+                         "r"(o[4 * i]), "r"(o[4 * i + 1]), "r"(o[4 * i + 2]), "r"(o[4 * i + 3])
+                         : "memory");
         }
+        __syncwarp();
+        constexpr int kAt = 32 / kChunks;  // rows a round of the warp stores
+#pragma unroll 4
+        for (int i = 0; i < 32 / kAt; ++i) {
+          const uint32_t row_l = i * kAt + lane / kChunks, c = lane % kChunks;
+          uint32_t x[4];
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                       : "r"(stage + row_l * (kCols * 4) + ((c ^ (row_l & 7u)) << 4))
+                       : "memory");
+          const bool ok = __shfl_sync(0xFFFFFFFFu, (int)valid, row_l) != 0;
+          if (direct) {
+            const float f = __shfl_sync(0xFFFFFFFFu, inv, row_l);
+            const int64_t to = __shfl_sync(0xFFFFFFFFu, (int64_t)query * a.o_tok + (int64_t)head * a.o_head, row_l);
+            if (ok)
+              *reinterpret_cast<uint2*>(a.out + to + half * kCols + 4 * c) =
+                  make_uint2(pack2<C::kFp16>(__uint_as_float(x[0]) * f, __uint_as_float(x[1]) * f),
+                             pack2<C::kFp16>(__uint_as_float(x[2]) * f, __uint_as_float(x[3]) * f));
+          } else if (ok) {
+            const uint64_t to = at - lane + row_l;
+            *reinterpret_cast<uint4*>(a.part + to * D + half * kCols + 4 * c) = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        }
+        __syncwarp();
       }
       if (valid) {
         if (!direct)
@@ -348,10 +416,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           tc_mma_ss(tmem + t * 128, qd + off, kd + off, id_s, k > 0);
         }
       };
-      auto values = [&](uint32_t t, uint32_t slot, bool acc) {
+      auto values = [&](uint32_t t, uint32_t slot, int half, bool acc) {
         const uint64_t vd = operand(ring + slot * C::kSlot, 1024, 16 * D);
 #pragma unroll
-        for (int k = 0; k < kTileKeys / 16; ++k)
+        for (int k = 4 * half; k < 4 * half + 4; ++k)
           tc_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + ((k * 32 * D) >> 4), id_o, acc || k > 0);
       };
       for (uint32_t pi = first; alive && pi < last; ++pi) {
@@ -390,11 +458,15 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           }
           if (more && !wait(full(slot(2 * j + 2)), parity(2 * j + 2))) break;
           for (uint32_t t = 0; alive && t < tiles; ++t) {
-            if (!wait(smem_u32(&bars.p_ready[t]), p_seen[t] & 1)) break;
+            if (!wait(smem_u32(&bars.p_ready[t][0]), p_seen[t] & 1)) break;
+            tc_fence_after();
+            if (lane == 0) values(t, slot(2 * j + 1), 0, j > 0);
+            __syncwarp();
+            if (!wait(smem_u32(&bars.p_ready[t][1]), p_seen[t] & 1)) break;
             ++p_seen[t];
             tc_fence_after();
             if (lane == 0) {
-              values(t, slot(2 * j + 1), j > 0);
+              values(t, slot(2 * j + 1), 1, true);
               if (t == tiles - 1) tc_commit(empty(slot(2 * j + 1)));
               if (more) {
                 scores(t, slot(2 * j + 2));
