@@ -127,7 +127,6 @@ ps_status store_args(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const 
 using pskv::kBlock;
 using pskv::kSmallRows;
 using pskv::kTileKeys;
-using pskv::kTileRows;
 
 // Where the tile kernel takes a span: from this many rows and keys on.
 constexpr uint32_t kTileLeastRows = 33;
@@ -219,7 +218,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
 
     // Tiles take the keys that all their rows see; cut[t]: how many those are for tile t.
     std::vector<int64_t> cut;
-    const uint32_t tile_rows = rows <= kTileRows / 2 ? kTileRows / 2 : kTileRows;
+    const uint32_t full = (uint32_t)pskv::tile_rows_of((int)pl.kv->D), tile_rows = rows <= full / 2 ? full / 2 : full;
     if (rows >= kTileLeastRows && len >= kTileLeastKeys) {
       const uint32_t tiles = (rows + tile_rows - 1) / tile_rows;
       o.layers.push_back(Layer{s.first_query, tile_rows, (uint32_t)o.groups.size(), 0});
@@ -293,7 +292,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     finish(o.row_units, o.row_pieces, first);
   }
   if (!o.tile_units.empty()) {
-    share_out(o.tile_units, (uint32_t)pl.kv->sms, 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
+    share_out(o.tile_units, (uint32_t)(pl.kv->sms / pskv::tile_ctas_of((int)pl.kv->D)), 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
     finish(o.tile_units, o.tile_pieces, first);
   }
 
@@ -406,7 +405,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.row_ctas = std::min<uint32_t>(d.row_workers, (uint32_t)kv->sms);
   d.tile_pieces = reinterpret_cast<const Piece*>(b.dev + tp);
   d.tile_off = reinterpret_cast<const uint32_t*>(b.dev + to);
-  d.tile_ctas = o.tile_off.empty() ? 0 : (uint32_t)o.tile_off.size() - 1;
+  d.tile_workers = o.tile_off.empty() ? 0 : (uint32_t)o.tile_off.size() - 1;
   d.layers = reinterpret_cast<const Layer*>(b.dev + la);
   d.groups = reinterpret_cast<const Group*>(b.dev + gr);
   d.tok_off = reinterpret_cast<const uint32_t*>(b.dev + tk);
@@ -609,7 +608,7 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   const int D = (int)kv->D;
   cudaError_t e = cudaSuccess;
   if (pl->dev.row_workers) e = pskv::launch_rows(D, kv->fmt, a, pl->dev, s);
-  if (e == cudaSuccess && pl->dev.tile_ctas) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, s);
+  if (e == cudaSuccess && pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, s);
   if (e == cudaSuccess && pl->dev.njoin) e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev, s);
   if (!capturing) {  // also after a failed launch: the ones before it read the buffer
     const cudaError_t r = cudaEventRecord(b.used, s);

@@ -3,14 +3,13 @@
 //
 // A cache is an array of records, one per (block, key/value head), the heads of a block next to each other.
 // A record holds 16 tokens:
-//   16-bit formats: K then V, each 16 * D * 2 bytes as two groups of 8 tokens, a group as D / 64 panels of
-//     8 rows x 128 bytes, 16-byte chunk c of row r at chunk c ^ r.  That is the 128-byte-swizzled order that
-//     the tensor cores read from shared memory (keys: K-major, 8-row groups 16 * D bytes apart; values:
-//     MN-major, panels 1024 bytes apart), so a plain bulk copy of a record's half lands ready for use,
-//     and ldmatrix reads it without bank conflicts.
-//   fp8: K codes, V codes (16 rows of D bytes, 16-byte chunk c of row r at c ^ swz(r)), then the 16 scale
-//     exponents of K and the 16 of V (biased by 127; 255: the row holds a NaN), which fill one 32-byte
-//     sector: one copy brings a record with its scales.
+//   16-bit formats: K then V, each D / 64 panels of 64 columns; a panel is 16 rows x 128 bytes, 16-byte chunk
+//     c of row r at chunk c ^ (r % 8).  That is the 128-byte-swizzled order that the tensor cores read from
+//     shared memory (keys K-major, values MN-major, groups of 8 rows 1024 bytes apart), so plain bulk copies
+//     of panels land ready for use, and ldmatrix reads them without bank conflicts.
+//   fp8: K codes (16 rows of D bytes, chunk c of row r at c ^ swz(r)), V codes (D / 64 panels of 16 rows x
+//     64 bytes, chunks swizzled too), then the 16 scale exponents of K and the 16 of V (biased by 127; 255:
+//     the row holds a NaN), which fill one 32-byte sector: one copy brings a record with its scales.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -24,7 +23,10 @@ namespace pskv {
 
 constexpr int kBlock = PS_BLOCK_TOKENS;
 constexpr int kSmallRows = 16;   // rows of a tile of the row kernel (one m16 of mma.sync)
-constexpr int kTileRows = 256;   // most rows of a tile of the tile kernel (two tcgen05 accumulators of 128)
+// Rows of a tile of the tile kernel, two accumulators of 128 rows a CTA: with head_dim 128 a pair of CTAs
+// shares the keys and values.
+__host__ __device__ constexpr int tile_ctas_of(int D) { return D == 128 ? 2 : 1; }
+__host__ __device__ constexpr int tile_rows_of(int D) { return 256 * tile_ctas_of(D); }
 constexpr int kTileKeys = 128;   // keys of one step of the tile kernel
 constexpr int kExpBias = 127;
 constexpr int kExpMin = -110, kExpMax = 119, kExpNan = 255;
@@ -36,14 +38,17 @@ __host__ __device__ constexpr int record_bytes(int D, int fmt) {
 }
 __host__ __device__ constexpr int half_bytes(int D, int fmt) { return kBlock * D * (fmt == PS_KV_FP8 ? 1 : 2); }
 
-// byte offset of 16-byte chunk c of token t inside the K (or V) part of a record
-template <int D, bool FP8>
-__device__ __forceinline__ uint32_t chunk_offset(uint32_t t, uint32_t c) {
-  if (FP8) {
-    const uint32_t swz = D == 128 ? (t & 7u) : ((t >> 1) & 3u);
-    return t * D + ((c ^ swz) << 4);
-  }
-  return (t >> 3) * (8 * D * 2) + (c >> 3) * 1024 + (t & 7u) * 128 + (((c & 7u) ^ (t & 7u)) << 4);
+// byte offset of 16-byte chunk c of token t inside the K or V part of a 16-bit record
+__device__ __forceinline__ uint32_t offset16(uint32_t t, uint32_t c) {
+  return (c >> 3) * (kBlock * 128) + (t >> 3) * 1024 + (t & 7u) * 128 + (((c & 7u) ^ (t & 7u)) << 4);
+}
+// the same inside the K part of an fp8 record, and inside its V part
+template <int D>
+__device__ __forceinline__ uint32_t offset8k(uint32_t t, uint32_t c) {
+  return D == 128 ? t * 128 + ((c ^ (t & 7u)) << 4) : t * 64 + ((c ^ ((t >> 1) & 3u)) << 4);
+}
+__device__ __forceinline__ uint32_t offset8v(uint32_t t, uint32_t c) {
+  return (c >> 2) * (kBlock * 64) + t * 64 + (((c & 3u) ^ ((t >> 1) & 3u)) << 4);
 }
 
 // A piece of work of either attention kernel: a run of key blocks for the rows of one tile and one
@@ -83,7 +88,7 @@ struct PlanDev {
   uint32_t row_workers, row_ctas;
   const Piece* tile_pieces;
   const uint32_t* tile_off;
-  uint32_t tile_ctas;
+  uint32_t tile_workers;  // CTAs, or pairs of them
   const Layer* layers;
   const Group* groups;
   const uint32_t* tok_off;  // layers of query t: tok_layer[tok_off[t]] ..
@@ -157,8 +162,8 @@ __device__ __forceinline__ uint64_t now_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// Waits for a phase, one second at most (the limit of the scheduler's waits); false: it gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+// Waits for a phase, by default one second at most (the limit of the scheduler's waits); false: it gave up.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint64_t limit_ns = 1000000000ull) {
   if (mbar_try(bar, parity)) return true;
   const uint64_t t0 = now_ns();
 #pragma unroll 1
@@ -166,7 +171,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
 #pragma unroll 1
     for (int i = 0; i < 64; ++i)
       if (mbar_try(bar, parity)) return true;
-    if (now_ns() - t0 > 1000000000ull) return false;
+    if (now_ns() - t0 > limit_ns) return false;
   }
 }
 // The same for a whole warp, which goes on or gives up together.

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
           uint32_t r[4];  // keys 0-7 and 8-15 of chunk c, then of chunk c + 1
-          ldsm4<false>(r, rec + chunk_offset<D, true>(tok, c + (mi >> 1)));
+          ldsm4<false>(r, rec + offset8k<D>(tok, c + (mi >> 1)));
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             mma16816<false>(s[i & 1], qf[c + (i >> 1)], e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x1404)),
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 #pragma unroll
         for (int kc = 0; kc < D / 16; ++kc) {
           uint32_t r[4];  // keys 0-7: elements 0-7 and 8-15 of the step; keys 8-15: the same
-          ldsm4<false>(r, rec + chunk_offset<D, false>(tok, 2 * kc + (mi & 1)));
+          ldsm4<false>(r, rec + offset16(tok, 2 * kc + (mi & 1)));
           mma16816<kFp16>(s[0], qf[kc], r[0], r[1]);
           mma16816<kFp16>(s[1], qf[kc], r[2], r[3]);
         }
@@ -234,14 +234,14 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           bool odd = false;
 #pragma unroll 4
           for (int c = 0; c < D / 16; ++c) {
-            const uint4 w = lds128(rec + kHalf + chunk_offset<D, false>(tok, 2 * c + (lane & 1)));
+            const uint4 w = lds128(rec + kHalf + offset16(tok, 2 * c + (lane & 1)));
             odd |= not_finite2<kFp16>(w.x) | not_finite2<kFp16>(w.y) | not_finite2<kFp16>(w.z) | not_finite2<kFp16>(w.w);
           }
           const uint32_t odds = __ballot_sync(0xFFFFFFFFu, odd && !past);
           const bool out = past || ((odds >> (lane & ~1u)) & 3u) != 0;
           if (out) {
 #pragma unroll 4
-            for (int c = 0; c < D / 16; ++c) sts128_zero(rec + kHalf + chunk_offset<D, false>(tok, 2 * c + (lane & 1)));
+            for (int c = 0; c < D / 16; ++c) sts128_zero(rec + kHalf + offset16(tok, 2 * c + (lane & 1)));
           }
           bad = odds | (odds >> 1);  // bit 2 * key
           __syncwarp();
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
           uint32_t r[4];
-          ldsm4<true>(r, rec + kHalf + chunk_offset<D, true>(tok, c + (mi >> 1)));
+          ldsm4<true>(r, rec + kHalf + offset8v(tok, c + (mi >> 1)));
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
             // a chunk's 16 columns: tile 2c has the even ones, tile 2c + 1 the odd ones
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 #pragma unroll
         for (int j = 0; j < kTiles; j += 2) {
           uint32_t r[4];
-          ldsm4<true>(r, rec + kHalf + chunk_offset<D, false>(tok, j + (mi >> 1)));
+          ldsm4<true>(r, rec + kHalf + offset16(tok, j + (mi >> 1)));
           mma16816<kFp16>(acc[j], pf, r[0], r[1]);
           mma16816<kFp16>(acc[j + 1], pf, r[2], r[3]);
         }
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
               const bool sa = key0 + (int32_t)kk <= lim_a, sb = key0 + (int32_t)kk <= lim_b;
 #pragma unroll
               for (int j = 0; j < kTiles; ++j) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(vals + chunk_offset<D, false>(kk, j) + t4 * 4);
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(vals + offset16(kk, j) + t4 * 4);
                 const float v0 = value16<kFp16>((uint16_t)w), v1 = value16<kFp16>((uint16_t)(w >> 16));
                 if (sa) {
                   acc[j][0] += pa * v0;

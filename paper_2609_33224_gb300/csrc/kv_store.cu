@@ -134,7 +134,8 @@ __global__ void __launch_bounds__(256) write_kernel(StoreArgs a) {
     }
     uint8_t* rec = a.pool + ((uint64_t)(ok ? slot : 0) / kBlock * a.kv_heads + h) * kRec;
     const uint32_t tok = (uint32_t)((uint64_t)(ok ? slot : 0) % kBlock);
-    const uint32_t off = chunk_offset<D, kFp8>(tok, c);
+    const uint32_t ko = kFp8 ? offset8k<D>(tok, c) : offset16(tok, c);
+    const uint32_t vo = kHalf + (kFp8 ? offset8v(tok, c) : offset16(tok, c));
     if constexpr (kFp8) {
       float x[16];
       uint32_t ek, ev;
@@ -143,8 +144,8 @@ __global__ void __launch_bounds__(256) write_kernel(StoreArgs a) {
       v.floats(x);
       const uint4 cv = quantise<D>(x, &ev);
       if (ok) {
-        *reinterpret_cast<uint4*>(rec + off) = ck;
-        *reinterpret_cast<uint4*>(rec + kHalf + off) = cv;
+        *reinterpret_cast<uint4*>(rec + ko) = ck;
+        *reinterpret_cast<uint4*>(rec + vo) = cv;
         if (c == 0) {
           rec[2 * kHalf + tok] = (uint8_t)ek;
           rec[2 * kHalf + kBlock + tok] = (uint8_t)ev;
@@ -152,17 +153,17 @@ __global__ void __launch_bounds__(256) write_kernel(StoreArgs a) {
       }
     } else if (ok) {
       if constexpr (TYPE == FMT) {
-        *reinterpret_cast<uint4*>(rec + off) = k.w[0];
-        *reinterpret_cast<uint4*>(rec + kHalf + off) = v.w[0];
+        *reinterpret_cast<uint4*>(rec + ko) = k.w[0];
+        *reinterpret_cast<uint4*>(rec + vo) = v.w[0];
       } else {
         float x[8];
         Row<FMT, 8> o;
         k.floats(x);
         o.set(x);
-        *reinterpret_cast<uint4*>(rec + off) = o.w[0];
+        *reinterpret_cast<uint4*>(rec + ko) = o.w[0];
         v.floats(x);
         o.set(x);
-        *reinterpret_cast<uint4*>(rec + kHalf + off) = o.w[0];
+        *reinterpret_cast<uint4*>(rec + vo) = o.w[0];
       }
     }
   }
@@ -205,9 +206,8 @@ __global__ void __launch_bounds__(256) read_kernel(StoreArgs a) {
     if (ok) {
       const uint8_t* rec = a.pool + ((uint64_t)slot / kBlock * a.kv_heads + h) * kRec;
       const uint32_t tok = (uint32_t)((uint64_t)slot % kBlock);
-      const uint32_t off = chunk_offset<D, kFp8>(tok, c);
-      ck = *reinterpret_cast<const uint4*>(rec + off);
-      cv = *reinterpret_cast<const uint4*>(rec + kHalf + off);
+      ck = *reinterpret_cast<const uint4*>(rec + (kFp8 ? offset8k<D>(tok, c) : offset16(tok, c)));
+      cv = *reinterpret_cast<const uint4*>(rec + kHalf + (kFp8 ? offset8v(tok, c) : offset16(tok, c)));
       if (kFp8) {
         ek = rec[2 * kHalf + tok];
         ev = rec[2 * kHalf + kBlock + tok];

@@ -1,13 +1,19 @@
 // Attention of many rows over the same keys (a prefix that a batch shares, new tokens over a cached prefix):
 // the tile kernel, on the 5th-generation tensor cores.
 //
-// A CTA holds 256 rows of one span and key/value head as two tiles of 128 and walks its keys in steps of 128.
-// Per step and tile: S = Q K^T into tensor memory (one thread issues tcgen05.mma, operands in shared memory),
-// a warpgroup, one thread per row, reads S, keeps the row's running maximum and sum, and writes the
-// probabilities back over S in 16 bits, and O += P V with P read from tensor memory.  The tiles take turns:
-// while one tile's softmax runs, the tensor cores work on the other's products.  O is rescaled in tensor
-// memory, by the threads that own its rows, only when a row's maximum has grown by more than 2^8.
+// A worker walks the keys of one span and key/value head in steps of 128 for two tiles of rows.  Per step and
+// tile: S = Q K^T into tensor memory (one thread issues tcgen05.mma, operands in shared memory), a
+// warpgroup, one thread per row, reads S, keeps the row's running maximum and sum, and writes the
+// probabilities back over S in 16 bits, by halves, and O += P V with P read from tensor memory.  The tiles
+// take turns: while one tile's softmax runs, the tensor cores work on the other's products.  O is rescaled
+// in tensor memory, by the threads that own its rows, only when a row's maximum has grown by more than 2^8.
 // Tensor memory (512 columns): S/P of tile 0 and 1, O of tile 0 and 1.
+//
+// With head_dim 128 a worker is a pair of CTAs (cta_group::2): a tile is 256 rows, 128 in each CTA, and each
+// CTA holds half of every key tile (64 keys) and of every value tile (64 columns), which the tensor cores of
+// both read.  That halves what an SM draws from L2 and through its shared memory per row, and what it has to
+// turn from fp8 to bf16; one CTA alone, drawing 64 KB per step, was bound by that.  With head_dim 64 half a
+// value tile is narrower than a swizzled panel, and a worker is one CTA with tiles of 128 rows.
 //
 // The cache's 16-bit records lie in memory in the swizzled order that the tensor cores read, so keys and
 // values arrive by plain bulk copies into a ring.  fp8 records land in a ring of their own and a fourth
@@ -17,48 +23,87 @@
 // last step can be partial; its scores past the end are masked, and its value rows past the end zeroed.
 //
 // Bound by the tensor cores for full tiles: 4 * D multiply-adds a row and key, and, near that, the
-// exponentials: one per row and key.  Work is cut into equal shares per SM; each share walks its pieces.
+// exponentials: one per row and key.  Work is cut into equal shares per worker; each walks its pieces.
 #include "kv_internal.cuh"
 
 namespace pskv {
 namespace {
 
-constexpr int kRowsPerTile = 128;
-
 template <int D, int FMT>
 struct Cfg {
   static constexpr bool kFp8 = FMT == PS_KV_FP8, kFp16 = FMT == PS_KV_FP16;
-  static constexpr int kSlot = kTileKeys * D * 2;               // keys or values of a step as operands
-  static constexpr int kQ = kRowsPerTile * D * 2;               // one tile's queries
+  static constexpr int kCtas = tile_ctas_of(D);
+  static constexpr int kRows = 128 * kCtas;                      // rows of a tile
+  static constexpr int kKeys = kTileKeys / kCtas;                // keys of a step that a CTA holds
+  static constexpr int kCols = D / kCtas;                        // value columns that it holds: one panel
+  static constexpr int kSlot = kTileKeys * 128;                  // a CTA's keys, or values, of a step
+  static constexpr int kQ = 128 * D * 2;                         // a CTA's queries of one tile
   static constexpr int kRec = record_bytes(D, FMT), kHalf = half_bytes(D, FMT);
-  static constexpr int kRaw = kFp8 ? 8 * kRec : 0;              // a step's fp8 records
-  static constexpr int kRaws = kFp8 ? (D == 128 ? 2 : 4) : 0;
-  static constexpr int kSlots = kFp8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 11);
+  static constexpr int kRawK = kKeys * D, kRawV = kTileKeys * 64;  // a step's fp8 codes
+  static constexpr int kRaw = kFp8 ? kRawK + kRawV + 8 * 32 : 0;   // and exponents
+  static constexpr int kRaws = kFp8 ? 4 : 0;
+  static constexpr int kSlots = kFp8 ? 6 : 10;
   static constexpr int kWarps = kFp8 ? 16 : 12;
   static constexpr int kRegSoft = kFp8 ? 192 : 208, kRegRest = kFp8 ? 64 : 88;
   static constexpr int kSmem = 2 * kQ + kSlots * kSlot + kRaws * kRaw + 1024;  // 1024: alignment
+  static_assert(kSlot == kKeys * D * 2 && kCols == 64, "a slot holds keys or values");
 };
 static_assert(192 * 256 + 64 * 256 <= 65536 && 208 * 256 + 88 * 128 <= 384 * 168, "register split");
 
 struct Bars {
-  uint64_t full[12], empty[12];  // operand ring
+  uint64_t full[10], empty[10];  // operand ring
+  uint64_t peer_full[10];        // 16-bit pairs: the other CTA's part has arrived
   uint64_t raw_full[4], raw_empty[4];
-  uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], drain;
+  uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], tail_here, tail_done, drain;
   uint32_t tmem;
 };
 
 // ---- tcgen05
+// (CTAS: the cta_group)
+template <int CTAS>
 __device__ __forceinline__ void tc_alloc(uint32_t dst, uint32_t cols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+  if (CTAS == 2)
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n"
+                 "tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::"r"(dst), "r"(cols) : "memory");
+  else
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n"
+                 "tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::"r"(dst), "r"(cols) : "memory");
 }
-__device__ __forceinline__ void tc_relinquish() {
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-}
+template <int CTAS>
 __device__ __forceinline__ void tc_dealloc(uint32_t addr, uint32_t cols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+  if (CTAS == 2)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+  else
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
 }
+// Arrives on the barrier, of both CTAs of a pair, when the products issued so far are done.
+template <int CTAS>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  if (CTAS == 2)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"((uint16_t)3)
+                 : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Arrives on the barrier of the worker's first CTA.  What it publishes is read by the tensor cores (tensor memory
+// after tcgen05.wait, shared memory after a proxy fence), so the release stays at the default scope: one at the
+// scope of the cluster took 500 to 1400 cycles here, a third of a step.
+template <int CTAS>
+__device__ __forceinline__ void arrive_first(uint32_t bar) {
+  if (CTAS == 2)
+    asm volatile(
+        "{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [a];\n}\n" ::"r"(bar)
+        : "memory");
+  else
+    mbar_arrive(bar);
+}
+template <int CTAS>
+__device__ __forceinline__ void sync_worker() {
+  if (CTAS == 2)
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  else
+    __syncthreads();
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -66,20 +111,36 @@ __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sy
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // D[tmem] (+)= A[smem] B[smem]
+template <int CTAS>
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
-      : "memory");
+  if (CTAS == 2)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
 }
 // D[tmem] (+)= A[tmem] B[smem]
+template <int CTAS>
 __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
-      : "memory");
+  if (CTAS == 2)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+        : "memory");
 }
 
 #define TC_R8(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
@@ -136,16 +197,51 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Shared-memory operand descriptor, 128-byte swizzle.  Keys and queries (K-major): sbo = bytes between groups of
-// 8 rows.  Values (MN-major): lbo = bytes between panels of 64 columns, sbo = bytes between groups of 8 keys.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
-         (1ull << 46) | (2ull << 61);
+// Shared-memory operand descriptor, 128-byte swizzle, groups of 8 rows (keys and queries, K-major; values,
+// MN-major, one panel of 64 columns) 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
-// f32 accumulator, M = 128, N, A and B of one 16-bit type; mn_b: B is MN-major
-__device__ __forceinline__ constexpr uint32_t instruction(bool fp16, int n, bool mn_b) {
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok));
+  return ok != 0;
+}
+// f32 accumulator, M and N, A and B of one 16-bit type; mn_b: B is MN-major
+__device__ __forceinline__ constexpr uint32_t instruction(bool fp16, int m, int n, bool mn_b) {
   return (1u << 4) | (fp16 ? 0u : (1u << 7) | (1u << 10)) | (mn_b ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) |
-         ((128u >> 4) << 24);
+         ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// fp8: the codes of `n` chunks of a row, at `src(c)`, as bf16 with the row's scale applied, to `dst(2 c)`, `dst(2 c + 1)`.
+// value = code * 2^120 * 2^(e - 127); the second factor as a bf16, a NaN for a row with a NaN.
+template <int N, class Src, class Dst>
+__device__ __forceinline__ void to_bf16(uint32_t e, bool live, Src src, Dst dst) {
+  const uint32_t f1 = e == (uint32_t)kExpNan ? 0x7FC0u : e << 7;
+  const uint32_t f = f1 | (f1 << 16);
+#pragma unroll 2
+  for (int c = 0; c < N; ++c) {
+    uint32_t w[4] = {0, 0, 0, 0}, o[8];
+    if (live)
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src(c)) : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[2 * i] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x1404));
+      o[2 * i + 1] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x3424));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(o[i]), "r"(f));
+    sts128(dst(2 * c), o[0], o[1], o[2], o[3]);
+    sts128(dst(2 * c + 1), o[4], o[5], o[6], o[7]);
+  }
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t addr) {
+  uint16_t b;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=h"(b) : "r"(addr) : "memory");
+  return b;
 }
 
 template <int D, int FMT>
@@ -153,7 +249,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   using C = Cfg<D, FMT>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) Bars bars;
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+  const uint32_t rank = C::kCtas == 2 ? blockIdx.x & 1u : 0u, worker = blockIdx.x / C::kCtas;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_smem = smem, ring = smem + 2 * C::kQ, raw_ring = ring + C::kSlots * C::kSlot;
   auto full = [&](uint32_t i) { return smem_u32(&bars.full[i]); };
@@ -161,32 +258,33 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(full(i), C::kFp8 ? 128 : 1);
+      mbar_init(full(i), C::kFp8 ? 4 * C::kCtas : 1);  // fp8: the converting warps, at the first CTA
       mbar_init(empty(i), 1);
+      mbar_init(smem_u32(&bars.peer_full[i]), 1);
     }
     for (int i = 0; i < C::kRaws; ++i) {
       mbar_init(smem_u32(&bars.raw_full[i]), 1);
-      mbar_init(smem_u32(&bars.raw_empty[i]), 128);
+      mbar_init(smem_u32(&bars.raw_empty[i]), 4);
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&bars.q_ready[t]), 128);
+      mbar_init(smem_u32(&bars.q_ready[t]), 4 * C::kCtas);
       mbar_init(smem_u32(&bars.s_full[t]), 1);
-      mbar_init(smem_u32(&bars.p_ready[t][0]), 128);
-      mbar_init(smem_u32(&bars.p_ready[t][1]), 128);
+      mbar_init(smem_u32(&bars.p_ready[t][0]), 4 * C::kCtas);
+      mbar_init(smem_u32(&bars.p_ready[t][1]), 4 * C::kCtas);
       mbar_init(smem_u32(&bars.o_done[t]), 1);
     }
+    mbar_init(smem_u32(&bars.tail_here), 1);
+    mbar_init(smem_u32(&bars.tail_done), 1);
     mbar_init(smem_u32(&bars.drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
-    tc_alloc(smem_u32(&bars.tmem), 512);
-    tc_relinquish();
-  }
+  if (warp == 9) tc_alloc<C::kCtas>(smem_u32(&bars.tmem), 512);
   tc_fence_before();
   __syncthreads();
+  sync_worker<C::kCtas>();
   tc_fence_after();
   const uint32_t tmem = bars.tmem;
-  const uint32_t first = p.tile_off[blockIdx.x], last = p.tile_off[blockIdx.x + 1];
+  const uint32_t first = p.tile_off[worker], last = p.tile_off[worker + 1];
 
   if (warp < 8) {
     // ================= softmax: warpgroup t owns tile t, thread r its row r =================
@@ -200,9 +298,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     bool alive = true;
     for (uint32_t pi = first; alive && pi < last; ++pi) {
       const Piece pc = p.tile_pieces[pi];
-      if (t * kRowsPerTile >= pc.nrows) continue;
-      const uint32_t row = pc.row0 + t * kRowsPerTile + r;
-      const bool valid = t * kRowsPerTile + r < pc.nrows;
+      if (t * C::kRows >= pc.nrows) continue;
+      const uint32_t in_tile = t * C::kRows + rank * 128 + r;
+      const uint32_t row = pc.row0 + in_tile;
+      const bool valid = in_tile < pc.nrows;
       const uint32_t query = pc.query0 + row / a.group, head = pc.head * a.group + row % a.group;
       {
         // a warp's 32 rows, each row's chunks by neighbouring lanes
@@ -220,13 +319,13 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
 #pragma unroll
         for (int i = 0; i < 32 / kAt; ++i) {
           const uint32_t to = (r & ~31u) + i * kAt + lane / kLanes;
-          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(q_smem + t * C::kQ + chunk_offset<D, false>(to, c)),
-                       "r"(w[i].x ^ flip), "r"(w[i].y ^ flip), "r"(w[i].z ^ flip), "r"(w[i].w ^ flip)
-                       : "memory");
+          sts128(q_smem + t * C::kQ + (c / 8) * (128 * 128) + to * 128 + (((c % 8) ^ (to & 7u)) << 4), w[i].x ^ flip, w[i].y ^ flip,
+                 w[i].z ^ flip, w[i].w ^ flip);
         }
       }
       fence_async_shared();
-      mbar_arrive(smem_u32(&bars.q_ready[t]));
+      __syncwarp();
+      if (lane == 0) arrive_first<C::kCtas>(smem_u32(&bars.q_ready[t]));
 
       float m = -INFINITY, l = 0.0f;
       for (uint32_t j = 0; j < pc.nblocks; ++j) {
@@ -297,7 +396,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           }
           tc_wait_st();
           tc_fence_before();
-          mbar_arrive(smem_u32(&bars.p_ready[t][h]));
+          __syncwarp();
+          if (lane == 0) arrive_first<C::kCtas>(smem_u32(&bars.p_ready[t][h]));
         }
         float l0, l1;
         unpair(sum2, l0, l1);
@@ -311,7 +411,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       tc_fence_after();
       const bool direct = pc.part_row == kDirect;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      const uint64_t at = (uint64_t)pc.part_row + t * kRowsPerTile + r;
+      const uint64_t at = (uint64_t)pc.part_row + in_tile;
       // The queries are used up: their rows' shared memory takes the warp's 32 rows, half of their columns at a
       // time, from which whole rows are stored by neighbouring lanes.
       const uint32_t stage = q_smem + t * C::kQ + (warp % 4) * (32 * D * 2);
@@ -325,9 +425,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * (kCols * 4) + (((4 * c + i) ^ (lane & 7u)) << 4)),
-                         "r"(o[4 * i]), "r"(o[4 * i + 1]), "r"(o[4 * i + 2]), "r"(o[4 * i + 3])
-                         : "memory");
+            sts128(stage + lane * (kCols * 4) + (((4 * c + i) ^ (lane & 7u)) << 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         }
         __syncwarp();
         constexpr int kAt = 32 / kChunks;  // rows a round of the warp stores
@@ -366,9 +464,39 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
     if (warp == 8) {
-      // ================= copies: a step's keys, then its values (fp8: its records) =================
+      // ================= copies: a step's keys, then its values (fp8: all at once) =================
       uint32_t n = 0, ids = 0;  // slots (fp8: raw stages) filled
       constexpr uint32_t kN = C::kFp8 ? (C::kRaws ? C::kRaws : 1) : C::kSlots;
+      // The copies of this lane: 16-bit keys (2 KB panels of this CTA's blocks) and values (its panel of
+      // every block), or fp8 keys, values and exponents.  blk: the block of the step; from: in its record.
+      constexpr uint32_t kOwn = C::kKeys / kBlock;  // blocks whose keys this CTA holds
+      uint32_t blk[2] = {0, 0}, from[2] = {0, 0}, to[2] = {0, 0}, bytes[2] = {0, 0};
+      if (!C::kFp8) {
+        if (lane < 8) {
+          constexpr uint32_t kPanels = D / 64;
+          blk[0] = rank * kOwn + lane / kPanels;
+          from[0] = (lane % kPanels) * (kBlock * 128);
+          to[0] = (lane % kPanels) * (C::kKeys * 128) + (lane / kPanels) * (kBlock * 128);
+          blk[1] = lane;
+          from[1] = C::kHalf + rank * (kBlock * 128);
+          to[1] = lane * (kBlock * 128);
+          bytes[0] = bytes[1] = kBlock * 128;
+        }
+      } else if (lane < kOwn) {
+        blk[0] = rank * kOwn + lane;
+        to[0] = lane * C::kHalf;
+        bytes[0] = C::kHalf;
+      } else if (lane >= 8 && lane < 16) {
+        blk[0] = lane - 8;
+        from[0] = C::kHalf + rank * (kBlock * 64);
+        to[0] = C::kRawK + (lane - 8) * (kBlock * 64);
+        bytes[0] = kBlock * 64;
+      } else if (lane >= 16 && lane < 24) {
+        blk[0] = lane - 16;
+        from[0] = 2 * C::kHalf;
+        to[0] = C::kRawK + C::kRawV + (lane - 16) * 32;
+        bytes[0] = 32;
+      }
       bool alive = true;
       for (uint32_t pi = first; alive && pi < last; ++pi) {
         const Piece* pp = p.tile_pieces + pi;
@@ -376,9 +504,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         const uint32_t nb = (end - key0 + kBlock - 1) / kBlock;  // blocks from here to the span's end
         for (uint32_t j = 0; alive && j < steps; ++j) {
           if ((j & 3u) == 0) ids = p.blocks[block + min(j * 8 + lane, nb - 1)];
-          const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, (j & 3u) * 8 + (lane & 7u));
           const uint32_t live = min(nb - j * 8, 8u);
-          const uint8_t* rec = a.pool + ((uint64_t)id * a.kv_heads + head) * C::kRec;
+#pragma unroll
           for (uint32_t part = 0; part < (C::kFp8 ? 1u : 2u); ++part, ++n) {
             const uint32_t at = n % kN;
             const uint32_t fb = C::kFp8 ? smem_u32(&bars.raw_full[at % 4]) : full(at);
@@ -387,103 +514,141 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
               alive = false;
               break;
             }
-            constexpr uint32_t bytes = C::kFp8 ? C::kRec : C::kHalf;
-            if (lane == 0) mbar_expect(fb, live * bytes);
+            const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, (j & 3u) * 8 + blk[part]);
+            const uint32_t mine = blk[part] < live ? bytes[part] : 0u;
+            const uint32_t sum = __reduce_add_sync(0xFFFFFFFFu, mine);
+            if (lane == 0) mbar_expect(fb, sum);
             __syncwarp();
-            if (lane < live)
-              bulk_load((C::kFp8 ? raw_ring + at * C::kRaw : ring + at * C::kSlot) + lane * bytes, rec + part * C::kHalf, bytes, fb);
+            if (mine)
+              bulk_load((C::kFp8 ? raw_ring + at * C::kRaw : ring + at * C::kSlot) + to[part],
+                        a.pool + ((uint64_t)id * a.kv_heads + head) * C::kRec + from[part], mine, fb);
           }
         }
       }
       for (uint32_t i = n > kN ? n - kN : 0; i < n; ++i)  // no copy is left in flight
         alive &= mbar_wait_warp(C::kFp8 ? smem_u32(&bars.raw_full[i % kN % 4]) : full(i % kN), (i / kN) & 1);
       if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
-    } else if (warp == 9) {
-      // ================= products: the whole warp follows, one lane issues =================
-      constexpr uint32_t id_s = instruction(C::kFp16, kTileKeys, false), id_o = instruction(C::kFp16, D, true);
-      uint32_t n = 0;          // slots taken
-      uint32_t p_seen[2] = {0, 0}, q_seen[2] = {0, 0};
+    } else if (warp == 9 && rank == 0 && elect_one()) {
+      // ================= products: one thread waits and issues =================
+      constexpr uint32_t id_s = instruction(C::kFp16, C::kRows, kTileKeys, false), id_o = instruction(C::kFp16, C::kRows, D, true);
+      uint32_t n = 0;  // slots taken
+      uint32_t p_seen[2] = {0, 0}, q_seen[2] = {0, 0}, tails = 0;
       bool alive = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (alive && !mbar_wait_warp(bar, parity)) alive = false;
-        return alive;
-      };
+      auto wait = [&](uint32_t bar, uint32_t parity) { return alive = alive && mbar_wait(bar, parity); };
+      const uint64_t q_desc[2] = {operand(q_smem), operand(q_smem + C::kQ)};
+      const uint64_t ring_desc = operand(ring);
       auto scores = [&](uint32_t t, uint32_t slot) {
-        const uint64_t qd = operand(q_smem + t * C::kQ, 16, 16 * D), kd = operand(ring + slot * C::kSlot, 16, 16 * D);
+        const uint64_t qd = q_desc[t], kd = ring_desc + slot * (C::kSlot >> 4);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint64_t off = ((k / 4) * 1024 + (k % 4) * 32) >> 4;
-          tc_mma_ss(tmem + t * 128, qd + off, kd + off, id_s, k > 0);
-        }
+        for (int k = 0; k < D / 16; ++k)
+          tc_mma_ss<C::kCtas>(tmem + t * 128, qd + (((k / 4) * (128 * 128) + (k % 4) * 32) >> 4),
+                              kd + (((k / 4) * (C::kKeys * 128) + (k % 4) * 32) >> 4), id_s, k > 0);
       };
       auto values = [&](uint32_t t, uint32_t slot, int half, bool acc) {
-        const uint64_t vd = operand(ring + slot * C::kSlot, 1024, 16 * D);
+        const uint64_t vd = ring_desc + slot * (C::kSlot >> 4);
 #pragma unroll
         for (int k = 4 * half; k < 4 * half + 4; ++k)
-          tc_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + ((k * 32 * D) >> 4), id_o, acc || k > 0);
+          tc_mma_ts<C::kCtas>(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + ((k * 16 * 128) >> 4), id_o, acc || k > 0);
       };
       for (uint32_t pi = first; alive && pi < last; ++pi) {
         const Piece* pp = p.tile_pieces + pi;
-        const uint32_t steps = pp->nblocks, key0 = pp->key0, end = pp->end;
-        const uint32_t tiles = pp->nrows > kRowsPerTile ? 2 : 1;
+        const uint32_t steps = pp->nblocks, keys = pp->end - pp->key0;
+        const uint32_t tiles = pp->nrows > C::kRows ? 2 : 1;
         // ring order: keys 0, values 0, keys 1, values 1, ...: step j's keys are slot n0 + 2j, values n0 + 2j + 1
         const uint32_t n0 = n;
         auto slot = [&](uint32_t i) { return (n0 + i) % C::kSlots; };
-        auto parity = [&](uint32_t i) { return ((n0 + i) / C::kSlots) & 1u; };
-        wait(full(slot(0)), parity(0));
-        for (uint32_t t = 0; alive && t < tiles; ++t) {
+        auto here = [&](uint32_t i) {  // both CTAs' parts of a slot
+          const uint32_t par = ((n0 + i) / C::kSlots) & 1u;
+          return wait(full(slot(i)), par) && (C::kFp8 || C::kCtas == 1 || wait(smem_u32(&bars.peer_full[slot(i)]), par));
+        };
+        here(0);
+        for (uint32_t t = 0; t < tiles; ++t) {
           if (!wait(smem_u32(&bars.q_ready[t]), q_seen[t] & 1)) break;
           ++q_seen[t];
           tc_fence_after();
-          if (lane == 0) {
-            scores(t, slot(0));
-            if (t == tiles - 1) tc_commit(empty(slot(0)));
-            tc_commit(smem_u32(&bars.s_full[t]));
-          }
-          __syncwarp();
+          scores(t, slot(0));
+          tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
         }
+        if (alive) tc_commit<C::kCtas>(empty(slot(0)));
         for (uint32_t j = 0; alive && j < steps; ++j) {
           const bool more = j + 1 < steps;
-          if (!wait(full(slot(2 * j + 1)), parity(2 * j + 1))) break;
-          const uint32_t left = end - (key0 + j * kTileKeys);
-          if (!C::kFp8 && left < (uint32_t)kTileKeys) {
-            // value rows past the end: what other tokens or earlier steps left there
-            const uint32_t v = ring + slot(2 * j + 1) * C::kSlot;
-            for (uint32_t i = left * (D / 8) + lane; i < kTileKeys * (D / 8); i += 32) {
-              const uint32_t tok = i / (D / 8), c = i % (D / 8);
-              asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(v + chunk_offset<D, false>(tok, c)), "r"(0) : "memory");
-            }
-            fence_async_shared();
-            __syncwarp();
+          if (!here(2 * j + 1)) break;
+          if (!C::kFp8 && keys - j * kTileKeys < (uint32_t)kTileKeys) {
+            mbar_arrive(smem_u32(&bars.tail_here));
+            if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
           }
-          if (more && !wait(full(slot(2 * j + 2)), parity(2 * j + 2))) break;
-          for (uint32_t t = 0; alive && t < tiles; ++t) {
+          if (more && !here(2 * j + 2)) break;
+          for (uint32_t t = 0; t < tiles; ++t) {
             if (!wait(smem_u32(&bars.p_ready[t][0]), p_seen[t] & 1)) break;
             tc_fence_after();
-            if (lane == 0) values(t, slot(2 * j + 1), 0, j > 0);
-            __syncwarp();
+            values(t, slot(2 * j + 1), 0, j > 0);
             if (!wait(smem_u32(&bars.p_ready[t][1]), p_seen[t] & 1)) break;
             ++p_seen[t];
             tc_fence_after();
-            if (lane == 0) {
-              values(t, slot(2 * j + 1), 1, true);
-              if (t == tiles - 1) tc_commit(empty(slot(2 * j + 1)));
-              if (more) {
-                scores(t, slot(2 * j + 2));
-                if (t == tiles - 1) tc_commit(empty(slot(2 * j + 2)));
-                tc_commit(smem_u32(&bars.s_full[t]));
-              } else {
-                tc_commit(smem_u32(&bars.o_done[t]));
-              }
+            values(t, slot(2 * j + 1), 1, true);
+            if (more) {
+              scores(t, slot(2 * j + 2));
+              tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
+            } else {
+              tc_commit<C::kCtas>(smem_u32(&bars.o_done[t]));
             }
-            __syncwarp();
+          }
+          if (alive) {
+            tc_commit<C::kCtas>(empty(slot(2 * j + 1)));
+            if (more) tc_commit<C::kCtas>(empty(slot(2 * j + 2)));
           }
         }
         n = n0 + 2 * steps;
       }
-      if (lane == 0) tc_commit(smem_u32(&bars.drain));
-      __syncwarp();
-      alive &= mbar_wait_warp(smem_u32(&bars.drain), 0);  // nothing is left in flight when tensor memory is freed
+      tc_commit<C::kCtas>(smem_u32(&bars.drain));
+      alive = mbar_wait(smem_u32(&bars.drain), 0) && alive;  // nothing is in flight when tensor memory is freed
+      if (!alive) {
+        atomicOr_system(a.err, kErrWait);
+        mbar_arrive(smem_u32(&bars.tail_here));  // releases the warp that waits for it
+      }
+    } else if (warp == 9 && rank == 1 && !C::kFp8 && elect_one()) {
+      // ================= the pair's second CTA: tells the first what has arrived here =================
+      uint32_t n = 0, tails = 0;
+      bool alive = true;
+      for (uint32_t pi = first; alive && pi < last; ++pi) {
+        const Piece* pp = p.tile_pieces + pi;
+        const uint32_t slots = 2 * pp->nblocks;
+        const bool partial = pp->end - pp->key0 < pp->nblocks * kTileKeys;
+        for (uint32_t i = 0; alive && i < slots; ++i, ++n) {
+          const uint32_t at = n % C::kSlots;
+          alive = mbar_wait(full(at), (n / C::kSlots) & 1);
+          if (alive && partial && i == slots - 1) {
+            mbar_arrive(smem_u32(&bars.tail_here));
+            alive = mbar_wait(smem_u32(&bars.tail_done), tails++ & 1);
+          }
+          if (alive) arrive_first<C::kCtas>(smem_u32(&bars.peer_full[at]));
+        }
+      }
+      if (!alive) {
+        atomicOr_system(a.err, kErrWait);
+        mbar_arrive(smem_u32(&bars.tail_here));
+      }
+    } else if (warp == 10 && !C::kFp8) {
+      // ================= partial steps: value rows past the end, which hold other tokens or earlier steps =================
+      uint32_t n = 0, tails = 0;
+      bool alive = true;
+      for (uint32_t pi = first; alive && pi < last; ++pi) {
+        const Piece* pp = p.tile_pieces + pi;
+        n += 2 * pp->nblocks;
+        const uint32_t left = pp->end - (pp->key0 + (pp->nblocks - 1) * kTileKeys);
+        if (left >= (uint32_t)kTileKeys) continue;
+        // The whole share may run before this step comes; the issuing thread's own waits are short, and it
+        // also arrives when it gives up.
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars.tail_here), tails++ & 1, 60000000000ull))) {
+          alive = false;
+          break;
+        }
+        const uint32_t v = ring + (n - 1) % C::kSlots * C::kSlot;  // the last step's values
+        for (uint32_t i = left * 8 + lane; i < kTileKeys * 8; i += 32) sts128(v + (i / 8) * 128 + (i % 8) * 16, 0, 0, 0, 0);
+        fence_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars.tail_done));
+      }
       if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
     }
   } else {
@@ -491,60 +656,51 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     if constexpr (C::kFp8) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
       const uint32_t tok = threadIdx.x % 128;
+      const uint32_t kt = tok % C::kKeys, kb = kt / kBlock, vb = tok / kBlock;  // this thread's key; blocks
+      constexpr int kChunks = D / 16 / C::kCtas;                               // and chunks of it: 4
+      const uint32_t kc = tok / C::kKeys * kChunks;
+      constexpr uint32_t kOwn = C::kKeys / kBlock;
       uint32_t n = 0, raws = 0;
       bool alive = true;
       for (uint32_t pi = first; alive && pi < last; ++pi) {
         const Piece* pp = p.tile_pieces + pi;
-        const uint32_t steps = pp->nblocks, key0 = pp->key0, end = pp->end;
+        const uint32_t steps = pp->nblocks, keys = pp->end - pp->key0;
         for (uint32_t j = 0; alive && j < steps; ++j, ++raws) {
           const uint32_t rs = raws % C::kRaws;
           if (!mbar_wait_warp(smem_u32(&bars.raw_full[rs]), (raws / C::kRaws) & 1)) {
             alive = false;
             break;
           }
-          const bool live = key0 + j * kTileKeys + tok < end;
-          const uint32_t rec = raw_ring + rs * C::kRaw + (tok / kBlock) * C::kRec;
+          const uint32_t raw = raw_ring + rs * C::kRaw, exps = raw + C::kRawK + C::kRawV;
+          const uint32_t left = keys - j * kTileKeys;
           for (uint32_t part = 0; part < 2; ++part, ++n) {
             const uint32_t at = n % C::kSlots;
             if (n >= (uint32_t)C::kSlots && !mbar_wait_warp(empty(at), (n / C::kSlots - 1) & 1)) {
               alive = false;
               break;
             }
-            uint32_t e = kExpBias;
-            if (live) {
-              uint16_t b;
-              asm volatile("ld.shared.u8 %0, [%1];" : "=h"(b) : "r"(rec + 2 * C::kHalf + part * kBlock + tok % kBlock) : "memory");
-              e = b;
-            }
-            // value = code * 2^120 * 2^(e - 127); the second factor as a bf16, a NaN for a row with a NaN
-            const uint32_t f1 = e == (uint32_t)kExpNan ? 0x7FC0u : e << 7;
-            const uint32_t f = f1 | (f1 << 16);
             const uint32_t dst = ring + at * C::kSlot;
-#pragma unroll 2
-            for (int c = 0; c < D / 16; ++c) {
-              uint32_t w[4] = {0, 0, 0, 0}, o[8];
-              if (live)
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                             : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                             : "r"(rec + part * C::kHalf + chunk_offset<D, true>(tok % kBlock, c))
-                             : "memory");
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                o[2 * i] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x1404));
-                o[2 * i + 1] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x3424));
-              }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(o[i]), "r"(f));
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-                asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst + chunk_offset<D, false>(tok, 2 * c + i)),
-                             "r"(o[4 * i]), "r"(o[4 * i + 1]), "r"(o[4 * i + 2]), "r"(o[4 * i + 3])
-                             : "memory");
+            if (part == 0) {
+              const bool live = rank * C::kKeys + kt < left;
+              const uint32_t e = live ? lds8(exps + (rank * kOwn + kb) * 32 + kt % kBlock) : (uint32_t)kExpBias;
+              to_bf16<kChunks>(
+                  e, live, [&](int c) { return raw + kb * C::kHalf + offset8k<D>(kt % kBlock, kc + c); },
+                  [&](int c) {
+                    const uint32_t cc = 2 * kc + c;
+                    return dst + (cc / 8) * (C::kKeys * 128) + kt * 128 + (((cc % 8) ^ (kt & 7u)) << 4);
+                  });
+            } else {
+              const bool live = tok < left;
+              const uint32_t e = live ? lds8(exps + vb * 32 + kBlock + tok % kBlock) : (uint32_t)kExpBias;
+              to_bf16<4>(
+                  e, live, [&](int c) { return raw + C::kRawK + vb * (kBlock * 64) + offset8v(tok % kBlock, c); },
+                  [&](int c) { return dst + tok * 128 + ((c ^ (tok & 7u)) << 4); });
             }
             fence_async_shared();
-            mbar_arrive(full(at));
+            __syncwarp();
+            if (lane == 0) arrive_first<C::kCtas>(full(at));
           }
-          if (alive) mbar_arrive(smem_u32(&bars.raw_empty[rs]));
+          if (alive && lane == 0) mbar_arrive(smem_u32(&bars.raw_empty[rs]));
         }
       }
       if (!alive && tok == 0) atomicOr_system(a.err, kErrWait);
@@ -553,8 +709,9 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  sync_worker<C::kCtas>();  // no CTA leaves while the other may arrive on its barriers or read its memory
   tc_fence_after();
-  if (warp == 9) tc_dealloc(tmem, 512);
+  if (warp == 9) tc_dealloc<C::kCtas>(tmem, 512);
 }
 
 template <int D, int FMT>
@@ -570,8 +727,19 @@ cudaError_t prepare_one() {
 }
 template <int D, int FMT>
 cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
-  tiles_kernel<D, FMT><<<p.tile_ctas, Cfg<D, FMT>::kWarps * 32, Cfg<D, FMT>::kSmem, s>>>(a, p);
-  return cudaGetLastError();
+  using C = Cfg<D, FMT>;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(p.tile_workers * C::kCtas);
+  cfg.blockDim = dim3(C::kWarps * 32);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = C::kCtas;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, tiles_kernel<D, FMT>, a, p);
 }
 
 }  // namespace
