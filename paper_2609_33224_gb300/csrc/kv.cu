@@ -9,8 +9,8 @@
 
 #include "kv_internal.cuh"
 
-using pskv::Group;
-using pskv::Layer;
+using pskv::JoinEntry;
+using pskv::JoinSeg;
 using pskv::Piece;
 
 struct ps_kv {
@@ -156,13 +156,23 @@ Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t fro
   return u;
 }
 
+// The rows of a span, tiled one way; tile t and head h have the parts groups[group0 + t * kv_heads + h].
+struct Layer {
+  uint32_t query0, num_queries, tile_rows, group0;
+};
+struct Group {
+  uint32_t part_row;  // kDirect: written by the attention kernel
+  uint32_t nparts;
+};
+
 struct Layout {
   std::vector<Layer> layers;
-  std::vector<uint32_t> layer_queries;
   std::vector<Group> groups;
   std::vector<Unit> row_units, tile_units;
   std::vector<Piece> row_pieces, tile_pieces;
-  std::vector<uint32_t> row_off, tile_off, tok_off, tok_layer, join;
+  std::vector<uint32_t> row_off, tile_off, tok_off, tok_layer;
+  std::vector<JoinEntry> join;
+  std::vector<JoinSeg> segs;
   uint64_t part_rows = 0;
   uint32_t max_parts = 1;
 };
@@ -221,8 +231,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     const uint32_t full = (uint32_t)pskv::tile_rows_of((int)pl.kv->D), tile_rows = rows <= full / 2 ? full / 2 : full;
     if (rows >= kTileLeastRows && len >= kTileLeastKeys) {
       const uint32_t tiles = (rows + tile_rows - 1) / tile_rows;
-      o.layers.push_back(Layer{s.first_query, tile_rows, (uint32_t)o.groups.size(), 0});
-      o.layer_queries.push_back(s.num_queries);
+      o.layers.push_back(Layer{s.first_query, s.num_queries, tile_rows, (uint32_t)o.groups.size()});
       for (uint32_t t = 0; t < tiles; ++t) {
         const uint32_t r0 = t * tile_rows, nr = std::min(rows - r0, tile_rows);
         int64_t c = len;
@@ -236,8 +245,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
       }
       if (!s.causal) continue;
     }
-    o.layers.push_back(Layer{s.first_query, (uint32_t)kSmallRows, (uint32_t)o.groups.size(), 0});
-    o.layer_queries.push_back(s.num_queries);
+    o.layers.push_back(Layer{s.first_query, s.num_queries, (uint32_t)kSmallRows, (uint32_t)o.groups.size()});
     for (uint32_t r0 = 0; r0 < rows; r0 += kSmallRows) {
       const uint32_t nr = std::min<uint32_t>(rows - r0, kSmallRows);
       const int64_t from = cut.empty() ? 0 : cut[r0 / tile_rows];
@@ -252,7 +260,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
   // which layers cover a query
   o.tok_off.assign((size_t)T + 1, 0);
   for (size_t l = 0; l < o.layers.size(); ++l)
-    for (uint32_t i = 0; i < o.layer_queries[l]; ++i) ++o.tok_off[o.layers[l].query0 + i + 1];
+    for (uint32_t i = 0; i < o.layers[l].num_queries; ++i) ++o.tok_off[o.layers[l].query0 + i + 1];
   std::vector<uint8_t> alone(T, 0);
   for (uint32_t t = 0; t < T; ++t) {
     alone[t] = o.tok_off[t + 1] == 1;
@@ -262,7 +270,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
   {
     std::vector<uint32_t> at(o.tok_off.begin(), o.tok_off.end() - 1);
     for (size_t l = 0; l < o.layers.size(); ++l)
-      for (uint32_t i = 0; i < o.layer_queries[l]; ++i) o.tok_layer[at[o.layers[l].query0 + i]++] = (uint32_t)l;
+      for (uint32_t i = 0; i < o.layers[l].num_queries; ++i) o.tok_layer[at[o.layers[l].query0 + i]++] = (uint32_t)l;
   }
 
   // pieces, and where their partial results go
@@ -296,18 +304,35 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     finish(o.tile_units, o.tile_pieces, first);
   }
 
-  // (query, head) pairs whose rows have something to join, or no key at all
-  for (uint32_t t = 0; t < T; ++t)
-    for (uint32_t h = 0; h < H; ++h) {
-      bool need = !alone[t];
-      if (!need) {
-        const Layer& ly = o.layers[o.tok_layer[o.tok_off[t]]];
-        const uint32_t r = (t - ly.query0) * g;
-        for (uint32_t tile = r / ly.tile_rows; tile <= (r + g - 1) / ly.tile_rows; ++tile)
-          need |= o.groups[ly.group0 + tile * H + h].part_row != pskv::kDirect;
+  // The rows of a query and head that have something to join, or no key at all; cut where one of the query's
+  // layers begins a new tile.
+  for (uint32_t t = 0; t < T; ++t) {
+    const uint32_t* ls = o.tok_layer.data() + o.tok_off[t];
+    const uint32_t nl = o.tok_off[t + 1] - o.tok_off[t];
+    for (uint32_t i = 0, n; i < g; i += n) {
+      n = g - i;
+      for (uint32_t l = 0; l < nl; ++l) {
+        const Layer& ly = o.layers[ls[l]];
+        n = std::min(n, ly.tile_rows - ((t - ly.query0) * g + i) % ly.tile_rows);
       }
-      if (need) o.join.push_back(t * H + h);
+      for (uint32_t h = 0; h < H; ++h) {
+        const uint32_t seg0 = (uint32_t)o.segs.size();
+        bool direct = false;
+        for (uint32_t l = 0; l < nl; ++l) {
+          const Layer& ly = o.layers[ls[l]];
+          const uint32_t r = (t - ly.query0) * g + i;
+          const Group& gr = o.groups[ly.group0 + r / ly.tile_rows * H + h];
+          direct = direct || gr.part_row == pskv::kDirect;
+          if (gr.nparts) o.segs.push_back(JoinSeg{gr.part_row + r % ly.tile_rows, ly.tile_rows, gr.nparts});
+        }
+        if (direct) {
+          o.segs.resize(seg0);
+          continue;
+        }
+        o.join.push_back(JoinEntry{t, (uint16_t)(h * g + i), (uint16_t)n, seg0, (uint32_t)o.segs.size() - seg0});
+      }
     }
+  }
 }
 
 template <class T>
@@ -377,8 +402,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   size_t at = 0;
   const size_t rp = place(&parts, &at, o.row_pieces), ro = place(&parts, &at, o.row_off);
   const size_t tp = place(&parts, &at, o.tile_pieces), to = place(&parts, &at, o.tile_off);
-  const size_t la = place(&parts, &at, o.layers), gr = place(&parts, &at, o.groups);
-  const size_t tk = place(&parts, &at, o.tok_off), tl = place(&parts, &at, o.tok_layer), jn = place(&parts, &at, o.join);
+  const size_t jn = place(&parts, &at, o.join), sg = place(&parts, &at, o.segs);
   const size_t bl = at;
   parts.emplace_back(blocks, n_blocks * sizeof(uint32_t));
   at += n_blocks * sizeof(uint32_t);
@@ -406,11 +430,8 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.tile_pieces = reinterpret_cast<const Piece*>(b.dev + tp);
   d.tile_off = reinterpret_cast<const uint32_t*>(b.dev + to);
   d.tile_workers = o.tile_off.empty() ? 0 : (uint32_t)o.tile_off.size() - 1;
-  d.layers = reinterpret_cast<const Layer*>(b.dev + la);
-  d.groups = reinterpret_cast<const Group*>(b.dev + gr);
-  d.tok_off = reinterpret_cast<const uint32_t*>(b.dev + tk);
-  d.tok_layer = reinterpret_cast<const uint32_t*>(b.dev + tl);
-  d.join = reinterpret_cast<const uint32_t*>(b.dev + jn);
+  d.join = reinterpret_cast<const JoinEntry*>(b.dev + jn);
+  d.segs = reinterpret_cast<const JoinSeg*>(b.dev + sg);
   d.njoin = (uint32_t)o.join.size();
   d.max_parts = o.max_parts;
   d.blocks = reinterpret_cast<const uint32_t*>(b.dev + bl);
@@ -511,7 +532,8 @@ ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_queries, u
   if (!kv) return PS_ERR_INVALID;
   if (!out) return fail(kv, PS_ERR_INVALID, "out is NULL");
   *out = nullptr;
-  if (q_heads < 1 || q_heads % kv->heads) return fail(kv, PS_ERR_INVALID, "q_heads must be a multiple of kv_heads");
+  if (q_heads < 1 || q_heads > 65535 || q_heads % kv->heads)
+    return fail(kv, PS_ERR_INVALID, "q_heads must be a multiple of kv_heads, at most 65535");
   if (max_queries < 1 || (uint64_t)max_queries * q_heads >= (1ull << 30))
     return fail(kv, PS_ERR_INVALID, "max_queries must be at least 1 and max_queries * q_heads < 2^30");
   if (max_blocks >= (1ull << 32)) return fail(kv, PS_ERR_INVALID, "max_blocks must be < 2^32");

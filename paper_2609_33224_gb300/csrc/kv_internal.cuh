@@ -70,16 +70,15 @@ static_assert(sizeof(Piece) == 48, "Piece layout");
 constexpr uint32_t kDirect = 0xFFFFFFFFu;
 constexpr int32_t kNoLimit = 0x3FFFFFFF;
 
-// The rows of a span, tiled one way; tile t and head h have the parts groups[group0 + t * kv_heads + h].
-struct Layer {
-  uint32_t query0;
-  uint32_t tile_rows;
-  uint32_t group0;
-  uint32_t pad;
+// What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments segs[seg0] ..:
+// the i-th row's are the partial rows row + i + k * stride, k < nparts.
+struct JoinEntry {
+  uint32_t query;
+  uint16_t head0, count;
+  uint32_t seg0, nsegs;
 };
-struct Group {
-  uint32_t part_row;  // kDirect: already in the output
-  uint32_t nparts;
+struct JoinSeg {
+  uint32_t row, stride, nparts;
 };
 
 struct PlanDev {
@@ -89,11 +88,8 @@ struct PlanDev {
   const Piece* tile_pieces;
   const uint32_t* tile_off;
   uint32_t tile_workers;  // CTAs, or pairs of them
-  const Layer* layers;
-  const Group* groups;
-  const uint32_t* tok_off;  // layers of query t: tok_layer[tok_off[t]] ..
-  const uint32_t* tok_layer;
-  const uint32_t* join;  // (query * kv_heads + head) that have parts to join, or nothing
+  const JoinEntry* join;
+  const JoinSeg* segs;
   uint32_t njoin;
   uint32_t max_parts;
   const uint32_t* blocks;
@@ -207,13 +203,20 @@ __device__ __forceinline__ float exp_value(uint32_t e) {
 
 // Two e4m3 codes in the high bytes of the halves of x -> bf16x2, without their scale.  A code's magnitude
 // bits, moved down by 4, are a bf16 whose exponent bias is 127 instead of 7 (subnormal codes become bf16
-// subnormals), so a product with 2^120 gives the value, exactly.  Code 0x7F (NaN) becomes 480: the caches
-// mark rows with a NaN by their scale.
+// subnormals), so a product with 2^120 gives the value, exactly.  (No code of a cache is a NaN: rows with
+// one are marked by their scale.)
 __device__ __forceinline__ uint32_t e4m3_to_bf16x2(uint32_t x) {
   const uint32_t y = ((x >> 4) & 0x07F007F0u) | (x & 0x80008000u);
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(y), "r"(0x7B807B80u));
   return r;
+}
+
+// The same to f16x2: the two codes in the lower or upper half of x.
+__device__ __forceinline__ void e4m3x4_to_f16x2(uint32_t x, uint32_t& lo, uint32_t& hi) {
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
+      : "=r"(lo), "=r"(hi)
+      : "r"(x));
 }
 
 }  // namespace pskv

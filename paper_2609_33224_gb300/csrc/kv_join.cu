@@ -5,53 +5,61 @@
 namespace pskv {
 namespace {
 
-// One (query, q head) row per warp, or with kWide per CTA of 8 warps, which share its parts.  A part is read
-// once: its maximum and sum (all lanes the same two floats), and its D values, D / 32 per lane.
+// One (query, q head) row per warp, or with kWide per CTA of 8 warps, which share its parts.  Up to 32 parts at
+// a time: each lane takes one part's maximum m_k and sum l_k, then all lanes add the parts' D values, D / 32 a
+// lane, with the weights 2^(m_k - M): the loads of the values do not wait for one another.
 // out = sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k with the running maximum M, in 32 bits.
 // Bound by the bytes of the parts (D * 4 + 8 each), which the attention kernels left in L2.
 template <int D, bool FP16, bool kWide>
 __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const PlanDev p) {
   constexpr int kV = D / 32;
+  constexpr uint32_t kStep = kWide ? 8 : 1;
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t row = kWide ? blockIdx.x : blockIdx.x * 8 + warp;
-  const uint32_t rows = p.njoin * a.group;
-  if (row >= rows) return;  // kWide: the whole CTA
-  const uint32_t entry = p.join[row / a.group], gi = row % a.group;
-  const uint32_t query = entry / a.kv_heads, kvh = entry % a.kv_heads;
-  const uint32_t head = kvh * a.group + gi;
+  if (row >= p.njoin * a.group) return;  // kWide: the whole CTA
+  const JoinEntry en = p.join[row / a.group];
+  const uint32_t gi = row % a.group;
+  if (gi >= en.count) return;  // the same
+  const uint32_t query = en.query, head = en.head0 + gi;
 
   float m = -INFINITY, l = 0.0f, acc[kV];
 #pragma unroll
   for (int i = 0; i < kV; ++i) acc[i] = 0.0f;
-  bool done = false;
-  for (uint32_t x = p.tok_off[query]; x < p.tok_off[query + 1]; ++x) {
-    const Layer ly = p.layers[p.tok_layer[x]];
-    const uint32_t r = (query - ly.query0) * a.group + gi;
-    const Group gr = p.groups[ly.group0 + r / ly.tile_rows * a.kv_heads + kvh];
-    if (gr.part_row == kDirect) {
-      done = true;  // written by the attention kernel
-      break;
-    }
-    const uint32_t base = gr.part_row + r % ly.tile_rows;
-#pragma unroll 4
-    for (uint32_t k = kWide ? warp : 0; k < gr.nparts; k += kWide ? 8 : 1) {
-      const uint64_t at = base + (uint64_t)k * ly.tile_rows;
-      const float2 ml = a.part_ml[at];
-      float v[kV];
-      const float* src = a.part + at * D + lane * kV;
-      if (kV == 4) {
-        const float4 w = *reinterpret_cast<const float4*>(src);
-        v[0] = w.x; v[1] = w.y; v[kV - 2] = w.z; v[kV - 1] = w.w;
-      } else {
-        const float2 w = *reinterpret_cast<const float2*>(src);
-        v[0] = w.x; v[1] = w.y;
-      }
-      const float n = fmaxf(m, ml.x);
-      const float f0 = m == n ? 1.0f : ex2(m - n), f1 = ml.x == n ? 1.0f : ex2(ml.x - n);
-      m = n;
-      l = l * f0 + ml.y * f1;
+  for (uint32_t x = 0; x < en.nsegs; ++x) {
+    const JoinSeg sg = p.segs[en.seg0 + x];
+    const uint64_t at0 = (uint64_t)sg.row + gi, stride = (uint64_t)sg.stride * kStep;
+    const uint64_t base = at0 + (kWide ? (uint64_t)warp * sg.stride : 0);
+    const uint32_t n = kWide ? (sg.nparts + 7 - warp) / 8 : sg.nparts;  // this warp's parts
+    for (uint32_t c = 0; c < n; c += 32) {
+      const uint32_t cnt = min(32u, n - c);
+      float2 ml = make_float2(-INFINITY, 0.0f);
+      if (lane < cnt) ml = a.part_ml[base + (uint64_t)(c + lane) * stride];
+      float mm = ml.x;
+      for (uint32_t o = 16; o; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, o));
+      mm = fmaxf(mm, m);
+      const float f = m == mm ? 1.0f : ex2(m - mm);
+      m = mm;
+      float w = lane < cnt ? (ml.x == mm ? 1.0f : ex2(ml.x - mm)) : 0.0f;
+      float wl = w * ml.y;
+      for (uint32_t o = 16; o; o >>= 1) wl += __shfl_xor_sync(0xFFFFFFFFu, wl, o);
+      l = l * f + wl;
 #pragma unroll
-      for (int i = 0; i < kV; ++i) acc[i] = acc[i] * f0 + v[i] * f1;
+      for (int i = 0; i < kV; ++i) acc[i] *= f;
+#pragma unroll 4
+      for (uint32_t k = 0; k < cnt; ++k) {
+        const float* src = a.part + (base + (uint64_t)(c + k) * stride) * D + lane * kV;
+        float v[kV];
+        if (kV == 4) {
+          const float4 y = *reinterpret_cast<const float4*>(src);
+          v[0] = y.x; v[1] = y.y; v[kV - 2] = y.z; v[kV - 1] = y.w;
+        } else {
+          const float2 y = *reinterpret_cast<const float2*>(src);
+          v[0] = y.x; v[1] = y.y;
+        }
+        const float wk = __shfl_sync(0xFFFFFFFFu, w, k);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) acc[i] = fmaf(v[i], wk, acc[i]);
+      }
     }
   }
   if (kWide) {
@@ -63,7 +71,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const PlanD
 #pragma unroll
     for (int i = 0; i < kV; ++i) sacc[warp][lane * kV + i] = acc[i];
     __syncthreads();
-    if (done || warp != 0) return;
+    if (warp != 0) return;
     float n = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 8; ++w) n = fmaxf(n, sm[w]);
@@ -79,7 +87,6 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const PlanD
     }
     m = n;
   }
-  if (done) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // no key: zeros (a NaN stays one)
   uint16_t* o = a.out + (int64_t)query * a.o_tok + (int64_t)head * a.o_head + lane * kV;
   uint32_t w[kV / 2];

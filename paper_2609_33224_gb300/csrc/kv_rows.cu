@@ -23,6 +23,9 @@ constexpr int ring_stages() {
   return kRingBytes / record_bytes(D, FMT);
 }
 
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
 template <bool FP16>
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if (FP16)
@@ -148,6 +151,37 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         qf[kc][3] = vb ? *reinterpret_cast<const uint32_t*>(qb + hi) : 0u;
       }
     }
+    // fp8: codes are exact in fp16 and one instruction turns two of them into it, so the products are fp16.
+    // The queries are first scaled by a power of two per row, which brings the largest element just below
+    // 2^15: all but elements 2^-32 of it keep their 8 bits.
+    float qa_scale = a.scale_log2, qb_scale = a.scale_log2;
+    if constexpr (kFp8) {
+      float x = 0.0f, y = 0.0f;
+#pragma unroll
+      for (int kc = 0; kc < D / 16; ++kc) {
+        x = fmaxf(fmaxf(x, fabsf(bf16_lo(qf[kc][0]))), fmaxf(fabsf(bf16_hi(qf[kc][0])), fmaxf(fabsf(bf16_lo(qf[kc][2])), fabsf(bf16_hi(qf[kc][2])))));
+        y = fmaxf(fmaxf(y, fabsf(bf16_lo(qf[kc][1]))), fmaxf(fabsf(bf16_hi(qf[kc][1])), fmaxf(fabsf(bf16_lo(qf[kc][3])), fabsf(bf16_hi(qf[kc][3])))));
+      }
+      x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 1));
+      y = fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, 1));
+      x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, 2));
+      y = fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, 2));
+      // exponents such that 2^up * max is in [2^14, 2^15); limited, so that 2^up and 2^-up are normal floats
+      const int ea = min(max(14 + 127 - (int)(__float_as_uint(x) >> 23), -112), 126);
+      const int eb = min(max(14 + 127 - (int)(__float_as_uint(y) >> 23), -112), 126);
+      const float ua = __uint_as_float((uint32_t)(127 + ea) << 23), ub = __uint_as_float((uint32_t)(127 + eb) << 23);
+      qa_scale *= __uint_as_float((uint32_t)(127 - ea) << 23);
+      qb_scale *= __uint_as_float((uint32_t)(127 - eb) << 23);
+#pragma unroll
+      for (int kc = 0; kc < D / 16; ++kc) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float u = (i & 1) ? ub : ua;
+          qf[kc][i] = pack2<true>(bf16_lo(qf[kc][i]) * u, bf16_hi(qf[kc][i]) * u);
+        }
+      }
+    }
+    int ve = 0;  // fp8: the exponent (biased) that the output so far is relative to
     // the last key each of the two rows sees, and the last that all rows of the tile see
     const int32_t last = (int32_t)pc.end - 1;
     const int32_t lim_a = min(last, pc.climit + (int32_t)ta), lim_b = min(last, pc.climit + (int32_t)tb);
@@ -182,9 +216,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           uint32_t r[4];  // keys 0-7 and 8-15 of chunk c, then of chunk c + 1
           ldsm4<false>(r, rec + offset8k<D>(tok, c + (mi >> 1)));
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            mma16816<false>(s[i & 1], qf[c + (i >> 1)], e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x1404)),
-                            e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x3424)));
+          for (int i = 0; i < 4; ++i) {
+            uint32_t b0, b1;
+            e4m3x4_to_f16x2(r[i], b0, b1);
+            mma16816<true>(s[i & 1], qf[c + (i >> 1)], b0, b1);
+          }
         }
       } else {
         const uint32_t tok = (mi >> 1) * 8 + mr;
@@ -200,12 +236,37 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
       if constexpr (kFp8) {
         const uint32_t e0 = lds16(rec + 2 * kHalf + t4 * 2), e1 = lds16(rec + 2 * kHalf + 8 + t4 * 2);
         const uint32_t f0 = lds16(rec + 2 * kHalf + 16 + t4 * 2), f1 = lds16(rec + 2 * kHalf + 24 + t4 * 2);
-        const float k0 = exp_value(e0 & 255u) * a.scale_log2, k1 = exp_value(e0 >> 8) * a.scale_log2;
-        const float k2 = exp_value(e1 & 255u) * a.scale_log2, k3 = exp_value(e1 >> 8) * a.scale_log2;
-        s[0][0] *= k0; s[0][1] *= k1; s[0][2] *= k0; s[0][3] *= k1;
-        s[1][0] *= k2; s[1][1] *= k3; s[1][2] *= k2; s[1][3] *= k3;
-        vs[0] = exp_value(f0 & 255u); vs[1] = exp_value(f0 >> 8);
-        vs[2] = exp_value(f1 & 255u); vs[3] = exp_value(f1 >> 8);
+        const float k0 = exp_value(e0 & 255u), k1 = exp_value(e0 >> 8), k2 = exp_value(e1 & 255u), k3 = exp_value(e1 >> 8);
+        s[0][0] = s[0][0] * qa_scale * k0;
+        s[0][1] = s[0][1] * qa_scale * k1;
+        s[0][2] = s[0][2] * qb_scale * k0;
+        s[0][3] = s[0][3] * qb_scale * k1;
+        s[1][0] = s[1][0] * qa_scale * k2;
+        s[1][1] = s[1][1] * qa_scale * k3;
+        s[1][2] = s[1][2] * qb_scale * k2;
+        s[1][3] = s[1][3] * qb_scale * k3;
+        // The values' scales go into the probabilities, relative to the largest scale so far and times 2^5: with
+        // probabilities of at most 2^8 (below), their products stay below 2^15, and what fp16 holds with fewer
+        // bits is below 2^-27 of what it could hold.
+        const int32_t here = (int32_t)pc.key0 + (int32_t)(bi * kBlock) + (int32_t)t4 * 2;
+        const int v0 = (int)(f0 & 255u), v1 = (int)(f0 >> 8), v2 = (int)(f1 & 255u), v3 = (int)(f1 >> 8);
+        int top = max(max(v0 < kExpNan && here <= last ? v0 : 0, v1 < kExpNan && here + 1 <= last ? v1 : 0),
+                      max(v2 < kExpNan && here + 8 <= last ? v2 : 0, v3 < kExpNan && here + 9 <= last ? v3 : 0));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        if (top > ve + 1) {  // the same for the whole warp
+          const float f = ex2((float)(ve - top));
+          ve = top;
+#pragma unroll
+          for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+        }
+        const int off = kExpBias + 5 - ve;
+        vs[0] = exp_value(v0 == kExpNan ? kExpNan : (uint32_t)max(v0 + off, 0));
+        vs[1] = exp_value(v1 == kExpNan ? kExpNan : (uint32_t)max(v1 + off, 0));
+        vs[2] = exp_value(v2 == kExpNan ? kExpNan : (uint32_t)max(v2 + off, 0));
+        vs[3] = exp_value(v3 == kExpNan ? kExpNan : (uint32_t)max(v3 + off, 0));
       } else {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
@@ -296,8 +357,9 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           }
       }
       // ---- product with the values
-      const uint32_t pf[4] = {pack2<kFp16>(s[0][0], s[0][1]), pack2<kFp16>(s[0][2], s[0][3]),
-                              pack2<kFp16>(s[1][0], s[1][1]), pack2<kFp16>(s[1][2], s[1][3])};
+      constexpr bool kHalfP = kFp16 || kFp8;
+      const uint32_t pf[4] = {pack2<kHalfP>(s[0][0], s[0][1]), pack2<kHalfP>(s[0][2], s[0][3]),
+                              pack2<kHalfP>(s[1][0], s[1][1]), pack2<kHalfP>(s[1][2], s[1][3])};
       if constexpr (kFp8) {
         const uint32_t tok = (mi & 1) * 8 + mr;
 #pragma unroll
@@ -307,10 +369,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
             // a chunk's 16 columns: tile 2c has the even ones, tile 2c + 1 the odd ones
-            mma16816<false>(acc[2 * c + i], pf, e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x2404)),
-                            e4m3_to_bf16x2(__byte_perm(r[i + 1], 0, 0x2404)));
-            mma16816<false>(acc[2 * c + i + 1], pf, e4m3_to_bf16x2(__byte_perm(r[i], 0, 0x3414)),
-                            e4m3_to_bf16x2(__byte_perm(r[i + 1], 0, 0x3414)));
+            uint32_t even0, odd0, even1, odd1;
+            e4m3x4_to_f16x2(__byte_perm(r[i], 0, 0x3120), even0, odd0);
+            e4m3x4_to_f16x2(__byte_perm(r[i + 1], 0, 0x3120), even1, odd1);
+            mma16816<true>(acc[2 * c + i], pf, even0, even1);
+            mma16816<true>(acc[2 * c + i + 1], pf, odd0, odd1);
           }
         }
       } else {
@@ -361,6 +424,13 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
     }
 
     // ---- the piece's result
+    if constexpr (kFp8) {
+      const float f = __uint_as_float((uint32_t)max(ve - 5, 1) << 23);
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+    }
     la += __shfl_xor_sync(0xFFFFFFFFu, la, 1);
     lb += __shfl_xor_sync(0xFFFFFFFFu, lb, 1);
     la += __shfl_xor_sync(0xFFFFFFFFu, la, 2);

@@ -95,6 +95,7 @@ __device__ __forceinline__ uint4 quantise(const float (&x)[16], uint32_t* exp_co
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2] * inv, x[4 * i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
     c[i] = lo | (hi << 16);
   }
+  if (nan) code = make_uint4(0, 0, 0, 0);  // the scale marks the row; no code of the cache is a NaN
   *exp_code = nan ? kExpNan : (uint32_t)(e + kExpBias);
   return code;
 }

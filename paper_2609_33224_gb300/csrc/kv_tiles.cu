@@ -52,7 +52,6 @@ static_assert(192 * 256 + 64 * 256 <= 65536 && 208 * 256 + 88 * 128 <= 384 * 168
 
 struct Bars {
   uint64_t full[10], empty[10];  // operand ring
-  uint64_t peer_full[10];        // 16-bit pairs: the other CTA's part has arrived
   uint64_t raw_full[4], raw_empty[4];
   uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], tail_here, tail_done, drain;
   uint32_t tmem;
@@ -258,9 +257,9 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(full(i), C::kFp8 ? 4 * C::kCtas : 1);  // fp8: the converting warps, at the first CTA
+      // 16-bit: the copies, and at the first CTA of a pair the other's word; fp8: the converting warps
+      mbar_init(full(i), C::kFp8 ? 4 * C::kCtas : rank == 0 ? C::kCtas : 1);
       mbar_init(empty(i), 1);
-      mbar_init(smem_u32(&bars.peer_full[i]), 1);
     }
     for (int i = 0; i < C::kRaws; ++i) {
       mbar_init(smem_u32(&bars.raw_full[i]), 1);
@@ -557,10 +556,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         // ring order: keys 0, values 0, keys 1, values 1, ...: step j's keys are slot n0 + 2j, values n0 + 2j + 1
         const uint32_t n0 = n;
         auto slot = [&](uint32_t i) { return (n0 + i) % C::kSlots; };
-        auto here = [&](uint32_t i) {  // both CTAs' parts of a slot
-          const uint32_t par = ((n0 + i) / C::kSlots) & 1u;
-          return wait(full(slot(i)), par) && (C::kFp8 || C::kCtas == 1 || wait(smem_u32(&bars.peer_full[slot(i)]), par));
-        };
+        auto here = [&](uint32_t i) { return wait(full(slot(i)), ((n0 + i) / C::kSlots) & 1u); };
         here(0);
         for (uint32_t t = 0; t < tiles; ++t) {
           if (!wait(smem_u32(&bars.q_ready[t]), q_seen[t] & 1)) break;
@@ -577,7 +573,6 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             mbar_arrive(smem_u32(&bars.tail_here));
             if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
           }
-          if (more && !here(2 * j + 2)) break;
           for (uint32_t t = 0; t < tiles; ++t) {
             if (!wait(smem_u32(&bars.p_ready[t][0]), p_seen[t] & 1)) break;
             tc_fence_after();
@@ -587,6 +582,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             tc_fence_after();
             values(t, slot(2 * j + 1), 1, true);
             if (more) {
+              if (t == 0 && !here(2 * j + 2)) break;
               scores(t, slot(2 * j + 2));
               tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
             } else {
@@ -621,7 +617,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             mbar_arrive(smem_u32(&bars.tail_here));
             alive = mbar_wait(smem_u32(&bars.tail_done), tails++ & 1);
           }
-          if (alive) arrive_first<C::kCtas>(smem_u32(&bars.peer_full[at]));
+          if (alive) arrive_first<C::kCtas>(full(at));
         }
       }
       if (!alive) {
