@@ -151,14 +151,13 @@ def lib() -> ctypes.CDLL:
             "ps_score_window_noalloc": [vp, vp, vp, u32, ctypes.POINTER(PsStateArrays), ctypes.POINTER(PsWindow),
                                         ctypes.POINTER(PsModel), i32, ctypes.POINTER(PsScores), vp],
             "ps_kv_create": [ctypes.POINTER(PsKvConfig), ctypes.POINTER(vp)],
-            "ps_kv_write": [vp, ctypes.POINTER(PsKvRows), ctypes.POINTER(PsKvRows), vp, u64, vp],
-            "ps_kv_read": [vp, vp, u64, ctypes.POINTER(PsKvRows), ctypes.POINTER(PsKvRows), vp],
+            "ps_kv_write": [vp, vp, vp, vp, u64, vp],  # the two ps_kv_rows by address
+            "ps_kv_read": [vp, vp, u64, vp, vp, vp],
             "ps_kv_check": [vp, vp],
             "ps_kv_plan_create": [vp, u32, u32, u32, u64, ctypes.POINTER(vp)],
             "ps_kv_plan_set": [vp, u32, vp, u32, vp, u64],
             "ps_kv_plan_workspace": [vp, ctypes.POINTER(u64)],
-            "ps_kv_attend": [vp, vp, ctypes.POINTER(PsKvRows), ctypes.POINTER(PsKvRows), vp, ctypes.c_float, vp, u64,
-                             vp],
+            "ps_kv_attend": [vp, vp, vp, vp, vp, ctypes.c_float, vp, u64, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)

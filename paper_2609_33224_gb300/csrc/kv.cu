@@ -9,6 +9,7 @@
 
 #include "kv_internal.cuh"
 
+using pskv::Fold;
 using pskv::JoinEntry;
 using pskv::JoinSeg;
 using pskv::Piece;
@@ -132,15 +133,21 @@ using pskv::kTileKeys;
 constexpr uint32_t kTileLeastRows = 33;
 constexpr int64_t kTileLeastKeys = 256;
 
+// A piece joins up to this many tile parts into its rows.  They are read one after the other by one warp, about
+// 1.5 us each: with 10 parts (64 queries on 8192 shared tokens) that took 32 us more than the join kernel's 10,
+// with 2 to 3 (192 new tokens on 16384) 28 us less than it.
+constexpr size_t kFoldMost = 3;
+
 // Rows of one tile and one head over a range of key blocks, before it is cut into pieces.
 struct Unit {
   Piece p;             // block, key0: of the whole range
   uint32_t group;      // its entry of the groups
   uint32_t tile_rows;  // rows of its partial results
+  uint32_t layer;
 };
 
 Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t from, int64_t end, int step, int32_t climit,
-          uint32_t tile_rows, uint32_t group) {
+          uint32_t tile_rows, uint32_t group, uint32_t layer) {
   Unit u{};
   u.p.block = (uint32_t)(s.first_block + (uint64_t)from / kBlock);
   u.p.nblocks = (uint32_t)((end - from + step - 1) / step);
@@ -153,6 +160,7 @@ Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t fro
   u.p.head = (uint16_t)h;
   u.group = group;
   u.tile_rows = tile_rows;
+  u.layer = layer;
   return u;
 }
 
@@ -173,6 +181,7 @@ struct Layout {
   std::vector<uint32_t> row_off, tile_off, tok_off, tok_layer;
   std::vector<JoinEntry> join;
   std::vector<JoinSeg> segs;
+  std::vector<Fold> folds;
   uint64_t part_rows = 0;
   uint32_t max_parts = 1;
 };
@@ -239,7 +248,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
         if (c < kTileLeastKeys) c = 0;
         cut.push_back(c);
         for (uint32_t h = 0; h < H; ++h) {
-          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, (uint32_t)o.groups.size()));
+          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, (uint32_t)o.groups.size(), (uint32_t)o.layers.size() - 1));
           o.groups.push_back(Group{0, 0});
         }
       }
@@ -251,7 +260,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
       const int64_t from = cut.empty() ? 0 : cut[r0 / tile_rows];
       const int64_t end = s.causal ? std::min<int64_t>(len, (int64_t)climit + (r0 + nr - 1) / g + 1) : len;
       for (uint32_t h = 0; h < H; ++h) {
-        if (end > from) o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, (uint32_t)o.groups.size()));
+        if (end > from) o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, (uint32_t)o.groups.size(), (uint32_t)o.layers.size() - 1));
         o.groups.push_back(Group{0, 0});
       }
     }
@@ -273,13 +282,63 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
       for (uint32_t i = 0; i < o.layers[l].num_queries; ++i) o.tok_layer[at[o.layers[l].query0 + i]++] = (uint32_t)l;
   }
 
-  // pieces, and where their partial results go
-  auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first) {
+  // Pieces, and where their results go.  A group of one piece writes the output where nothing is to be joined,
+  // or, in the row kernel, which comes after the tile kernel, where only tiles are to be joined.
+  auto layers_of = [&](uint32_t t, uint32_t* n) {
+    *n = o.tok_off[t + 1] - o.tok_off[t];
+    return o.tok_layer.data() + o.tok_off[t];
+  };
+  auto fold = [&](const Unit& u, Piece* p) {
+    const size_t segs = o.segs.size(), folds = o.folds.size();
+    for (uint32_t i = 0, n; i < p->nrows; i += n) {
+      const uint32_t r = p->row0 + i, t = p->query0 + r / g;
+      uint32_t nl;
+      const uint32_t* ls = layers_of(t, &nl);
+      n = g - r % g;  // and the queries after it that have the same layers
+      for (uint32_t t2 = t + 1; i + n < p->nrows; ++t2, n += g) {
+        uint32_t nl2;
+        const uint32_t* ls2 = layers_of(t2, &nl2);
+        if (nl2 != nl || !std::equal(ls, ls + nl, ls2)) break;
+      }
+      n = std::min<uint32_t>(n, p->nrows - i);
+      const uint32_t seg0 = (uint32_t)o.segs.size();
+      for (uint32_t l = 0; l < nl; ++l) {
+        const Layer& ly = o.layers[ls[l]];
+        if (ls[l] == u.layer) continue;
+        if (ly.tile_rows <= (uint32_t)kSmallRows) {
+          o.segs.resize(segs);
+          o.folds.resize(folds);
+          return false;
+        }
+        n = std::min(n, ly.tile_rows - ((t - ly.query0) * g + r % g) % ly.tile_rows);
+      }
+      for (uint32_t l = 0; l < nl; ++l) {
+        const Layer& ly = o.layers[ls[l]];
+        if (ls[l] == u.layer) continue;
+        const uint32_t rr = (t - ly.query0) * g + r % g;
+        const Group& gr = o.groups[ly.group0 + rr / ly.tile_rows * H + p->head];
+        if (gr.nparts) o.segs.push_back(JoinSeg{gr.part_row + rr % ly.tile_rows, ly.tile_rows, gr.nparts});
+      }
+      o.folds.push_back(Fold{seg0, (uint16_t)(o.segs.size() - seg0), (uint8_t)i, (uint8_t)n});
+    }
+    uint32_t parts = 0;
+    for (size_t x = segs; x < o.segs.size(); ++x) parts += o.segs[x].nparts;
+    if (parts > kFoldMost * (o.folds.size() - folds)) {
+      o.segs.resize(segs);
+      o.folds.resize(folds);
+      return false;
+    }
+    p->fold0 = (uint32_t)folds;
+    p->nfold = (uint32_t)(o.folds.size() - folds);
+    return true;
+  };
+  auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
       const Piece& p = units[i].p;
       bool direct = b - a == 1;
       for (uint32_t q = p.row0 / g; direct && q <= (p.row0 + p.nrows - 1) / g; ++q) direct = alone[p.query0 + q];
+      if (!direct && rows && b - a == 1) direct = fold(units[i], &pieces[a]);
       Group& gr = o.groups[units[i].group];
       if (direct) {
         gr = Group{pskv::kDirect, 1};
@@ -295,13 +354,13 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     }
   };
   std::vector<uint32_t> first;
-  if (!o.row_units.empty()) {
-    share_out(o.row_units, (uint32_t)pl.kv->sms * pskv::kRowWarps, 2, 2, 1, &o.row_pieces, &o.row_off, &first);
-    finish(o.row_units, o.row_pieces, first);
-  }
   if (!o.tile_units.empty()) {
     share_out(o.tile_units, (uint32_t)(pl.kv->sms / pskv::tile_ctas_of((int)pl.kv->D)), 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
-    finish(o.tile_units, o.tile_pieces, first);
+    finish(o.tile_units, o.tile_pieces, first, false);
+  }
+  if (!o.row_units.empty()) {
+    share_out(o.row_units, (uint32_t)pl.kv->sms * pskv::kRowWarps, 2, 2, 1, &o.row_pieces, &o.row_off, &first);
+    finish(o.row_units, o.row_pieces, first, true);
   }
 
   // The rows of a query and head that have something to join, or no key at all; cut where one of the query's
@@ -402,7 +461,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   size_t at = 0;
   const size_t rp = place(&parts, &at, o.row_pieces), ro = place(&parts, &at, o.row_off);
   const size_t tp = place(&parts, &at, o.tile_pieces), to = place(&parts, &at, o.tile_off);
-  const size_t jn = place(&parts, &at, o.join), sg = place(&parts, &at, o.segs);
+  const size_t jn = place(&parts, &at, o.join), sg = place(&parts, &at, o.segs), fd = place(&parts, &at, o.folds);
   const size_t bl = at;
   parts.emplace_back(blocks, n_blocks * sizeof(uint32_t));
   at += n_blocks * sizeof(uint32_t);
@@ -432,6 +491,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.tile_workers = o.tile_off.empty() ? 0 : (uint32_t)o.tile_off.size() - 1;
   d.join = reinterpret_cast<const JoinEntry*>(b.dev + jn);
   d.segs = reinterpret_cast<const JoinSeg*>(b.dev + sg);
+  d.folds = reinterpret_cast<const Fold*>(b.dev + fd);
   d.njoin = (uint32_t)o.join.size();
   d.max_parts = o.max_parts;
   d.blocks = reinterpret_cast<const uint32_t*>(b.dev + bl);
@@ -629,8 +689,8 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   a.err = kv->err_dev;
   const int D = (int)kv->D;
   cudaError_t e = cudaSuccess;
-  if (pl->dev.row_workers) e = pskv::launch_rows(D, kv->fmt, a, pl->dev, s);
-  if (e == cudaSuccess && pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, s);
+  if (pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, s);
+  if (e == cudaSuccess && pl->dev.row_workers) e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0, s);
   if (e == cudaSuccess && pl->dev.njoin) e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev, s);
   if (!capturing) {  // also after a failed launch: the ones before it read the buffer
     const cudaError_t r = cudaEventRecord(b.used, s);

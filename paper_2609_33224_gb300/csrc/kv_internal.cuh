@@ -61,10 +61,11 @@ struct alignas(16) Piece {
   int32_t climit;     // the span's i-th query sees keys j <= climit + i
   uint32_t query0;    // the span's first query
   uint32_t row0;      // the tile's first row
-  uint32_t part_row;  // first row of the partial result, or kDirect: the only piece of its rows
+  uint32_t part_row;  // first row of the partial result, or kDirect: the output is written
   uint16_t nrows;
   uint16_t head;
-  uint32_t pad[3];
+  uint32_t fold0, nfold;  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in
+  uint32_t pad;
 };
 static_assert(sizeof(Piece) == 48, "Piece layout");
 constexpr uint32_t kDirect = 0xFFFFFFFFu;
@@ -80,6 +81,12 @@ struct JoinEntry {
 struct JoinSeg {
   uint32_t row, stride, nparts;
 };
+// The same for the rows first .. first + count - 1 of a piece.
+struct Fold {
+  uint32_t seg0;
+  uint16_t nsegs;
+  uint8_t first, count;
+};
 
 struct PlanDev {
   const Piece* row_pieces;
@@ -90,6 +97,7 @@ struct PlanDev {
   uint32_t tile_workers;  // CTAs, or pairs of them
   const JoinEntry* join;
   const JoinSeg* segs;
+  const Fold* folds;
   uint32_t njoin;
   uint32_t max_parts;
   const uint32_t* blocks;
@@ -123,7 +131,7 @@ struct StoreArgs {
 
 cudaError_t launch_write(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_read(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
-cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
+cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
 cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
@@ -178,6 +186,29 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
                "l"(src), "r"(bytes), "r"(bar)
                : "memory");
+}
+// A call's kernels are launched so that the next may start while the last one ends: a kernel lets the next one
+// start at once, and waits for the one before (and with it all earlier ones) where it reads their results, at
+// the latest before it ends.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, unsigned cluster, bool overlap,
+                   cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = overlap ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) {

@@ -14,6 +14,7 @@ template <int D, bool FP16, bool kWide>
 __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const PlanDev p) {
   constexpr int kV = D / 32;
   constexpr uint32_t kStep = kWide ? 8 : 1;
+  wait_for_last();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t row = kWide ? blockIdx.x : blockIdx.x * 8 + warp;
   if (row >= p.njoin * a.group) return;  // kWide: the whole CTA
@@ -105,10 +106,8 @@ cudaError_t go(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
   const uint32_t rows = p.njoin * a.group;
   // Few rows of many parts (one request on all SMs): a CTA a row.
   if (p.max_parts > 16)
-    join_kernel<D, FP16, true><<<rows, 256, 0, s>>>(a, p);
-  else
-    join_kernel<D, FP16, false><<<(rows + 7) / 8, 256, 0, s>>>(a, p);
-  return cudaGetLastError();
+    return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, true, s, a, p);
+  return launch(join_kernel<D, FP16, false>, (rows + 7) / 8, 256, 0, 1, true, s, a, p);
 }
 
 }  // namespace

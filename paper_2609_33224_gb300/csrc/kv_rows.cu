@@ -89,7 +89,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t worker = warp * p.row_ctas + blockIdx.x;  // neighbours in the plan go to different SMs
-  if (worker >= p.row_workers) return;                     // no barrier of the CTA is used
+  let_next_start();
+  if (worker >= p.row_workers) {  // no barrier of the CTA is used
+    wait_for_last();
+    return;
+  }
   const uint32_t ring = smem_u32(smem) + warp * kStages * kRec;
   const uint32_t bar = smem_u32(bars) + warp * kStages * 8;
   if (lane < kStages) mbar_init(bar + lane * 8, 1);
@@ -129,6 +133,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
   const uint32_t quad = lane / 4, t4 = lane % 4;  // row (or key, or column) of a fragment, place in the quad
   const uint32_t mi = lane / 8, mr = lane % 8;    // ldmatrix: matrix and row whose address this lane gives
   uint32_t st = 0, phase = 0;
+  bool waited = false;
 
   for (uint32_t pi = p.row_off[worker]; pi < piece_end; ++pi) {
     const Piece pc = p.row_pieces[pi];
@@ -203,6 +208,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           }
           mbar_wait(bar + st * 8, phase);
         }
+        wait_for_last();
         return;
       }
       // ---- scores
@@ -463,6 +469,50 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         if (t4 == 0) a.part_ml[pc.part_row + 8 + quad] = make_float2(mb, lb);
       }
     } else {
+      // The tile kernel's parts of these rows (the prefix that they share) are joined in here, which saves the
+      // write and the read of this part and, mostly, the join kernel.
+      if (pc.nfold && !waited) {
+        wait_for_last();
+        waited = true;
+      }
+      for (uint32_t fi = 0; fi < pc.nfold; ++fi) {
+        const Fold fo = p.folds[pc.fold0 + fi];
+        const bool ia = quad >= fo.first && quad < (uint32_t)fo.first + fo.count;
+        const bool ib = quad + 8 >= fo.first && quad + 8 < (uint32_t)fo.first + fo.count;
+        for (uint32_t x = 0; x < fo.nsegs; ++x) {
+          const JoinSeg sg = p.segs[fo.seg0 + x];
+          for (uint32_t k = 0; k < sg.nparts; ++k) {
+            const uint64_t at = (uint64_t)sg.row + (uint64_t)k * sg.stride + quad - fo.first;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              if (half ? !ib : !ia) continue;
+              float& m = half ? mb : ma;
+              float& l = half ? lb : la;
+              const float2 ml = a.part_ml[at + 8 * half];
+              const float* src = a.part + (at + 8 * half) * D;
+              const float n = fmaxf(m, ml.x);
+              const float f0 = m == n ? 1.0f : ex2(m - n), f1 = ml.x == n ? 1.0f : ex2(ml.x - n);
+              m = n;
+              l = l * f0 + ml.y * f1;
+#pragma unroll
+              for (int j = 0; j < kTiles; ++j) {
+                if (kFp8) {
+                  if (j & 1) continue;
+                  const float4 v = *reinterpret_cast<const float4*>(src + 8 * j + 4 * t4);
+                  acc[j][2 * half] = acc[j][2 * half] * f0 + v.x * f1;
+                  acc[j + 1][2 * half] = acc[j + 1][2 * half] * f0 + v.y * f1;
+                  acc[j][2 * half + 1] = acc[j][2 * half + 1] * f0 + v.z * f1;
+                  acc[j + 1][2 * half + 1] = acc[j + 1][2 * half + 1] * f0 + v.w * f1;
+                } else {
+                  const float2 v = *reinterpret_cast<const float2*>(src + 8 * j + 2 * t4);
+                  acc[j][2 * half] = acc[j][2 * half] * f0 + v.x * f1;
+                  acc[j][2 * half + 1] = acc[j][2 * half + 1] * f0 + v.y * f1;
+                }
+              }
+            }
+          }
+        }
+      }
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         if (half ? !vb : !va) continue;
@@ -487,6 +537,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
       }
     }
   }
+  if (!waited) wait_for_last();
 }
 
 template <int D, int FMT>
@@ -499,9 +550,8 @@ cudaError_t prepare_one() {
   return cudaFuncSetAttribute(rows_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FMT>());
 }
 template <int D, int FMT>
-cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
-  rows_kernel<D, FMT><<<p.row_ctas, kRowWarps * 32, smem_bytes<D, FMT>(), s>>>(a, p);
-  return cudaGetLastError();
+cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
+  return launch(rows_kernel<D, FMT>, p.row_ctas, kRowWarps * 32, smem_bytes<D, FMT>(), 1, overlap, s, a, p);
 }
 
 }  // namespace
@@ -516,14 +566,14 @@ cudaError_t prepare_rows(int D, int fmt) {
                              : prepare_one<64, PS_KV_FP8>();
 }
 
-cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   if (D == 128)
-    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, s)
-           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, s)
-                               : launch_one<128, PS_KV_FP8>(a, p, s);
-  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, s)
-         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, s)
-                             : launch_one<64, PS_KV_FP8>(a, p, s);
+    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, overlap, s)
+           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, overlap, s)
+                               : launch_one<128, PS_KV_FP8>(a, p, overlap, s);
+  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, overlap, s)
+         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, overlap, s)
+                             : launch_one<64, PS_KV_FP8>(a, p, overlap, s);
 }
 
 }  // namespace pskv

@@ -255,6 +255,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   auto full = [&](uint32_t i) { return smem_u32(&bars.full[i]); };
   auto empty = [&](uint32_t i) { return smem_u32(&bars.empty[i]); };
 
+  let_next_start();
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
       // 16-bit: the copies, and at the first CTA of a pair the other's word; fp8: the converting warps
@@ -724,18 +725,7 @@ cudaError_t prepare_one() {
 template <int D, int FMT>
 cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
   using C = Cfg<D, FMT>;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(p.tile_workers * C::kCtas);
-  cfg.blockDim = dim3(C::kWarps * 32);
-  cfg.dynamicSmemBytes = C::kSmem;
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = C::kCtas;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tiles_kernel<D, FMT>, a, p);
+  return launch(tiles_kernel<D, FMT>, p.tile_workers * C::kCtas, C::kWarps * 32, C::kSmem, C::kCtas, false, s, a, p);
 }
 
 }  // namespace

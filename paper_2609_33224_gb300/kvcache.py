@@ -9,6 +9,7 @@ without waiting for it; what a kernel finds wrong raises ``PSError`` from the ne
 from __future__ import annotations
 
 import ctypes
+import struct
 import weakref
 
 import numpy as np
@@ -19,6 +20,9 @@ from . import PS_OK, PSError, PsKvConfig, PsKvRows, lib
 FORMATS = {"bf16": 0, "fp16": 1, "fp8": 2}
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 3}
 BLOCK_TOKENS = 16
+_ROWS = struct.Struct("@Pqqi4x")  # ps_kv_rows
+assert _ROWS.size == ctypes.sizeof(PsKvRows)
+_stream = torch._C._cuda_getCurrentRawStream  # torch's current stream of a device, as a number
 # ps_kv_span: a run of cached tokens (their blocks start at first_block of the plan's block array) and the
 # queries that see it; causal: the last num_queries tokens are the queries' own
 SPAN_DTYPE = np.dtype([("first_query", np.uint32), ("num_queries", np.uint32), ("length", np.uint64),
@@ -48,6 +52,10 @@ class KVCache:
         self._h = h
         self._lib = lib()
         self._plans = weakref.WeakSet()
+        self._device = torch.device("cuda", self.device)
+        self._args = (ctypes.c_char * (2 * _ROWS.size))()
+        self._arg0 = ctypes.addressof(self._args)
+        self._arg1 = self._arg0 + _ROWS.size
 
     def _check(self, s: int):
         if s != PS_OK:
@@ -78,47 +86,61 @@ class KVCache:
             raise ValueError("the cache is closed")
         return self._h
 
-    def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
-
-    def _rows(self, x, name: str, n: int, heads: int) -> PsKvRows:
-        if x.device.type != "cuda" or x.device.index != self.device:
-            raise ValueError(f"{name} must be a tensor on cuda:{self.device}")
+    # The calls below are made once per layer and step, and a small one's kernel takes no longer than its call:
+    # descriptors are packed into one buffer of the cache, and tensors are asked for nothing twice.
+    def _rows(self, at: int, x, name: str, n: int, heads: int):
+        """Packs x's ps_kv_rows at slot ``at`` of the cache's buffer."""
         t = _TYPES.get(x.dtype)
-        if t is None:
-            raise ValueError(f"{name} must be bfloat16, float16 or float32, not {x.dtype}")
-        if x.dim() != 3 or x.shape[0] != n or x.shape[1] != heads or x.shape[2] != self.head_dim:
-            raise ValueError(f"{name} must have shape {(n, heads, self.head_dim)}, not {tuple(x.shape)}")
         st = x.stride()
-        if st[2] != 1:
+        if x.get_device() != self.device or t is None or x.shape != (n, heads, self.head_dim) or st[2] != 1:
+            if x.get_device() != self.device:
+                raise ValueError(f"{name} must be a tensor on cuda:{self.device}")
+            if t is None:
+                raise ValueError(f"{name} must be bfloat16, float16 or float32, not {x.dtype}")
+            if tuple(x.shape) != (n, heads, self.head_dim):
+                raise ValueError(f"{name} must have shape {(n, heads, self.head_dim)}, not {tuple(x.shape)}")
             raise ValueError(f"{name}'s head_dim elements must lie next to each other")
-        return PsKvRows(x.data_ptr(), st[0], st[1], t)
+        _ROWS.pack_into(self._args, at, x.data_ptr(), st[0], st[1], t)
+
+    def _out(self, at: int, x, name: str, n: int, heads: int, dtype):
+        """Packs the result tensor x, or a new one of ``dtype``."""
+        if x is not None:
+            if dtype is not None and x.dtype != dtype:
+                raise ValueError(f"{name} is not of the dtype asked for")
+            self._rows(at, x, name, n, heads)
+            return x
+        dtype = dtype or self.dtype
+        t = _TYPES.get(dtype)
+        if t is None:
+            raise ValueError(f"dtype must be bfloat16, float16 or float32, not {dtype}")
+        x = torch.empty((n, heads, self.head_dim), dtype=dtype, device=self._device)
+        _ROWS.pack_into(self._args, at, x.data_ptr(), heads * self.head_dim, self.head_dim, t)
+        return x
 
     def _slots(self, slots) -> int:
-        if slots.dtype != torch.int64 or slots.dim() != 1 or slots.device.type != "cuda" or \
-                slots.device.index != self.device or not slots.is_contiguous():
+        if slots.dtype != torch.int64 or slots.dim() != 1 or slots.get_device() != self.device or \
+                not slots.is_contiguous():
             raise ValueError(f"slots must be a contiguous int64 vector on cuda:{self.device}")
         return slots.shape[0]
 
     def write(self, k, v, slots):
         """Store row t of k and v ([T, kv_heads, head_dim]) at slot ``slots[t]`` (int64; negative: skipped)."""
         h, n = self._open(), self._slots(slots)
-        rk, rv = self._rows(k, "k", n, self.kv_heads), self._rows(v, "v", n, self.kv_heads)
-        self._check(self._lib.ps_kv_write(h, rk, rv, slots.data_ptr(), n, self._stream()))
+        self._rows(0, k, "k", n, self.kv_heads)
+        self._rows(_ROWS.size, v, "v", n, self.kv_heads)
+        s = self._lib.ps_kv_write(h, self._arg0, self._arg1, slots.data_ptr(), n, _stream(self.device))
+        if s:
+            self._check(s)
 
     def read(self, slots, dtype=None, k=None, v=None):
         """The cached keys and values at ``slots``, as (k, v) of ``dtype`` (default: ``self.dtype``) or in the
         tensors given; a negative slot gives zeros."""
         h, n = self._open(), self._slots(slots)
-        shape = (n, self.kv_heads, self.head_dim)
-        if k is None:
-            k = torch.empty(shape, dtype=dtype or self.dtype, device=slots.device)
-        if v is None:
-            v = torch.empty(shape, dtype=dtype or self.dtype, device=slots.device)
-        if dtype is not None and (k.dtype != dtype or v.dtype != dtype):
-            raise ValueError("k and v are not of the dtype asked for")
-        rk, rv = self._rows(k, "k", n, self.kv_heads), self._rows(v, "v", n, self.kv_heads)
-        self._check(self._lib.ps_kv_read(h, slots.data_ptr(), n, rk, rv, self._stream()))
+        k = self._out(0, k, "k", n, self.kv_heads, dtype)
+        v = self._out(_ROWS.size, v, "v", n, self.kv_heads, dtype)
+        s = self._lib.ps_kv_read(h, slots.data_ptr(), n, self._arg0, self._arg1, _stream(self.device))
+        if s:
+            self._check(s)
         return k, v
 
     def attend(self, q, plan: "AttentionPlan", scale: float | None = None, out=None, lse=None):
@@ -129,22 +151,23 @@ class KVCache:
         """
         h, p = self._open(), plan._open()
         n, heads = plan.num_queries, plan.q_heads
-        if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=q.device)
-        rq, ro = self._rows(q, "q", n, heads), self._rows(out, "out", n, heads)
+        self._rows(0, q, "q", n, heads)
+        out = self._out(_ROWS.size, out, "out", n, heads, None if out is not None else q.dtype)
         if lse is not None and (lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or
                                 tuple(lse.shape) != (n, heads)):
             raise ValueError(f"lse must be a contiguous float32 tensor of shape {(n, heads)} on q's device")
         nb = plan.workspace_bytes
-        ws = torch.empty(nb, dtype=torch.uint8, device=q.device) if nb else None
-        self._check(self._lib.ps_kv_attend(h, p, rq, ro, None if lse is None else lse.data_ptr(),
-                                           self.head_dim ** -0.5 if scale is None else scale,
-                                           None if ws is None else ws.data_ptr(), nb, self._stream()))
+        ws = torch.empty(nb, dtype=torch.uint8, device=self._device) if nb else None
+        s = self._lib.ps_kv_attend(h, p, self._arg0, self._arg1, None if lse is None else lse.data_ptr(),
+                                   self.head_dim ** -0.5 if scale is None else scale,
+                                   None if ws is None else ws.data_ptr(), nb, _stream(self.device))
+        if s:
+            self._check(s)
         return out
 
     def check(self):
         """Wait for the current stream and raise what kernels have reported since the last report."""
-        self._check(self._lib.ps_kv_check(self._open(), self._stream()))
+        self._check(self._lib.ps_kv_check(self._open(), _stream(self.device)))
 
 
 class AttentionPlan:
