@@ -133,10 +133,11 @@ using pskv::kTileKeys;
 constexpr uint32_t kTileLeastRows = 33;
 constexpr int64_t kTileLeastKeys = 256;
 
-// A piece joins up to this many tile parts into its rows.  They are read one after the other by one warp, about
-// 1.5 us each: with 10 parts (64 queries on 8192 shared tokens) that took 32 us more than the join kernel's 10,
-// with 2 to 3 (192 new tokens on 16384) 28 us less than it.
-constexpr size_t kFoldMost = 3;
+// A piece of the row kernel joins up to this many tile parts into its rows, where a worker has at least so many
+// units of rows that the time this takes evens out.  192 new tokens on 16384 (4 units a worker, 2 to 3 parts):
+// 456 us, 491 with the join kernel; 256 queries on 32768 (1 unit a worker, 3 parts) 288 and 277 us, 64 on 8192
+// (10 parts) 92 and 60.
+constexpr size_t kFoldMost = 3, kFoldUnits = 3;
 
 // Rows of one tile and one head over a range of key blocks, before it is cut into pieces.
 struct Unit {
@@ -146,23 +147,6 @@ struct Unit {
   uint32_t layer;
 };
 
-Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t from, int64_t end, int step, int32_t climit,
-          uint32_t tile_rows, uint32_t group, uint32_t layer) {
-  Unit u{};
-  u.p.block = (uint32_t)(s.first_block + (uint64_t)from / kBlock);
-  u.p.nblocks = (uint32_t)((end - from + step - 1) / step);
-  u.p.key0 = (uint32_t)from;
-  u.p.end = (uint32_t)end;
-  u.p.climit = climit;
-  u.p.query0 = s.first_query;
-  u.p.row0 = r0;
-  u.p.nrows = (uint16_t)nr;
-  u.p.head = (uint16_t)h;
-  u.group = group;
-  u.tile_rows = tile_rows;
-  u.layer = layer;
-  return u;
-}
 
 // The rows of a span, tiled one way; tile t and head h have the parts groups[group0 + t * kv_heads + h].
 struct Layer {
@@ -185,6 +169,25 @@ struct Layout {
   uint64_t part_rows = 0;
   uint32_t max_parts = 1;
 };
+
+// A unit of the layer and group that come last.
+Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t from, int64_t end, int step, int32_t climit,
+          uint32_t tile_rows, const Layout& o) {
+  Unit u{};
+  u.p.block = (uint32_t)(s.first_block + (uint64_t)from / kBlock);
+  u.p.nblocks = (uint32_t)((end - from + step - 1) / step);
+  u.p.key0 = (uint32_t)from;
+  u.p.end = (uint32_t)end;
+  u.p.climit = climit;
+  u.p.query0 = s.first_query;
+  u.p.row0 = r0;
+  u.p.nrows = (uint16_t)nr;
+  u.p.head = (uint16_t)h;
+  u.group = (uint32_t)o.groups.size();
+  u.tile_rows = tile_rows;
+  u.layer = (uint32_t)o.layers.size() - 1;
+  return u;
+}
 
 // Cuts units into pieces for at most `most` workers with equal shares of the work; a piece costs its steps
 // and `extra` (its rows' load and result).  Every worker gets whole steps; a remainder of one step stays
@@ -248,7 +251,8 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
         if (c < kTileLeastKeys) c = 0;
         cut.push_back(c);
         for (uint32_t h = 0; h < H; ++h) {
-          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, (uint32_t)o.groups.size(), (uint32_t)o.layers.size() - 1));
+          if (c > 0)
+            o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, o));
           o.groups.push_back(Group{0, 0});
         }
       }
@@ -260,7 +264,7 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
       const int64_t from = cut.empty() ? 0 : cut[r0 / tile_rows];
       const int64_t end = s.causal ? std::min<int64_t>(len, (int64_t)climit + (r0 + nr - 1) / g + 1) : len;
       for (uint32_t h = 0; h < H; ++h) {
-        if (end > from) o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, (uint32_t)o.groups.size(), (uint32_t)o.layers.size() - 1));
+        if (end > from) o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, o));
         o.groups.push_back(Group{0, 0});
       }
     }
@@ -332,13 +336,15 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     p->nfold = (uint32_t)(o.folds.size() - folds);
     return true;
   };
+  const uint32_t row_workers = (uint32_t)(pl.kv->sms * pskv::row_warps_of(pl.kv->fmt));
+  const bool may_fold = o.row_units.size() >= kFoldUnits * row_workers;
   auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
       const Piece& p = units[i].p;
       bool direct = b - a == 1;
       for (uint32_t q = p.row0 / g; direct && q <= (p.row0 + p.nrows - 1) / g; ++q) direct = alone[p.query0 + q];
-      if (!direct && rows && b - a == 1) direct = fold(units[i], &pieces[a]);
+      if (!direct && rows && may_fold && b - a == 1) direct = fold(units[i], &pieces[a]);
       Group& gr = o.groups[units[i].group];
       if (direct) {
         gr = Group{pskv::kDirect, 1};
@@ -355,11 +361,12 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
   };
   std::vector<uint32_t> first;
   if (!o.tile_units.empty()) {
-    share_out(o.tile_units, (uint32_t)(pl.kv->sms / pskv::tile_ctas_of((int)pl.kv->D)), 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
+    const uint32_t workers = (uint32_t)(pl.kv->sms / pskv::tile_ctas_of((int)pl.kv->D));
+    share_out(o.tile_units, workers, 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
     finish(o.tile_units, o.tile_pieces, first, false);
   }
   if (!o.row_units.empty()) {
-    share_out(o.row_units, (uint32_t)pl.kv->sms * pskv::kRowWarps, 2, 2, 1, &o.row_pieces, &o.row_off, &first);
+    share_out(o.row_units, row_workers, 2, 2, 1, &o.row_pieces, &o.row_off, &first);
     finish(o.row_units, o.row_pieces, first, true);
   }
 

@@ -136,7 +136,10 @@ cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, c
 cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
 cudaError_t prepare_tiles(int D, int fmt);
-constexpr int kRowWarps = 8;  // workers (warps) of a CTA of the row kernel
+// Workers (warps) of a CTA of the row kernel.  fp8 blocks take as many instructions as 16-bit ones of twice the
+// bytes: 12 warps hide more of their latency (131072 tokens of 5 requests: 182 us, 187 with 8); 16-bit ones are
+// bound by bytes with 8 (64 requests on a prefix: 58 us, 59 with 12, whose shares are shorter).
+__host__ __device__ constexpr int row_warps_of(int fmt) { return fmt == PS_KV_FP8 ? 12 : 8; }
 
 // ---- PTX ----------------------------------------------------------------------------------------------
 

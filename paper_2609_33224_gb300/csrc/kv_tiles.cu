@@ -98,11 +98,17 @@ __device__ __forceinline__ void arrive_first(uint32_t bar) {
     mbar_arrive(bar);
 }
 template <int CTAS>
+__device__ __forceinline__ void arrive_worker() {
+  if (CTAS == 2) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+template <int CTAS>
+__device__ __forceinline__ void wait_worker() {
+  if (CTAS == 2) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <int CTAS>
 __device__ __forceinline__ void sync_worker() {
-  if (CTAS == 2)
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-  else
-    __syncthreads();
+  arrive_worker<CTAS>();
+  wait_worker<CTAS>();
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -256,7 +262,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   auto empty = [&](uint32_t i) { return smem_u32(&bars.empty[i]); };
 
   let_next_start();
-  if (threadIdx.x == 0) {
+  const uint32_t first = p.tile_off[worker], last = p.tile_off[worker + 1];
+  if (warp == 8 && lane == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
       // 16-bit: the copies, and at the first CTA of a pair the other's word; fp8: the converting warps
       mbar_init(full(i), C::kFp8 ? 4 * C::kCtas : rank == 0 ? C::kCtas : 1);
@@ -279,19 +286,24 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) tc_alloc<C::kCtas>(smem_u32(&bars.tmem), 512);
-  tc_fence_before();
-  __syncthreads();
-  sync_worker<C::kCtas>();
-  tc_fence_after();
-  const uint32_t tmem = bars.tmem;
-  const uint32_t first = p.tile_off[worker], last = p.tile_off[worker + 1];
+  // Every warp comes here once before it uses a barrier that others set up, tensor memory or the other CTA: the
+  // softmax when its first queries are on their way.  The copying warp only says that it has set the barriers
+  // up; it has to be met before it waits for anything but its own copies.
+  auto all_here = [&]() {
+    __syncwarp();
+    tc_fence_before();
+    asm volatile("barrier.cta.sync 1, %0;" ::"n"(C::kWarps * 32) : "memory");
+    sync_worker<C::kCtas>();
+    tc_fence_after();
+    return bars.tmem;
+  };
 
   if (warp < 8) {
     // ================= softmax: warpgroup t owns tile t, thread r its row r =================
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRegSoft));
     const uint32_t t = warp / 4, r = threadIdx.x % 128;
-    const uint32_t s_addr = tmem + t * 128 + ((warp % 4) * 32 << 16);
-    const uint32_t o_addr = tmem + 256 + t * 128 + ((warp % 4) * 32 << 16);
+    uint32_t s_addr = 0, o_addr = 0;
+    bool here = false;
     const float sc = fmaxf(fabsf(a.scale_log2), 1.2e-38f);  // a scale of 0 still sends masked scores to -inf
     const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
     uint32_t steps = 0, done = 0;  // phases of s_full; of o_done
@@ -315,6 +327,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, from);
           const bool ok = __shfl_sync(0xFFFFFFFFu, (int)valid, from) != 0;
           w[i] = ok ? *reinterpret_cast<const uint4*>(a.q + at + 8 * c) : make_uint4(0, 0, 0, 0);
+        }
+        if (!here) {
+          const uint32_t tmem = all_here();
+          here = true;
+          s_addr = tmem + t * 128 + ((warp % 4) * 32 << 16);
+          o_addr = s_addr + 256;
         }
 #pragma unroll
         for (int i = 0; i < 32 / kAt; ++i) {
@@ -460,6 +478,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       }
       tc_fence_before();  // the reads of O before the next piece's products, which p_ready orders
     }
+    if (!here) all_here();
     if (!alive && r == 0) atomicOr_system(a.err, kErrWait);
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
@@ -497,7 +516,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         to[0] = C::kRawK + C::kRawV + (lane - 16) * 32;
         bytes[0] = 32;
       }
-      bool alive = true;
+      __syncwarp();
+      asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kWarps * 32) : "memory");
+      arrive_worker<C::kCtas>();
+      bool alive = true, begun = false;
       for (uint32_t pi = first; alive && pi < last; ++pi) {
         const Piece* pp = p.tile_pieces + pi;
         const uint32_t steps = pp->nblocks, block = pp->block, head = pp->head, key0 = pp->key0, end = pp->end;
@@ -510,9 +532,13 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             const uint32_t at = n % kN;
             const uint32_t fb = C::kFp8 ? smem_u32(&bars.raw_full[at % 4]) : full(at);
             const uint32_t eb = C::kFp8 ? smem_u32(&bars.raw_empty[at % 4]) : empty(at);
-            if (n >= kN && !mbar_wait_warp(eb, (n / kN - 1) & 1)) {
-              alive = false;
-              break;
+            if (n >= kN) {
+              if (!begun) wait_worker<C::kCtas>();
+              begun = true;
+              if (!mbar_wait_warp(eb, (n / kN - 1) & 1)) {
+                alive = false;
+                break;
+              }
             }
             const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, (j & 3u) * 8 + blk[part]);
             const uint32_t mine = blk[part] < live ? bytes[part] : 0u;
@@ -525,10 +551,13 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           }
         }
       }
+      if (!begun) wait_worker<C::kCtas>();
       for (uint32_t i = n > kN ? n - kN : 0; i < n; ++i)  // no copy is left in flight
         alive &= mbar_wait_warp(C::kFp8 ? smem_u32(&bars.raw_full[i % kN % 4]) : full(i % kN), (i / kN) & 1);
       if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
-    } else if (warp == 9 && rank == 0 && elect_one()) {
+    } else {
+    const uint32_t tmem = all_here();
+    if (warp == 9 && rank == 0 && elect_one()) {
       // ================= products: one thread waits and issues =================
       constexpr uint32_t id_s = instruction(C::kFp16, C::kRows, kTileKeys, false), id_o = instruction(C::kFp16, C::kRows, D, true);
       uint32_t n = 0;  // slots taken
@@ -648,10 +677,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       }
       if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
     }
+    }
   } else {
     // ================= fp8: records to operands, a thread a token =================
     if constexpr (C::kFp8) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
+      all_here();
       const uint32_t tok = threadIdx.x % 128;
       const uint32_t kt = tok % C::kKeys, kb = kt / kBlock, vb = tok / kBlock;  // this thread's key; blocks
       constexpr int kChunks = D / 16 / C::kCtas;                               // and chunks of it: 4
@@ -708,7 +739,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   __syncthreads();
   sync_worker<C::kCtas>();  // no CTA leaves while the other may arrive on its barriers or read its memory
   tc_fence_after();
-  if (warp == 9) tc_dealloc<C::kCtas>(tmem, 512);
+  if (warp == 9) tc_dealloc<C::kCtas>(bars.tmem, 512);
 }
 
 template <int D, int FMT>
