@@ -97,18 +97,15 @@ __device__ __forceinline__ void arrive_first(uint32_t bar) {
   else
     mbar_arrive(bar);
 }
+// The relaxed arrival publishes the barriers' set-up (after fence.mbarrier_init) and nothing else, and does not wait for
+// the copies in flight, as a releasing one does (3 us when the ring has just been asked for).
 template <int CTAS>
 __device__ __forceinline__ void arrive_worker() {
-  if (CTAS == 2) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  if (CTAS == 2) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 }
 template <int CTAS>
 __device__ __forceinline__ void wait_worker() {
   if (CTAS == 2) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-template <int CTAS>
-__device__ __forceinline__ void sync_worker() {
-  arrive_worker<CTAS>();
-  wait_worker<CTAS>();
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -293,7 +290,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     __syncwarp();
     tc_fence_before();
     asm volatile("barrier.cta.sync 1, %0;" ::"n"(C::kWarps * 32) : "memory");
-    sync_worker<C::kCtas>();
+    arrive_worker<C::kCtas>();
+    wait_worker<C::kCtas>();
     tc_fence_after();
     return bars.tmem;
   };
@@ -737,7 +735,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  sync_worker<C::kCtas>();  // no CTA leaves while the other may arrive on its barriers or read its memory
+  arrive_worker<C::kCtas>();
+  wait_worker<C::kCtas>();  // no CTA leaves while the other may arrive on its barriers or read its memory
   tc_fence_after();
   if (warp == 9) tc_dealloc<C::kCtas>(bars.tmem, 512);
 }
