@@ -1,19 +1,23 @@
 // Joining the partial results of a query's rows: those of the spans that cover it and of the pieces that a
 // span's keys were cut into.
+#include <type_traits>
+
 #include "kv_internal.cuh"
 
 namespace pskv {
 namespace {
 
 // One (query, q head) row per warp, or with kWide per CTA of 8 warps, which share its parts.  Up to 32 parts at
-// a time: each lane takes one part's maximum m_k and sum l_k, then all lanes add the parts' D values, D / 32 a
-// lane, with the weights 2^(m_k - M): the loads of the values do not wait for one another.
+// a time: each lane finds one part and takes its maximum m_k and sum l_k, then all lanes add the parts' D
+// values, D / 32 a lane, with the weights 2^(m_k - M).  The loads of the first four parts' values wait for
+// nothing but the parts' places: few rows are bound by the chain of dependent loads.
 // out = sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k with the running maximum M, in 32 bits.
 // Bound by the bytes of the parts (D * 4 + 8 each), which the attention kernels left in L2.
 template <int D, bool FP16, bool kWide>
-__global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const PlanDev p) {
-  constexpr int kV = D / 32;
-  constexpr uint32_t kStep = kWide ? 8 : 1;
+__global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const PlanDev p) {
+  constexpr int kV = D / 32, kAhead = 4;
+  constexpr uint32_t kStep = kWide ? 8 : 1, kFull = 0xFFFFFFFFu;
+  using Vec = typename std::conditional<kV == 4, float4, float2>::type;
   wait_for_last();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t row = kWide ? blockIdx.x : blockIdx.x * 8 + warp;
@@ -23,43 +27,62 @@ __global__ void __launch_bounds__(256) join_kernel(const AttnArgs a, const PlanD
   if (gi >= en.count) return;  // the same
   const uint32_t query = en.query, head = en.head0 + gi;
 
+  const float* part = a.part + lane * kV;
   float m = -INFINITY, l = 0.0f, acc[kV];
 #pragma unroll
   for (int i = 0; i < kV; ++i) acc[i] = 0.0f;
-  for (uint32_t x = 0; x < en.nsegs; ++x) {
-    const JoinSeg sg = p.segs[en.seg0 + x];
-    const uint64_t at0 = (uint64_t)sg.row + gi, stride = (uint64_t)sg.stride * kStep;
-    const uint64_t base = at0 + (kWide ? (uint64_t)warp * sg.stride : 0);
-    const uint32_t n = kWide ? (sg.nparts + 7 - warp) / 8 : sg.nparts;  // this warp's parts
-    for (uint32_t c = 0; c < n; c += 32) {
-      const uint32_t cnt = min(32u, n - c);
+  auto add = [&](const Vec& v, float w) {
+    acc[0] = fmaf(v.x, w, acc[0]);
+    acc[1] = fmaf(v.y, w, acc[1]);
+    if constexpr (kV == 4) {
+      acc[2] = fmaf(v.z, w, acc[2]);
+      acc[3] = fmaf(v.w, w, acc[3]);
+    }
+  };
+  for (uint32_t s0 = 0; s0 < en.nsegs; s0 += 32) {
+    const uint32_t ns = min(32u, en.nsegs - s0);
+    JoinSeg sg{0, 0, 0};
+    if (lane < ns) sg = p.segs[en.seg0 + s0 + lane];
+    const uint32_t total = __reduce_add_sync(kFull, sg.nparts);
+    for (uint32_t c = kWide ? warp : 0; c < total; c += 32 * kStep) {
+      const uint32_t mine = c + lane * kStep;
+      const uint32_t cnt = min(32u, (total - c + kStep - 1) / kStep);
+      uint32_t at = 0;
+      for (uint32_t s = 0, start = 0; s < ns; ++s) {
+        const uint32_t np = __shfl_sync(kFull, sg.nparts, s), r0 = __shfl_sync(kFull, sg.row, s);
+        const uint32_t st = __shfl_sync(kFull, sg.stride, s);
+        if (mine >= start && mine - start < np) at = r0 + gi + (mine - start) * st;
+        start += np;
+      }
       float2 ml = make_float2(-INFINITY, 0.0f);
-      if (lane < cnt) ml = a.part_ml[base + (uint64_t)(c + lane) * stride];
+      if (lane < cnt) ml = a.part_ml[at];
+      Vec ahead[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t ak = __shfl_sync(kFull, at, k);
+        if (k < (int)cnt) ahead[k] = *reinterpret_cast<const Vec*>(part + (uint64_t)ak * D);
+      }
       float mm = ml.x;
-      for (uint32_t o = 16; o; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xFFFFFFFFu, mm, o));
+      for (uint32_t o = 16; o; o >>= 1) mm = fmaxf(mm, __shfl_xor_sync(kFull, mm, o));
       mm = fmaxf(mm, m);
       const float f = m == mm ? 1.0f : ex2(m - mm);
       m = mm;
-      float w = lane < cnt ? (ml.x == mm ? 1.0f : ex2(ml.x - mm)) : 0.0f;
+      const float w = lane < cnt ? (ml.x == mm ? 1.0f : ex2(ml.x - mm)) : 0.0f;
       float wl = w * ml.y;
-      for (uint32_t o = 16; o; o >>= 1) wl += __shfl_xor_sync(0xFFFFFFFFu, wl, o);
+      for (uint32_t o = 16; o; o >>= 1) wl += __shfl_xor_sync(kFull, wl, o);
       l = l * f + wl;
 #pragma unroll
       for (int i = 0; i < kV; ++i) acc[i] *= f;
-#pragma unroll 4
-      for (uint32_t k = 0; k < cnt; ++k) {
-        const float* src = a.part + (base + (uint64_t)(c + k) * stride) * D + lane * kV;
-        float v[kV];
-        if (kV == 4) {
-          const float4 y = *reinterpret_cast<const float4*>(src);
-          v[0] = y.x; v[1] = y.y; v[kV - 2] = y.z; v[kV - 1] = y.w;
-        } else {
-          const float2 y = *reinterpret_cast<const float2*>(src);
-          v[0] = y.x; v[1] = y.y;
-        }
-        const float wk = __shfl_sync(0xFFFFFFFFu, w, k);
 #pragma unroll
-        for (int i = 0; i < kV; ++i) acc[i] = fmaf(v[i], wk, acc[i]);
+      for (int k = 0; k < kAhead; ++k) {
+        const float wk = __shfl_sync(kFull, w, k);
+        if (k < (int)cnt) add(ahead[k], wk);
+      }
+#pragma unroll 4
+      for (uint32_t k = kAhead; k < cnt; ++k) {
+        const uint32_t ak = __shfl_sync(kFull, at, k);
+        const float wk = __shfl_sync(kFull, w, k);
+        add(*reinterpret_cast<const Vec*>(part + (uint64_t)ak * D), wk);
       }
     }
   }
