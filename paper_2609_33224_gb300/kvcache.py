@@ -156,11 +156,12 @@ class KVCache:
         if lse is not None and (lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or
                                 tuple(lse.shape) != (n, heads)):
             raise ValueError(f"lse must be a contiguous float32 tensor of shape {(n, heads)} on q's device")
+        stream = _stream(self.device)
         nb = plan.workspace_bytes
-        ws = torch.empty(nb, dtype=torch.uint8, device=self._device) if nb else None
+        ws = plan._workspace(stream, nb) if nb else None
         s = self._lib.ps_kv_attend(h, p, self._arg0, self._arg1, None if lse is None else lse.data_ptr(),
                                    self.head_dim ** -0.5 if scale is None else scale,
-                                   None if ws is None else ws.data_ptr(), nb, _stream(self.device))
+                                   None if ws is None else ws.data_ptr(), nb, stream)
         if s:
             self._check(s)
         return out
@@ -186,12 +187,22 @@ class AttentionPlan:
         self.cache, self.q_heads, self.num_queries, self.workspace_bytes = cache, limits[0], 0, 0
         cache._check(cache._lib.ps_kv_plan_create(cache._open(), *limits, ctypes.byref(h)))
         self._h = h
+        self._spaces = {}  # workspace by stream: a stream's calls run one after the other
         cache._plans.add(self)
 
     def _open(self):
         if not self._h:
             raise ValueError("the plan is closed")
         return self._h
+
+    def _workspace(self, stream: int, nbytes: int):
+        if torch.cuda.is_current_stream_capturing():  # a graph's own: it may run beside other calls
+            return torch.empty(nbytes, dtype=torch.uint8, device=self.cache._device)
+        ws = self._spaces.get(stream)
+        if ws is None or ws.numel() < nbytes:
+            # a quarter more than asked for: the next steps' batches grow
+            ws = self._spaces[stream] = torch.empty(nbytes + nbytes // 4, dtype=torch.uint8, device=self.cache._device)
+        return ws
 
     def set(self, num_queries: int, spans, blocks):
         L, h = self.cache._lib, self._open()
@@ -222,6 +233,7 @@ class AttentionPlan:
         if getattr(self, "_h", None):
             self.cache._lib.ps_kv_plan_destroy(self._h)
             self._h = None
+            self._spaces = {}
 
     def __del__(self):
         try:
