@@ -46,6 +46,12 @@ struct ps_kv_plan {
   uint32_t queries = 0;
   uint64_t part_rows = 0;
   uint32_t top_block = 0;
+
+  // rows of the tile kernel's tiles for a span of so many rows
+  uint32_t tile_rows(uint32_t rows) const {
+    const uint32_t full = (uint32_t)pskv::tile_rows_of((int)kv->D);
+    return rows <= full / 2 ? full / 2 : full;
+  }
 };
 
 namespace {
@@ -129,9 +135,27 @@ using pskv::kBlock;
 using pskv::kSmallRows;
 using pskv::kTileKeys;
 
-// Where the tile kernel takes a span: from this many rows and keys on.
-constexpr uint32_t kTileLeastRows = 33;
-constexpr int64_t kTileLeastKeys = 256;
+// Which kernel takes the rows of a tile and head over the keys that all of them see: the one that adds less time to
+// the batch.  Nanoseconds of the whole GPU, from spans of 24 to 256 rows on 512 to 65536 keys: the row kernel per 16
+// rows and 16 keys, the tile kernel per step of 128 keys, a piece of it costing three steps more; the tile kernel
+// adds kTileLaunch to a call.  In front of a causal span's end, of which the row kernel has a short piece per 16 rows
+// anyway, its blocks cost about four times as much, as its pieces then are of uneven lengths (192 new tokens on 16384:
+// 457 us, 500 without this).  By tiles / by rows, us, one span of 8 key/value heads: bf16 with head_dim 128,
+// 128 rows on 512 keys 10.9/11.2, on 4096 16.7/19.0, 64 rows on 2048 12.0/10.3, on 16384 22.7/24.7, 32 rows on 16384
+// 22.4/18.8; fp8, 64 rows on 4096 15.5/16.3; bf16 with head_dim 64, 64 rows on 4096 9.1/10.3.
+constexpr double kTileLaunch = 1000.0;
+double tile_saves(const ps_kv& kv, uint32_t rows, int64_t keys, bool causal) {
+  const bool fp8 = kv.fmt == PS_KV_FP8;
+  const double block = (kv.D == 128 ? (fp8 ? 0.73 : 0.51) : (fp8 ? 0.50 : 0.40)) * (causal && rows > (uint32_t)kSmallRows ? 4 : 1);
+  const double step = kv.D == 128 ? (fp8 ? 18.0 : 16.0) : (fp8 ? 9.0 : 8.0);
+  const double by_rows = block * ((rows + kSmallRows - 1) / kSmallRows) * (double)((keys + kBlock - 1) / kBlock);
+  return by_rows - step * (double)((keys + kTileKeys - 1) / kTileKeys + 3);
+}
+
+// From so many steps on, a piece of one tile of rows runs as two.  64 rows on 65536 tokens: 65 us, 79 as one; on
+// 1024 (2 steps a piece), where the second result costs more than it brings, 11.4 and 11.0.  With head_dim 64,
+// whose steps are half as long, it brought nothing (35 and 34 us).
+constexpr uint32_t kSplitSteps = 8;
 
 // A piece of the row kernel joins up to this many tile parts into its rows, where a worker has at least so many
 // units of rows that the time this takes evens out.  192 new tokens on 16384 (4 units a worker, 2 to 3 parts):
@@ -231,6 +255,26 @@ void share_out(const std::vector<Unit>& units, uint32_t most, uint32_t extra, ui
 void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t n_spans, Layout* out) {
   Layout& o = *out;
   const uint32_t H = pl.kv->heads, g = pl.group;
+  // The keys that all rows of a tile see, where the tile kernel is the one to take them (else 0).
+  auto cut_of = [&](const ps_kv_span& s, uint32_t r0, uint32_t nr) -> int64_t {
+    int64_t c = (int64_t)s.length;
+    if (s.causal) c = std::max<int64_t>(0, c - (int64_t)s.num_queries + r0 / g + 1) / kBlock * kBlock;
+    return tile_saves(*pl.kv, nr, c, s.causal != 0) > 0 ? c : 0;
+  };
+  auto tiles_save = [&](const ps_kv_span& s) {
+    double sum = 0;
+    const uint32_t rows = s.num_queries * g, tr = pl.tile_rows(rows);
+    for (uint32_t r0 = 0; r0 < rows; r0 += tr) {
+      const uint32_t nr = std::min(rows - r0, tr);
+      const int64_t c = cut_of(s, r0, nr);
+      if (c > 0) sum += tile_saves(*pl.kv, nr, c, s.causal != 0) * H;
+    }
+    return sum;
+  };
+  double saved = 0;
+  for (uint32_t si = 0; si < n_spans; ++si) saved += tiles_save(spans[si]);
+  auto tiles_for = [&](const ps_kv_span& s) { return saved > kTileLaunch && tiles_save(s) > 0; };
+
   for (uint32_t si = 0; si < n_spans; ++si) {
     const ps_kv_span& s = spans[si];
     if (s.num_queries == 0 || s.length == 0) continue;
@@ -240,23 +284,19 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
 
     // Tiles take the keys that all their rows see; cut[t]: how many those are for tile t.
     std::vector<int64_t> cut;
-    const uint32_t full = (uint32_t)pskv::tile_rows_of((int)pl.kv->D), tile_rows = rows <= full / 2 ? full / 2 : full;
-    if (rows >= kTileLeastRows && len >= kTileLeastKeys) {
-      const uint32_t tiles = (rows + tile_rows - 1) / tile_rows;
+    const uint32_t tile_rows = pl.tile_rows(rows);
+    if (tiles_for(s)) {
       o.layers.push_back(Layer{s.first_query, s.num_queries, tile_rows, (uint32_t)o.groups.size()});
-      for (uint32_t t = 0; t < tiles; ++t) {
-        const uint32_t r0 = t * tile_rows, nr = std::min(rows - r0, tile_rows);
-        int64_t c = len;
-        if (s.causal) c = std::max<int64_t>(0, (int64_t)climit + r0 / g + 1) / kBlock * kBlock;
-        if (c < kTileLeastKeys) c = 0;
+      for (uint32_t r0 = 0; r0 < rows; r0 += tile_rows) {
+        const uint32_t nr = std::min(rows - r0, tile_rows);
+        const int64_t c = cut_of(s, r0, nr);
         cut.push_back(c);
         for (uint32_t h = 0; h < H; ++h) {
-          if (c > 0)
-            o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, o));
+          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, pskv::kNoLimit, tile_rows, o));
           o.groups.push_back(Group{0, 0});
         }
       }
-      if (!s.causal) continue;
+      if (*std::min_element(cut.begin(), cut.end()) == len) continue;  // not causal, and all of it to tiles
     }
     o.layers.push_back(Layer{s.first_query, s.num_queries, (uint32_t)kSmallRows, (uint32_t)o.groups.size()});
     for (uint32_t r0 = 0; r0 < rows; r0 += kSmallRows) {
@@ -342,20 +382,27 @@ void lay_out(const ps_kv_plan& pl, uint32_t T, const ps_kv_span* spans, uint32_t
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
       const Piece& p = units[i].p;
-      bool direct = b - a == 1;
+      // a tile piece that is split by steps has two parts
+      uint32_t nparts = 0;
+      for (uint32_t k = a; k < b; ++k) {
+        if (!rows && pl.kv->D == 128 && p.nrows <= pskv::tile_rows_of(128) / 2 && pieces[k].nblocks >= kSplitSteps)
+          pieces[k].split = units[i].tile_rows;
+        nparts += pieces[k].split ? 2 : 1;
+      }
+      bool direct = nparts == 1;
       for (uint32_t q = p.row0 / g; direct && q <= (p.row0 + p.nrows - 1) / g; ++q) direct = alone[p.query0 + q];
-      if (!direct && rows && may_fold && b - a == 1) direct = fold(units[i], &pieces[a]);
+      if (!direct && rows && may_fold && nparts == 1) direct = fold(units[i], &pieces[a]);
       Group& gr = o.groups[units[i].group];
       if (direct) {
         gr = Group{pskv::kDirect, 1};
         pieces[a].part_row = pskv::kDirect;
         continue;
       }
-      gr = Group{(uint32_t)o.part_rows, b - a};
-      o.max_parts = std::max(o.max_parts, b - a);
+      gr = Group{(uint32_t)o.part_rows, nparts};
+      o.max_parts = std::max(o.max_parts, nparts);
       for (uint32_t k = a; k < b; ++k) {
         pieces[k].part_row = (uint32_t)o.part_rows;
-        o.part_rows += units[i].tile_rows;
+        o.part_rows += units[i].tile_rows * (pieces[k].split ? 2 : 1);
       }
     }
   };

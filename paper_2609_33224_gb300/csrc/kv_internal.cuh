@@ -65,7 +65,7 @@ struct alignas(16) Piece {
   uint16_t nrows;
   uint16_t head;
   uint32_t fold0, nfold;  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in
-  uint32_t pad;
+  uint32_t split;  // tile kernel: not 0: its even steps in tile 0, its odd ones in tile 1, so many rows behind
 };
 static_assert(sizeof(Piece) == 48, "Piece layout");
 constexpr uint32_t kDirect = 0xFFFFFFFFu;

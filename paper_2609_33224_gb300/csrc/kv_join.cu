@@ -127,8 +127,8 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
 template <int D, bool FP16>
 cudaError_t go(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
   const uint32_t rows = p.njoin * a.group;
-  // Few rows of many parts (one request on all SMs): a CTA a row.
-  if (p.max_parts > 16)
+  // A CTA a row where there are few: 64 rows of 64 parts 7 us less than a warp a row; 2048 rows of 38 parts 3 us more.
+  if (p.max_parts > 4 && rows <= 1024)
     return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, true, s, a, p);
   return launch(join_kernel<D, FP16, false>, (rows + 7) / 8, 256, 0, 1, true, s, a, p);
 }

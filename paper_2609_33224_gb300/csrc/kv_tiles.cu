@@ -308,8 +308,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     bool alive = true;
     for (uint32_t pi = first; alive && pi < last; ++pi) {
       const Piece pc = p.tile_pieces[pi];
-      if (t * C::kRows >= pc.nrows) continue;
-      const uint32_t in_tile = t * C::kRows + rank * 128 + r;
+      if (!pc.split && t * C::kRows >= pc.nrows) continue;
+      const uint32_t in_tile = (pc.split ? 0 : t * C::kRows) + rank * 128 + r;
       const uint32_t row = pc.row0 + in_tile;
       const bool valid = in_tile < pc.nrows;
       const uint32_t query = pc.query0 + row / a.group, head = pc.head * a.group + row % a.group;
@@ -344,7 +344,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       if (lane == 0) arrive_first<C::kCtas>(smem_u32(&bars.q_ready[t]));
 
       float m = -INFINITY, l = 0.0f;
-      for (uint32_t j = 0; j < pc.nblocks; ++j) {
+      const uint32_t j0 = pc.split ? t : 0, dj = pc.split ? 2 : 1;
+      for (uint32_t j = j0; j < pc.nblocks; j += dj) {
         if (!mbar_wait_warp(smem_u32(&bars.s_full[t]), steps & 1)) {
           alive = false;
           break;
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           const float n = fmaxf(m, x), f = n == m ? 1.0f : ex2(m - n);
           m = n;
           l *= f;
-          if (j > 0) {  // the product before this step's scores is done: it was issued, and so finished, first
+          if (j > j0) {  // the product before this step's scores is done: it was issued, and so finished, first
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
               uint32_t o[16];
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       tc_fence_after();
       const bool direct = pc.part_row == kDirect;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      const uint64_t at = (uint64_t)pc.part_row + in_tile;
+      const uint64_t at = (uint64_t)pc.part_row + t * (pc.split ? pc.split : C::kRows) + rank * 128 + r;
       // The queries are used up: their rows' shared memory takes the warp's 32 rows, half of their columns at a
       // time, from which whole rows are stored by neighbouring lanes.
       const uint32_t stage = q_smem + t * C::kQ + (warp % 4) * (32 * D * 2);
@@ -585,41 +586,50 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         const uint32_t n0 = n;
         auto slot = [&](uint32_t i) { return (n0 + i) % C::kSlots; };
         auto here = [&](uint32_t i) { return wait(full(slot(i)), ((n0 + i) / C::kSlots) & 1u); };
-        here(0);
-        for (uint32_t t = 0; t < tiles; ++t) {
-          if (!wait(smem_u32(&bars.q_ready[t]), q_seen[t] & 1)) break;
+        // A step's values and its rows' next scores, by tile t; `ahead` steps lie between them.
+        auto turn = [&](uint32_t t, uint32_t j, uint32_t ahead) {
+          if (!wait(smem_u32(&bars.p_ready[t][0]), p_seen[t] & 1)) return false;
+          tc_fence_after();
+          values(t, slot(2 * j + 1), 0, j >= ahead);
+          if (!wait(smem_u32(&bars.p_ready[t][1]), p_seen[t] & 1)) return false;
+          ++p_seen[t];
+          tc_fence_after();
+          values(t, slot(2 * j + 1), 1, true);
+          if (j + ahead < steps) {
+            if (!here(2 * (j + ahead))) return false;
+            scores(t, slot(2 * (j + ahead)));
+            tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
+          } else {
+            tc_commit<C::kCtas>(smem_u32(&bars.o_done[t]));
+          }
+          return true;
+        };
+        // One tile of rows alone would leave the tensor cores idle during its softmax: its even and odd steps run as
+        // two tiles, each with a result of its own.
+        const uint32_t ahead = pp->split ? 2 : 1;
+        for (uint32_t t = 0; t < (pp->split ? 2 : tiles); ++t) {
+          if (!here(pp->split ? 2 * t : 0) || !wait(smem_u32(&bars.q_ready[t]), q_seen[t] & 1)) break;
           ++q_seen[t];
           tc_fence_after();
-          scores(t, slot(0));
+          scores(t, slot(pp->split ? 2 * t : 0));
           tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
+          if (pp->split || t == tiles - 1) tc_commit<C::kCtas>(empty(slot(pp->split ? 2 * t : 0)));
         }
-        if (alive) tc_commit<C::kCtas>(empty(slot(0)));
         for (uint32_t j = 0; alive && j < steps; ++j) {
-          const bool more = j + 1 < steps;
           if (!here(2 * j + 1)) break;
           if (!C::kFp8 && keys - j * kTileKeys < (uint32_t)kTileKeys) {
             mbar_arrive(smem_u32(&bars.tail_here));
             if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
           }
-          for (uint32_t t = 0; t < tiles; ++t) {
-            if (!wait(smem_u32(&bars.p_ready[t][0]), p_seen[t] & 1)) break;
-            tc_fence_after();
-            values(t, slot(2 * j + 1), 0, j > 0);
-            if (!wait(smem_u32(&bars.p_ready[t][1]), p_seen[t] & 1)) break;
-            ++p_seen[t];
-            tc_fence_after();
-            values(t, slot(2 * j + 1), 1, true);
-            if (more) {
-              if (t == 0 && !here(2 * j + 2)) break;
-              scores(t, slot(2 * j + 2));
-              tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
-            } else {
-              tc_commit<C::kCtas>(smem_u32(&bars.o_done[t]));
-            }
+          if (pp->split) {
+            if (!turn(j & 1, j, 2)) break;
+          } else {
+            for (uint32_t t = 0; t < tiles; ++t)
+              if (!turn(t, j, 1)) break;
           }
           if (alive) {
             tc_commit<C::kCtas>(empty(slot(2 * j + 1)));
-            if (more) tc_commit<C::kCtas>(empty(slot(2 * j + 2)));
+            if (j + ahead < steps) tc_commit<C::kCtas>(empty(slot(2 * (j + ahead))));
           }
         }
         n = n0 + 2 * steps;
