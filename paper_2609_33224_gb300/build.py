@@ -45,7 +45,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     headers = [os.path.join(CSRC, "ps_internal.cuh"), os.path.join(CSRC, "calibrate.h"),
                os.path.join(CSRC, "greedy_grid.h"),
                os.path.join(ROOT, "include", "packserve.h")]
-    kv_headers = [os.path.join(CSRC, "kv_internal.cuh"), os.path.join(ROOT, "include", "packserve_kv.h"), headers[-1]]
+    kv_headers = [os.path.join(CSRC, "kv_internal.cuh"), os.path.join(CSRC, "kv_plan.h"),
+                  os.path.join(ROOT, "include", "packserve_kv.h"), headers[-1]]
     jobs = []
     for src in SOURCES:
         s = os.path.join(CSRC, src)

@@ -17,17 +17,11 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "kv_plan.h"
 #include "packserve_kv.h"
 
 namespace pskv {
 
-constexpr int kBlock = PS_BLOCK_TOKENS;
-constexpr int kSmallRows = 16;   // rows of a tile of the row kernel (one m16 of mma.sync)
-// Rows of a tile of the tile kernel, two accumulators of 128 rows a CTA: with head_dim 128 a pair of CTAs
-// shares the keys and values.
-__host__ __device__ constexpr int tile_ctas_of(int D) { return D == 128 ? 2 : 1; }
-__host__ __device__ constexpr int tile_rows_of(int D) { return 256 * tile_ctas_of(D); }
-constexpr int kTileKeys = 128;   // keys of one step of the tile kernel
 constexpr int kExpBias = 127;
 constexpr int kExpMin = -110, kExpMax = 119, kExpNan = 255;
 
@@ -50,43 +44,6 @@ __device__ __forceinline__ uint32_t offset8k(uint32_t t, uint32_t c) {
 __device__ __forceinline__ uint32_t offset8v(uint32_t t, uint32_t c) {
   return (c >> 2) * (kBlock * 64) + t * 64 + (((c & 3u) ^ ((t >> 1) & 3u)) << 4);
 }
-
-// A piece of work of either attention kernel: a run of key blocks for the rows of one tile and one
-// key/value head.  A span's rows are its queries' heads of the group, row r = (r / g)-th query, head r % g.
-struct alignas(16) Piece {
-  uint32_t block;     // where the piece's block ids start
-  uint32_t nblocks;   // blocks (row kernel) or key tiles of 8 blocks (tile kernel; the last may be partial)
-  uint32_t key0;      // index in the span of the first key
-  uint32_t end;       // keys end before this index
-  int32_t climit;     // the span's i-th query sees keys j <= climit + i
-  uint32_t query0;    // the span's first query
-  uint32_t row0;      // the tile's first row
-  uint32_t part_row;  // first row of the partial result, or kDirect: the output is written
-  uint16_t nrows;
-  uint16_t head;
-  uint32_t fold0, nfold;  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in
-  uint32_t split;  // tile kernel: not 0: its even steps in tile 0, its odd ones in tile 1, so many rows behind
-};
-static_assert(sizeof(Piece) == 48, "Piece layout");
-constexpr uint32_t kDirect = 0xFFFFFFFFu;
-constexpr int32_t kNoLimit = 0x3FFFFFFF;
-
-// What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments segs[seg0] ..:
-// the i-th row's are the partial rows row + i + k * stride, k < nparts.
-struct JoinEntry {
-  uint32_t query;
-  uint16_t head0, count;
-  uint32_t seg0, nsegs;
-};
-struct JoinSeg {
-  uint32_t row, stride, nparts;
-};
-// The same for the rows first .. first + count - 1 of a piece.
-struct Fold {
-  uint32_t seg0;
-  uint16_t nsegs;
-  uint8_t first, count;
-};
 
 struct PlanDev {
   const Piece* row_pieces;
@@ -136,11 +93,6 @@ cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, c
 cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
 cudaError_t prepare_tiles(int D, int fmt);
-// Workers (warps) of a CTA of the row kernel.  fp8 blocks take as many instructions as 16-bit ones of twice the
-// bytes: 12 warps hide more of their latency (131072 tokens of 5 requests: 182 us, 187 with 8); 16-bit ones are
-// bound by bytes with 8 (64 requests on a prefix: 58 us, 59 with 12, whose shares are shorter).
-__host__ __device__ constexpr int row_warps_of(int fmt) { return fmt == PS_KV_FP8 ? 12 : 8; }
-
 // ---- PTX ----------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {

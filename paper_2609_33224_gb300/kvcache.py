@@ -240,3 +240,60 @@ class AttentionPlan:
             self.close()
         except Exception:
             pass
+
+
+def shared_spans(tables, lengths, new_tokens, min_blocks: int = 4):
+    """The spans of a batch whose requests hold block tables with common beginnings.
+
+    ``tables[i]``: the block ids of request i's tokens, in order; ``lengths[i]``: its tokens, the last
+    ``new_tokens[i]`` of which (at least one) are its queries.  Blocks that hold no query's token and that several
+    requests have in common from the start become one span for all of them, level by level as the tables part;
+    runs of fewer than ``min_blocks`` common blocks stay with their requests.  Returns ``(order, spans, blocks)``:
+    the batch has request ``order[0]``'s queries first, then ``order[1]``'s, and so on; ``spans`` and ``blocks`` are
+    what ``AttentionPlan.set`` takes.
+    """
+    tabs = [np.ascontiguousarray(t, dtype=np.uint32) for t in tables]
+    lengths, new = [int(x) for x in lengths], [int(x) for x in new_tokens]
+    if not len(tabs) == len(lengths) == len(new):
+        raise ValueError("one table, length and number of new tokens per request")
+    for t, n, q in zip(tabs, lengths, new):
+        if t.ndim != 1 or not 1 <= q <= n or n > BLOCK_TOKENS * t.size:
+            raise ValueError("a request needs 1 <= new tokens <= length <= its blocks' tokens")
+    full = [(n - q) // BLOCK_TOKENS for n, q in zip(lengths, new)]  # blocks without a query's token
+    order = sorted(range(len(tabs)), key=lambda i: tabs[i][:full[i]].astype(">u4").tobytes())
+    first = np.concatenate([[0], np.cumsum([new[i] for i in order])]).astype(np.int64) if order else np.zeros(1, np.int64)
+    spans, blocks, at = [], [], 0
+
+    def add(lo, hi, ids, length, causal):
+        nonlocal at
+        spans.append((first[lo], first[hi] - first[lo], length, causal, at))
+        blocks.append(ids)
+        at += ids.size
+
+    def common(lo, hi):  # of a sorted run: what its ends have in common
+        a, b = (tabs[order[x]][:full[order[x]]] for x in (lo, hi - 1))
+        n = min(a.size, b.size)
+        diff = np.flatnonzero(a[:n] != b[:n])
+        return int(diff[0]) if diff.size else n
+
+    todo = [(0, len(order), 0)] if order else []
+    while todo:
+        lo, hi, depth = todo.pop()
+        if hi - lo == 1:
+            i = order[lo]
+            add(lo, hi, tabs[i][depth:-(-lengths[i] // BLOCK_TOKENS)], lengths[i] - depth * BLOCK_TOKENS, 1)
+            continue
+        n = common(lo, hi)
+        if n - depth >= min_blocks:
+            add(lo, hi, tabs[order[lo]][depth:n], (n - depth) * BLOCK_TOKENS, 0)
+            depth = n
+        # runs that go on together; a request whose table ends here goes on alone
+        start = lo
+        for x in range(lo + 1, hi + 1):
+            i, j = order[start], order[x] if x < hi else -1
+            if x < hi and full[i] > n and full[j] > n and tabs[i][n] == tabs[j][n]:
+                continue
+            todo.append((start, x, depth))
+            start = x
+    return (np.array(order, np.int64), np.array(spans, SPAN_DTYPE) if spans else np.zeros(0, SPAN_DTYPE),
+            np.concatenate(blocks).astype(np.uint32) if blocks else np.zeros(0, np.uint32))

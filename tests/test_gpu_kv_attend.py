@@ -283,3 +283,32 @@ def test_refusals(kv):
         c.check()
     with pytest.raises(ValueError, match="closed"):
         c.attend(q, p)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(kv, seed):
+    """Random spans, formats, groups and head sizes: rows and tiles, joins of every kind."""
+    import random
+    rng = random.Random(seed)
+    D, fmt = rng.choice([64, 128]), rng.choice(["bf16", "fp16", "fp8"])
+    Hkv, g = rng.choice([1, 2, 3]), rng.choice([1, 2, 4, 5, 8, 16])
+    T = rng.choice([3, 40, 130])
+    spans = [(0, T, rng.choice([0, 37, 1200, 5000]), 0)]
+    first = 0
+    while first < T:
+        n = min(T - first, rng.choice([1, 1, 7, 70]))
+        if rng.random() < 0.9:
+            spans.append((first, n, rng.choice([0, n, n + 15, n + 300, 900, max(1, n - 2)]), 1))
+        if n > 1 and rng.random() < 0.3:
+            spans.append((first, n, rng.randrange(1, 700), 0))
+        first += n
+    b = Batch(kv, fmt, Hkv, g, D, spans, T, seed=100 + seed)
+    b.check(*b.run())
+
+
+@pytest.mark.parametrize("fmt,D", [("bf16", 128), ("fp8", 128), ("fp16", 64), ("fp8", 64)])
+def test_one_tile_over_many_keys(kv, fmt, D):
+    """A few queries on a long prefix: one tile of rows, its steps cut over many workers and by parity."""
+    T = 40
+    b = Batch(kv, fmt, 2, 4, D, [(0, T, 40003, 0)] + [(i, 1, 5, 1) for i in range(T)], T, seed=7)
+    b.check(*b.run())
