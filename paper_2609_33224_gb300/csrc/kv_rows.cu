@@ -68,6 +68,8 @@ __device__ __forceinline__ void sts128_zero(uint32_t addr) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(addr), "r"(0) : "memory");
 }
 
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+
 // Whether one of the two 16-bit floats in w is an infinity or a NaN.
 template <bool FP16>
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
@@ -114,6 +116,14 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
       ahead_n = q->nblocks;
       ahead_block = q->block;
       ahead_head = q->head;
+      // the piece's queries, and what it has to join in, are wanted when its turn comes
+      const uint32_t row = q->row0 + lane / 2;
+      if (lane / 2 < q->nrows) {
+        const uint16_t* src = a.q + (int64_t)(q->query0 + row / a.group) * a.q_tok +
+                              (int64_t)(ahead_head * a.group + row % a.group) * a.q_head + (lane & 1u) * (D / 2);
+        prefetch(src);
+      }
+      if (q->nfold && lane == 0) prefetch(p.folds + q->fold0);
     }
     if ((ahead_i & 31u) == 0) ids = p.blocks[ahead_block + min(ahead_i + lane, ahead_n - 1)];
     const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, ahead_i & 31u);
