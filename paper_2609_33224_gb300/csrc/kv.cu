@@ -209,7 +209,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.row_pieces = reinterpret_cast<const pskv::Piece*>(b.dev + rp);
   d.row_off = reinterpret_cast<const uint32_t*>(b.dev + ro);
   d.row_workers = o.row_off.empty() ? 0 : (uint32_t)o.row_off.size() - 1;
-  d.row_ctas = std::min<uint32_t>(d.row_workers, (uint32_t)kv->sms);
+  d.row_ctas = std::min<uint32_t>(d.row_workers, (uint32_t)o.row_sms);
   d.tile_pieces = reinterpret_cast<const pskv::Piece*>(b.dev + tp);
   d.tile_off = reinterpret_cast<const uint32_t*>(b.dev + to);
   d.tile_workers = o.tile_off.empty() ? 0 : (uint32_t)o.tile_off.size() - 1;

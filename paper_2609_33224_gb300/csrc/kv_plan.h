@@ -88,19 +88,45 @@ struct PlanShape {
 // 128 rows on 512 keys 10.9/11.2, on 4096 16.7/19.0, 64 rows on 2048 12.0/10.3, on 16384 22.7/24.7, 32 rows on 16384
 // 22.4/18.8; fp8, 64 rows on 4096 15.5/16.3; bf16 with head_dim 64, 64 rows on 4096 9.1/10.3.
 constexpr double kTileLaunch = 1000.0;
-inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool causal) {
+inline double block_ns(const PlanShape& kv) {
   const bool fp8 = kv.fmt == PS_KV_FP8;
+  return kv.D == 128 ? (fp8 ? 0.73 : 0.51) : (fp8 ? 0.50 : 0.40);
+}
+inline double step_ns(const PlanShape& kv) {
+  const bool fp8 = kv.fmt == PS_KV_FP8;
+  return kv.D == 128 ? (fp8 ? 18.0 : 16.0) : (fp8 ? 9.0 : 8.0);
+}
+constexpr int kPieceSteps = 3;
+inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool causal) {
   const double dear = causal && rows > (uint32_t)kSmallRows ? 4 : 1;
-  const double block = dear * (kv.D == 128 ? (fp8 ? 0.73 : 0.51) : (fp8 ? 0.50 : 0.40));
-  const double step = kv.D == 128 ? (fp8 ? 18.0 : 16.0) : (fp8 ? 9.0 : 8.0);
-  const double by_rows = block * ((rows + kSmallRows - 1) / kSmallRows) * (double)((keys + kBlock - 1) / kBlock);
-  return by_rows - step * (double)((keys + kTileKeys - 1) / kTileKeys + 3);
+  const double by_rows = dear * block_ns(kv) * ((rows + kSmallRows - 1) / kSmallRows) * (double)((keys + kBlock - 1) / kBlock);
+  return by_rows - step_ns(kv) * (double)((keys + kTileKeys - 1) / kTileKeys + kPieceSteps);
 }
 
 // From so many steps on, a piece of one tile of rows runs as two.  64 rows on 65536 tokens: 65 us, 79 as one; on
 // 1024 (2 steps a piece), where the second result costs more than it brings, 11.4 and 11.0.  With head_dim 64,
 // whose steps are half as long, it brought nothing (35 and 34 us).
 constexpr uint32_t kSplitSteps = 8;
+
+// The row kernel is bound by the cache's bytes, which a part of the SMs can draw, the tile kernel by its SMs: side by
+// side they take less time than one after the other.  Returns how many SMs the row kernel gets (all: one after the
+// other), by the times above, the bytes at 6.2 TB/s and 6 us that the tile kernel takes whatever its SMs.
+constexpr double kBytesPerNs = 6200.0, kTileFixed = 6000.0;
+inline int row_sms(const PlanShape& kv, double steps, double blocks) {
+  const double tile = step_ns(kv) * steps, work = block_ns(kv) * blocks;
+  const double bytes = blocks * (kv.fmt == PS_KV_FP8 ? 2 * kBlock * (kv.D + 1.0) : 4.0 * kBlock * kv.D) / kBytesPerNs;
+  double best = kTileFixed + tile + std::max(work, bytes);
+  int sms = kv.sms;
+  for (int x = 2; x < kv.sms; x += 2) {
+    const double f = (double)x / kv.sms;
+    const double t = std::max(kTileFixed + tile / (1 - f), std::max(work / f, bytes));
+    if (t < 0.97 * best || (sms < kv.sms && t < best)) {
+      best = t;
+      sms = x;
+    }
+  }
+  return sms;
+}
 
 // A piece of the row kernel joins up to this many tile parts into its rows, where a worker has at least so many
 // units of rows that the time this takes evens out.  192 new tokens on 16384 (4 units a worker, 2 to 3 parts):
@@ -136,6 +162,7 @@ struct Layout {
   std::vector<Fold> folds;
   uint64_t part_rows = 0;
   uint32_t max_parts = 1;
+  int row_sms = 0;  // SMs of the row kernel; fewer than all: beside the tile kernel
 };
 
 // A unit of the layer and group that come last.
@@ -320,8 +347,16 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     p->nfold = (uint32_t)(o.folds.size() - folds);
     return true;
   };
-  const uint32_t row_workers = (uint32_t)(pl.sms * row_warps_of(pl.fmt));
-  const bool may_fold = o.row_units.size() >= kFoldUnits * row_workers;
+  const bool may_fold = o.row_units.size() >= kFoldUnits * (size_t)(pl.sms * row_warps_of(pl.fmt));
+  o.row_sms = pl.sms;
+  if (!o.tile_units.empty() && !o.row_units.empty() && !may_fold) {
+    double steps = 0, blocks = 0;
+    for (const Unit& u : o.tile_units) steps += u.p.nblocks + kPieceSteps;
+    for (const Unit& u : o.row_units) blocks += u.p.nblocks;
+    o.row_sms = row_sms(pl, steps, blocks);
+  }
+  const int tile_sms = o.row_sms < pl.sms ? pl.sms - o.row_sms : pl.sms;
+  const uint32_t row_workers = (uint32_t)(o.row_sms * row_warps_of(pl.fmt));
   auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
@@ -352,7 +387,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   };
   std::vector<uint32_t> first;
   if (!o.tile_units.empty()) {
-    const uint32_t workers = (uint32_t)std::max(1, pl.sms / tile_ctas_of((int)pl.D));
+    const uint32_t workers = (uint32_t)std::max(1, tile_sms / tile_ctas_of((int)pl.D));
     share_out(o.tile_units, workers, 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
     finish(o.tile_units, o.tile_pieces, first, false);
   }
