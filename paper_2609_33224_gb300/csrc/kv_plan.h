@@ -90,11 +90,11 @@ struct PlanShape {
 constexpr double kTileLaunch = 1000.0;
 inline double block_ns(const PlanShape& kv) {
   const bool fp8 = kv.fmt == PS_KV_FP8;
-  return kv.D == 128 ? (fp8 ? 0.73 : 0.51) : (fp8 ? 0.50 : 0.40);
+  return kv.D == 128 ? (fp8 ? 0.67 : 0.51) : (fp8 ? 0.50 : 0.40);
 }
 inline double step_ns(const PlanShape& kv) {
   const bool fp8 = kv.fmt == PS_KV_FP8;
-  return kv.D == 128 ? (fp8 ? 18.0 : 16.0) : (fp8 ? 9.0 : 8.0);
+  return kv.D == 128 ? (fp8 ? 20.5 : 17.5) : (fp8 ? 9.0 : 8.0);
 }
 constexpr int kPieceSteps = 3;
 inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool causal) {
@@ -110,17 +110,19 @@ constexpr uint32_t kSplitSteps = 8;
 
 // The row kernel is bound by the cache's bytes, which a part of the SMs can draw, the tile kernel by its SMs: side by
 // side they take less time than one after the other.  Returns how many SMs the row kernel gets (all: one after the
-// other), by the times above, the bytes at 6.2 TB/s and 6 us that the tile kernel takes whatever its SMs.
-constexpr double kBytesPerNs = 6200.0, kTileFixed = 6000.0;
-inline int row_sms(const PlanShape& kv, double steps, double blocks) {
-  const double tile = step_ns(kv) * steps, work = block_ns(kv) * blocks;
+// other), by the times above, 3.3 ns of the GPU for a unit's start and end, the bytes at 6.2 TB/s, and what the
+// kernels take whatever their SMs: 6 and 4 us.  64 queries on 8192 shared tokens 55.7 -> 41.8 us, 9 groups under one
+// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 272 -> 260.
+constexpr double kUnitNs = 3.3, kBytesPerNs = 6200.0, kTileFixed = 6000.0, kRowFixed = 4000.0;
+inline int row_sms(const PlanShape& kv, double steps, double blocks, double units) {
+  const double tile = step_ns(kv) * steps, work = block_ns(kv) * blocks + kUnitNs * units;
   const double bytes = blocks * (kv.fmt == PS_KV_FP8 ? 2 * kBlock * (kv.D + 1.0) : 4.0 * kBlock * kv.D) / kBytesPerNs;
-  double best = kTileFixed + tile + std::max(work, bytes);
+  double best = kTileFixed + tile + kRowFixed + std::max(work, bytes);
   int sms = kv.sms;
   for (int x = 2; x < kv.sms; x += 2) {
     const double f = (double)x / kv.sms;
-    const double t = std::max(kTileFixed + tile / (1 - f), std::max(work / f, bytes));
-    if (t < 0.97 * best || (sms < kv.sms && t < best)) {
+    const double t = std::max(kTileFixed + tile / (1 - f), kRowFixed + std::max(work / f, bytes));
+    if (t < 0.995 * best || (sms < kv.sms && t < best)) {
       best = t;
       sms = x;
     }
@@ -353,7 +355,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     double steps = 0, blocks = 0;
     for (const Unit& u : o.tile_units) steps += u.p.nblocks + kPieceSteps;
     for (const Unit& u : o.row_units) blocks += u.p.nblocks;
-    o.row_sms = row_sms(pl, steps, blocks);
+    o.row_sms = row_sms(pl, steps, blocks, (double)o.row_units.size());
   }
   const int tile_sms = o.row_sms < pl.sms ? pl.sms - o.row_sms : pl.sms;
   const uint32_t row_workers = (uint32_t)(o.row_sms * row_warps_of(pl.fmt));
