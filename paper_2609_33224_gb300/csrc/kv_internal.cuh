@@ -9,7 +9,8 @@
 //     of panels land ready for use, and ldmatrix reads them without bank conflicts.
 //   fp8: K codes (16 rows of D bytes, chunk c of row r at c ^ swz(r)), V codes (D / 64 panels of 16 rows x
 //     64 bytes, chunks swizzled too), then the 16 scale exponents of K and the 16 of V (biased by 127; 255:
-//     the row holds a NaN), which fill one 32-byte sector: one copy brings a record with its scales.
+//     the row holds a NaN, and its codes are 0), which fill one 32-byte sector: one copy brings a record with
+//     its scales.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -44,6 +45,8 @@ __device__ __forceinline__ uint32_t offset8k(uint32_t t, uint32_t c) {
 __device__ __forceinline__ uint32_t offset8v(uint32_t t, uint32_t c) {
   return (c >> 2) * (kBlock * 64) + t * 64 + (((c & 3u) ^ ((t >> 1) & 3u)) << 4);
 }
+// where token t's exponent lies among the 16: the four that a lane of an m16n8 result needs next to each other
+__device__ __forceinline__ uint32_t exp_place(uint32_t t) { return ((t & 7u) >> 1) * 4 + (t >> 3) * 2 + (t & 1u); }
 
 struct PlanDev {
   const Piece* row_pieces;

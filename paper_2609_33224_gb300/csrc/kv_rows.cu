@@ -20,9 +20,14 @@ namespace {
 // the memory then only answers later.
 constexpr int kRingBytes = 16640;
 
+// A stage starts on a multiple of 128 bytes, so that a swizzled address is an exclusive or with a constant.
+template <int D, int FMT>
+constexpr int stage_bytes() {
+  return (record_bytes(D, FMT) + 127) / 128 * 128;
+}
 template <int D, int FMT>
 constexpr int ring_stages() {
-  return kRingBytes / record_bytes(D, FMT);
+  return kRingBytes / stage_bytes<D, FMT>();
 }
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -54,10 +59,16 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
                  : "r"(addr)
                  : "memory");
 }
-__device__ __forceinline__ uint32_t lds16(uint32_t addr) {
-  uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
+}
+// Byte i of w as the exponent field of a float: a row's scale, or, for the mark of a row with a NaN, an infinity, whose
+// product with such a row's codes, zeros, is the NaN that is wanted.
+template <int I>
+__device__ __forceinline__ float exp_byte(uint32_t w) {
+  return __uint_as_float((I == 3 ? w >> 1 : w << (23 - 8 * I)) & 0x7F800000u);
 }
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   uint4 v;
@@ -98,7 +109,8 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
     wait_for_last();
     return;
   }
-  const uint32_t ring = smem_u32(smem) + warp * kStages * kRec;
+  constexpr int kStage = stage_bytes<D, FMT>();
+  const uint32_t ring = smem_u32(smem) + warp * kStages * kStage;
   const uint32_t bar = smem_u32(bars) + warp * kStages * 8;
   if (lane < kStages) mbar_init(bar + lane * 8, 1);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -129,7 +141,7 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
     const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, ahead_i & 31u);
     if (lane == 0) {
       mbar_expect(bar + ahead_st * 8, kRec);
-      bulk_load(ring + ahead_st * kRec, a.pool + ((uint64_t)id * a.kv_heads + ahead_head) * kRec, kRec,
+      bulk_load(ring + ahead_st * kStage, a.pool + ((uint64_t)id * a.kv_heads + ahead_head) * kRec, kRec,
                 bar + ahead_st * 8);
     }
     ++in_flight;
@@ -144,6 +156,10 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
 
   const uint32_t quad = lane / 4, t4 = lane % 4;  // row (or key, or column) of a fragment, place in the quad
   const uint32_t mi = lane / 8, mr = lane % 8;    // ldmatrix: matrix and row whose address this lane gives
+  // fp8 keys: keys 0-7 and 8-15 of a 16-byte chunk, then of the next; 16-bit: keys 0-7 of a chunk and of the next,
+  // then keys 8-15.  Values: keys 0-7 and 8-15 of a chunk, then of the next.
+  const uint32_t k_at = kFp8 ? offset8k<D>((mi & 1) * 8 + mr, mi >> 1) : offset16((mi >> 1) * 8 + mr, mi & 1);
+  const uint32_t v_at = kHalf + (kFp8 ? offset8v((mi & 1) * 8 + mr, mi >> 1) : offset16((mi & 1) * 8 + mr, mi >> 1));
   uint32_t st = 0, phase = 0;
   bool waited = false;
 
@@ -198,7 +214,7 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
         }
       }
     }
-    int ve = 0;  // fp8: the exponent (biased) that the output so far is relative to
+    float v_ref = 0.0f, v_inv = 0.0f;  // fp8: the scale that the output so far is relative to; 2^5 over it
     // the last key each of the two rows sees, and the last that all rows of the tile see
     const int32_t last = (int32_t)pc.end - 1;
     const int32_t lim_a = min(last, pc.climit + (int32_t)ta), lim_b = min(last, pc.climit + (int32_t)tb);
@@ -210,7 +226,7 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
     float ma = -INFINITY, mb = -INFINITY, la = 0.0f, lb = 0.0f;
 
     for (uint32_t bi = 0; bi < pc.nblocks; ++bi) {
-      const uint32_t rec = ring + st * kRec;
+      const uint32_t rec = ring + st * kStage;
       if (!mbar_wait_warp(bar + st * 8, phase)) {
         if (lane == 0) atomicOr_system(a.err, kErrWait);
         while (--in_flight) {  // the copies behind it write this warp's memory: they are waited for too
@@ -228,11 +244,10 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
 #pragma unroll
       for (int n = 0; n < 2; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
       if constexpr (kFp8) {
-        const uint32_t tok = (mi & 1) * 8 + mr;
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
-          uint32_t r[4];  // keys 0-7 and 8-15 of chunk c, then of chunk c + 1
-          ldsm4<false>(r, rec + offset8k<D>(tok, c + (mi >> 1)));
+          uint32_t r[4];
+          ldsm4<false>(r, (rec + k_at) ^ (c << 4));
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t b0, b1;
@@ -241,20 +256,18 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
           }
         }
       } else {
-        const uint32_t tok = (mi >> 1) * 8 + mr;
 #pragma unroll
         for (int kc = 0; kc < D / 16; ++kc) {
-          uint32_t r[4];  // keys 0-7: elements 0-7 and 8-15 of the step; keys 8-15: the same
-          ldsm4<false>(r, rec + offset16(tok, 2 * kc + (mi & 1)));
+          uint32_t r[4];
+          ldsm4<false>(r, (rec + k_at + (kc / 4) * (kBlock * 128)) ^ ((2 * kc % 8) << 4));
           mma16816<kFp16>(s[0], qf[kc], r[0], r[1]);
           mma16816<kFp16>(s[1], qf[kc], r[2], r[3]);
         }
       }
       float vs[4];  // fp8: the value rows' scales of this lane's keys
       if constexpr (kFp8) {
-        const uint32_t e0 = lds16(rec + 2 * kHalf + t4 * 2), e1 = lds16(rec + 2 * kHalf + 8 + t4 * 2);
-        const uint32_t f0 = lds16(rec + 2 * kHalf + 16 + t4 * 2), f1 = lds16(rec + 2 * kHalf + 24 + t4 * 2);
-        const float k0 = exp_value(e0 & 255u), k1 = exp_value(e0 >> 8), k2 = exp_value(e1 & 255u), k3 = exp_value(e1 >> 8);
+        const uint32_t ke = lds32(rec + 2 * kHalf + t4 * 4), vx = lds32(rec + 2 * kHalf + kBlock + t4 * 4);
+        const float k0 = exp_byte<0>(ke), k1 = exp_byte<1>(ke), k2 = exp_byte<2>(ke), k3 = exp_byte<3>(ke);
         s[0][0] = s[0][0] * qa_scale * k0;
         s[0][1] = s[0][1] * qa_scale * k1;
         s[0][2] = s[0][2] * qb_scale * k0;
@@ -266,25 +279,34 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
         // The values' scales go into the probabilities, relative to the largest scale so far and times 2^5: with
         // probabilities of at most 2^8 (below), their products stay below 2^15, and what fp16 holds with fewer
         // bits is below 2^-27 of what it could hold.
-        const int32_t here = (int32_t)pc.key0 + (int32_t)(bi * kBlock) + (int32_t)t4 * 2;
-        const int v0 = (int)(f0 & 255u), v1 = (int)(f0 >> 8), v2 = (int)(f1 & 255u), v3 = (int)(f1 >> 8);
-        int top = max(max(v0 < kExpNan && here <= last ? v0 : 0, v1 < kExpNan && here + 1 <= last ? v1 : 0),
-                      max(v2 < kExpNan && here + 8 <= last ? v2 : 0, v3 < kExpNan && here + 9 <= last ? v3 : 0));
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        if (top > ve + 1) {  // the same for the whole warp
-          const float f = ex2((float)(ve - top));
-          ve = top;
+        vs[0] = exp_byte<0>(vx);
+        vs[1] = exp_byte<1>(vx);
+        vs[2] = exp_byte<2>(vx);
+        vs[3] = exp_byte<3>(vx);
+        float top = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        if (top > 2.0f * v_ref) {  // the same for the whole warp; also where a row is marked or past the end
+          const int32_t here = (int32_t)pc.key0 + (int32_t)(bi * kBlock) + (int32_t)t4 * 2;
+          top = 0x1p-110f;
 #pragma unroll
-          for (int j = 0; j < kTiles; ++j)
+          for (int i = 0; i < 4; ++i)
+            if (vs[i] < 0x1p120f && here + (i & 1) + (i >> 1) * 8 <= last) top = fmaxf(top, vs[i]);
+          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+          if (top > 2.0f * v_ref) {
+            const uint32_t inverse = (254u << 23) - __float_as_uint(top);  // of a power of two
+            const float f = v_ref * __uint_as_float(inverse);
+            v_ref = top;
+            v_inv = __uint_as_float(inverse + (5u << 23));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+            for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+          }
         }
-        const int off = kExpBias + 5 - ve;
-        vs[0] = exp_value(v0 == kExpNan ? kExpNan : (uint32_t)max(v0 + off, 0));
-        vs[1] = exp_value(v1 == kExpNan ? kExpNan : (uint32_t)max(v1 + off, 0));
-        vs[2] = exp_value(v2 == kExpNan ? kExpNan : (uint32_t)max(v2 + off, 0));
-        vs[3] = exp_value(v3 == kExpNan ? kExpNan : (uint32_t)max(v3 + off, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vs[i] *= v_inv;
       } else {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
@@ -379,11 +401,10 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
       const uint32_t pf[4] = {pack2<kHalfP>(s[0][0], s[0][1]), pack2<kHalfP>(s[0][2], s[0][3]),
                               pack2<kHalfP>(s[1][0], s[1][1]), pack2<kHalfP>(s[1][2], s[1][3])};
       if constexpr (kFp8) {
-        const uint32_t tok = (mi & 1) * 8 + mr;
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
           uint32_t r[4];
-          ldsm4<true>(r, rec + kHalf + offset8v(tok, c + (mi >> 1)));
+          ldsm4<true>(r, (rec + v_at + (c / 4) * (kBlock * 64)) ^ ((c % 4) << 4));
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
             // a chunk's 16 columns: tile 2c has the even ones, tile 2c + 1 the odd ones
@@ -395,11 +416,10 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
           }
         }
       } else {
-        const uint32_t tok = (mi & 1) * 8 + mr;
 #pragma unroll
         for (int j = 0; j < kTiles; j += 2) {
           uint32_t r[4];
-          ldsm4<true>(r, rec + kHalf + offset16(tok, j + (mi >> 1)));
+          ldsm4<true>(r, (rec + v_at + (j / 8) * (kBlock * 128)) ^ ((j % 8) << 4));
           mma16816<kFp16>(acc[j], pf, r[0], r[1]);
           mma16816<kFp16>(acc[j + 1], pf, r[2], r[3]);
         }
@@ -443,7 +463,7 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
 
     // ---- the piece's result
     if constexpr (kFp8) {
-      const float f = __uint_as_float((uint32_t)max(ve - 5, 1) << 23);
+      const float f = v_ref * 0x1p-5f;
 #pragma unroll
       for (int j = 0; j < kTiles; ++j)
 #pragma unroll
@@ -554,7 +574,7 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
 
 template <int D, int FMT>
 constexpr int smem_bytes() {
-  return row_warps_of(FMT) * ring_stages<D, FMT>() * record_bytes(D, FMT);
+  return row_warps_of(FMT) * ring_stages<D, FMT>() * stage_bytes<D, FMT>();
 }
 
 template <int D, int FMT>

@@ -148,8 +148,8 @@ __global__ void __launch_bounds__(256) write_kernel(StoreArgs a) {
         *reinterpret_cast<uint4*>(rec + ko) = ck;
         *reinterpret_cast<uint4*>(rec + vo) = cv;
         if (c == 0) {
-          rec[2 * kHalf + tok] = (uint8_t)ek;
-          rec[2 * kHalf + kBlock + tok] = (uint8_t)ev;
+          rec[2 * kHalf + exp_place(tok)] = (uint8_t)ek;
+          rec[2 * kHalf + kBlock + exp_place(tok)] = (uint8_t)ev;
         }
       }
     } else if (ok) {
@@ -210,8 +210,8 @@ __global__ void __launch_bounds__(256) read_kernel(StoreArgs a) {
       ck = *reinterpret_cast<const uint4*>(rec + (kFp8 ? offset8k<D>(tok, c) : offset16(tok, c)));
       cv = *reinterpret_cast<const uint4*>(rec + kHalf + (kFp8 ? offset8v(tok, c) : offset16(tok, c)));
       if (kFp8) {
-        ek = rec[2 * kHalf + tok];
-        ev = rec[2 * kHalf + kBlock + tok];
+        ek = rec[2 * kHalf + exp_place(tok)];
+        ev = rec[2 * kHalf + kBlock + exp_place(tok)];
       }
     }
     const int64_t ko = (int64_t)t * a.k_tok + (int64_t)h * a.k_head + c * kN;

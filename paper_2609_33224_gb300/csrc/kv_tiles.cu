@@ -718,7 +718,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             const uint32_t dst = ring + at * C::kSlot;
             if (part == 0) {
               const bool live = rank * C::kKeys + kt < left;
-              const uint32_t e = live ? lds8(exps + (rank * kOwn + kb) * 32 + kt % kBlock) : (uint32_t)kExpBias;
+              const uint32_t e = live ? lds8(exps + (rank * kOwn + kb) * 32 + exp_place(kt % kBlock)) : (uint32_t)kExpBias;
               to_bf16<kChunks>(
                   e, live, [&](int c) { return raw + kb * C::kHalf + offset8k<D>(kt % kBlock, kc + c); },
                   [&](int c) {
@@ -727,7 +727,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
                   });
             } else {
               const bool live = tok < left;
-              const uint32_t e = live ? lds8(exps + vb * 32 + kBlock + tok % kBlock) : (uint32_t)kExpBias;
+              const uint32_t e = live ? lds8(exps + vb * 32 + kBlock + exp_place(tok % kBlock)) : (uint32_t)kExpBias;
               to_bf16<4>(
                   e, live, [&](int c) { return raw + C::kRawK + vb * (kBlock * 64) + offset8v(tok % kBlock, c); },
                   [&](int c) { return dst + tok * 128 + ((c ^ (tok & 7u)) << 4); });
