@@ -280,7 +280,8 @@ ps_status ps_kv_create(const ps_kv_config* cfg, ps_kv** out) {
   return PS_OK;
 }
 
-ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const int64_t* slots, uint64_t n, void* stream) {
+ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const int64_t* slots, uint64_t n,
+                      void* stream) {
   if (!kv) return PS_ERR_INVALID;
   ps_status st = reported(kv);
   if (st != PS_OK) return st;
@@ -292,7 +293,8 @@ ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const
   return PS_OK;
 }
 
-ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_rows* k, const ps_kv_rows* v, void* stream) {
+ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_rows* k, const ps_kv_rows* v,
+                     void* stream) {
   if (!kv) return PS_ERR_INVALID;
   ps_status st = reported(kv);
   if (st != PS_OK) return st;
@@ -333,7 +335,8 @@ ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_queries, u
   cudaError_t e = cudaStreamCreateWithFlags(&pl->copy, cudaStreamNonBlocking);
   for (int i = 0; i < 2 && e == cudaSuccess; ++i) e = cudaEventCreateWithFlags(&pl->buf[i].used, cudaEventDisableTiming);
   ps_status st = PS_OK;
-  for (int i = 0; i < 2 && e == cudaSuccess && st == PS_OK; ++i) st = grow(kv, pl->buf[i], max_blocks * 4 + max_spans * 256);
+  for (int i = 0; i < 2 && e == cudaSuccess && st == PS_OK; ++i)
+    st = grow(kv, pl->buf[i], max_blocks * 4 + max_spans * 256);
   if (e != cudaSuccess || st != PS_OK) {
     ps_kv_plan_destroy(pl);
     return e != cudaSuccess ? fail_cuda(kv, "ps_kv_plan_create", e) : st;
@@ -414,7 +417,8 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   const int D = (int)kv->D;
   cudaError_t e = cudaSuccess;
   if (pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, s);
-  if (e == cudaSuccess && pl->dev.row_workers) e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0, s);
+  if (e == cudaSuccess && pl->dev.row_workers)
+    e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0, s);
   if (e == cudaSuccess && pl->dev.njoin) e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev, s);
   if (!capturing) {  // also after a failed launch: the ones before it read the buffer
     const cudaError_t r = cudaEventRecord(b.used, s);

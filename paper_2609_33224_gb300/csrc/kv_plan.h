@@ -17,13 +17,14 @@
 namespace pskv {
 
 constexpr int kBlock = PS_BLOCK_TOKENS;
-constexpr int kSmallRows = 16;   // rows of a tile of the row kernel (one m16 of mma.sync)
+constexpr int kSmallRows = 16;  // rows of a tile of the row kernel (one m16 of mma.sync)
 
 // Rows of a tile of the tile kernel, two accumulators of 128 rows a CTA: with head_dim 128 a pair of CTAs
 // shares the keys and values.
 constexpr int tile_ctas_of(int D) { return D == 128 ? 2 : 1; }
 constexpr int tile_rows_of(int D) { return 256 * tile_ctas_of(D); }
-constexpr int kTileKeys = 128;   // keys of one step of the tile kernel
+constexpr int kTileKeys = 128;  // keys of one step of the tile kernel
+
 // Workers (warps) of a CTA of the row kernel.  fp8 blocks take as many instructions as 16-bit ones of twice the
 // bytes: 12 warps hide more of their latency (131072 tokens of 5 requests: 182 us, 187 with 8); 16-bit ones are
 // bound by bytes with 8 (64 requests on a prefix: 58 us, 59 with 12, whose shares are shorter).
@@ -49,8 +50,8 @@ static_assert(sizeof(Piece) == 48, "Piece layout");
 constexpr uint32_t kDirect = 0xFFFFFFFFu;
 constexpr int32_t kNoLimit = 0x3FFFFFFF;
 
-// What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments segs[seg0] ..:
-// the i-th row's are the partial rows row + i + k * stride, k < nparts.
+// What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments
+// segs[seg0] ..: the i-th row's are the partial rows row + i + k * stride, k < nparts.
 struct JoinEntry {
   uint32_t query;
   uint16_t head0, count;
@@ -90,16 +91,23 @@ struct PlanShape {
 constexpr double kTileLaunch = 1000.0;
 inline double block_ns(const PlanShape& kv) {
   const bool fp8 = kv.fmt == PS_KV_FP8;
-  return kv.D == 128 ? (fp8 ? 0.67 : 0.51) : (fp8 ? 0.50 : 0.40);
+  return kv.D == 128 ? (fp8 ? 0.60 : 0.51) : (fp8 ? 0.50 : 0.40);
 }
 inline double step_ns(const PlanShape& kv) {
   const bool fp8 = kv.fmt == PS_KV_FP8;
   return kv.D == 128 ? (fp8 ? 20.5 : 17.5) : (fp8 ? 9.0 : 8.0);
 }
 constexpr int kPieceSteps = 3;
+// Bytes that a token has in one head.
+inline double token_bytes(const PlanShape& kv) { return kv.fmt == PS_KV_FP8 ? 2 * (kv.D + 1.0) : 4.0 * kv.D; }
 inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool causal) {
-  const double dear = causal && rows > (uint32_t)kSmallRows ? 4 : 1;
-  const double by_rows = dear * block_ns(kv) * ((rows + kSmallRows - 1) / kSmallRows) * (double)((keys + kBlock - 1) / kBlock);
+  const uint32_t row_tiles = (rows + kSmallRows - 1) / kSmallRows;
+  const double dear = causal && row_tiles > 1 ? 4 : 1;
+  double by_rows = dear * block_ns(kv) * row_tiles * (double)((keys + kBlock - 1) / kBlock);
+  // Keys that L2 does not hold come from memory again for every other 16 rows: 64 rows on 65536 tokens (268 MB) 124 us,
+  // 65 by tiles; 32 rows 55 and 65.
+  if (row_tiles > 2 && (double)keys * token_bytes(kv) * kv.heads > 96e6)
+    by_rows = std::max(by_rows, row_tiles / 2.0 * (double)keys * token_bytes(kv) / 5000.0);
   return by_rows - step_ns(kv) * (double)((keys + kTileKeys - 1) / kTileKeys + kPieceSteps);
 }
 
@@ -112,11 +120,11 @@ constexpr uint32_t kSplitSteps = 8;
 // side they take less time than one after the other.  Returns how many SMs the row kernel gets (all: one after the
 // other), by the times above, 3.3 ns of the GPU for a unit's start and end, the bytes at 6.2 TB/s, and what the
 // kernels take whatever their SMs: 6 and 4 us.  64 queries on 8192 shared tokens 55.7 -> 41.8 us, 9 groups under one
-// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 272 -> 260.
+// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 267 -> 260.
 constexpr double kUnitNs = 3.3, kBytesPerNs = 6200.0, kTileFixed = 6000.0, kRowFixed = 4000.0;
 inline int row_sms(const PlanShape& kv, double steps, double blocks, double units) {
   const double tile = step_ns(kv) * steps, work = block_ns(kv) * blocks + kUnitNs * units;
-  const double bytes = blocks * (kv.fmt == PS_KV_FP8 ? 2 * kBlock * (kv.D + 1.0) : 4.0 * kBlock * kv.D) / kBytesPerNs;
+  const double bytes = blocks * kBlock * token_bytes(kv) / kBytesPerNs;
   double best = kTileFixed + tile + kRowFixed + std::max(work, bytes);
   int sms = kv.sms;
   for (int x = 2; x < kv.sms; x += 2) {

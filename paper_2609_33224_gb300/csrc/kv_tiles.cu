@@ -24,6 +24,11 @@
 //
 // Bound by the tensor cores for full tiles: 4 * D multiply-adds a row and key, and, near that, the
 // exponentials: one per row and key.  Work is cut into equal shares per worker; each walks its pieces.
+// 9900 rows of 8 heads and 128 columns on 16384 keys, bf16, 665 GFLOP: 393 us = 1.69 PFLOP/s, 98% of what a
+// library product keeps up at the card's power limit (1.72; 1.94 in a burst); fp8, 2048 rows on 32768: 180 us
+// = 1.56 PFLOP/s (the ALU pipe, which the conversions share with the softmax, at half).  A step of 128 keys takes
+// 2400 cycles (2048 at the nominal rate); start and end of a worker take about 12000, the queries' and the
+// first keys' way 7000, the result's 5000.
 #include "kv_internal.cuh"
 
 namespace pskv {
@@ -79,8 +84,8 @@ __device__ __forceinline__ void tc_dealloc(uint32_t addr, uint32_t cols) {
 template <int CTAS>
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   if (CTAS == 2)
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                 "h"((uint16_t)3)
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3)
                  : "memory");
   else
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -92,7 +97,8 @@ template <int CTAS>
 __device__ __forceinline__ void arrive_first(uint32_t bar) {
   if (CTAS == 2)
     asm volatile(
-        "{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [a];\n}\n" ::"r"(bar)
+        "{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, 0;\n"
+        " mbarrier.arrive.shared::cluster.b64 _, [a];\n}\n" ::"r"(bar)
         : "memory");
   else
     mbar_arrive(bar);
@@ -145,8 +151,10 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
         : "memory");
 }
 
-#define TC_R8(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3]), "=r"(a[i + 4]), "=r"(a[i + 5]), "=r"(a[i + 6]), "=r"(a[i + 7])
-#define TC_I8(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3]), "r"(a[i + 4]), "r"(a[i + 5]), "r"(a[i + 6]), "r"(a[i + 7])
+#define TC_R4(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3])
+#define TC_I4(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3])
+#define TC_R8(a, i) TC_R4(a, i), TC_R4(a, i + 4)
+#define TC_I8(a, i) TC_I4(a, i), TC_I4(a, i + 4)
 
 // 32 columns of the calling warp's 32 lanes, one lane a thread
 __device__ __forceinline__ void tc_ld32(uint32_t (&r)[32], uint32_t addr) {
@@ -166,8 +174,8 @@ __device__ __forceinline__ void tc_ld16(uint32_t (&r)[16], uint32_t addr) {
 }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::TC_I8(r, 0),
-      TC_I8(r, 8), "r"(addr)
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+      ::TC_I8(r, 0), TC_I8(r, 8), "r"(addr)
       : "memory");
 }
 
@@ -218,7 +226,8 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, ui
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// fp8: the codes of `n` chunks of a row, at `src(c)`, as bf16 with the row's scale applied, to `dst(2 c)`, `dst(2 c + 1)`.
+// fp8: the codes of `n` chunks of a row, at `src(c)`, as bf16 with the row's scale applied, to `dst(2 c)` and
+// `dst(2 c + 1)`.
 // value = code * 2^120 * 2^(e - 127); the second factor as a bf16, a NaN for a row with a NaN.
 template <int N, class Src, class Dst>
 __device__ __forceinline__ void to_bf16(uint32_t e, bool live, Src src, Dst dst) {
@@ -228,7 +237,10 @@ __device__ __forceinline__ void to_bf16(uint32_t e, bool live, Src src, Dst dst)
   for (int c = 0; c < N; ++c) {
     uint32_t w[4] = {0, 0, 0, 0}, o[8];
     if (live)
-      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src(c)) : "memory");
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                   : "r"(src(c))
+                   : "memory");
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       o[2 * i] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x1404));
@@ -335,8 +347,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
 #pragma unroll
         for (int i = 0; i < 32 / kAt; ++i) {
           const uint32_t to = (r & ~31u) + i * kAt + lane / kLanes;
-          sts128(q_smem + t * C::kQ + (c / 8) * (128 * 128) + to * 128 + (((c % 8) ^ (to & 7u)) << 4), w[i].x ^ flip, w[i].y ^ flip,
-                 w[i].z ^ flip, w[i].w ^ flip);
+          sts128(q_smem + t * C::kQ + (c / 8) * (128 * 128) + to * 128 + (((c % 8) ^ (to & 7u)) << 4),
+                 w[i].x ^ flip, w[i].y ^ flip, w[i].z ^ flip, w[i].w ^ flip);
         }
       }
       fence_async_shared();
@@ -442,7 +454,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           tc_wait_ld();
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            sts128(stage + lane * (kCols * 4) + (((4 * c + i) ^ (lane & 7u)) << 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            sts128(stage + lane * (kCols * 4) + (((4 * c + i) ^ (lane & 7u)) << 4), o[4 * i], o[4 * i + 1],
+                   o[4 * i + 2], o[4 * i + 3]);
         }
         __syncwarp();
         constexpr int kAt = 32 / kChunks;  // rows a round of the warp stores
@@ -473,7 +486,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         if (!direct)
           a.part_ml[at] = make_float2(m, l);
         else if (a.lse)
-          a.lse[(uint64_t)query * a.kv_heads * a.group + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+          a.lse[(uint64_t)query * a.kv_heads * a.group + head] =
+              l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
       }
       tc_fence_before();  // the reads of O before the next piece's products, which p_ready orders
     }
@@ -558,7 +572,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     const uint32_t tmem = all_here();
     if (warp == 9 && rank == 0 && elect_one()) {
       // ================= products: one thread waits and issues =================
-      constexpr uint32_t id_s = instruction(C::kFp16, C::kRows, kTileKeys, false), id_o = instruction(C::kFp16, C::kRows, D, true);
+      constexpr uint32_t id_s = instruction(C::kFp16, C::kRows, kTileKeys, false);
+      constexpr uint32_t id_o = instruction(C::kFp16, C::kRows, D, true);
       uint32_t n = 0;  // slots taken
       uint32_t p_seen[2] = {0, 0}, q_seen[2] = {0, 0}, tails = 0;
       bool alive = true;
@@ -576,7 +591,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         const uint64_t vd = ring_desc + slot * (C::kSlot >> 4);
 #pragma unroll
         for (int k = 4 * half; k < 4 * half + 4; ++k)
-          tc_mma_ts<C::kCtas>(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + ((k * 16 * 128) >> 4), id_o, acc || k > 0);
+          tc_mma_ts<C::kCtas>(tmem + 256 + t * 128, tmem + t * 128 + k * 8, vd + ((k * 16 * 128) >> 4), id_o,
+                              acc || k > 0);
       };
       for (uint32_t pi = first; alive && pi < last; ++pi) {
         const Piece* pp = p.tile_pieces + pi;
@@ -663,7 +679,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         mbar_arrive(smem_u32(&bars.tail_here));
       }
     } else if (warp == 10 && !C::kFp8) {
-      // ================= partial steps: value rows past the end, which hold other tokens or earlier steps =================
+      // ================= partial steps: value rows past the end hold other tokens or earlier steps =================
       uint32_t n = 0, tails = 0;
       bool alive = true;
       for (uint32_t pi = first; alive && pi < last; ++pi) {
@@ -678,7 +694,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           break;
         }
         const uint32_t v = ring + (n - 1) % C::kSlots * C::kSlot;  // the last step's values
-        for (uint32_t i = left * 8 + lane; i < kTileKeys * 8; i += 32) sts128(v + (i / 8) * 128 + (i % 8) * 16, 0, 0, 0, 0);
+        for (uint32_t i = left * 8 + lane; i < kTileKeys * 8; i += 32)
+          sts128(v + (i / 8) * 128 + (i % 8) * 16, 0, 0, 0, 0);
         fence_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars.tail_done));
@@ -718,7 +735,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             const uint32_t dst = ring + at * C::kSlot;
             if (part == 0) {
               const bool live = rank * C::kKeys + kt < left;
-              const uint32_t e = live ? lds8(exps + (rank * kOwn + kb) * 32 + exp_place(kt % kBlock)) : (uint32_t)kExpBias;
+              const uint32_t at_e = exps + (rank * kOwn + kb) * 32 + exp_place(kt % kBlock);
+              const uint32_t e = live ? lds8(at_e) : (uint32_t)kExpBias;
               to_bf16<kChunks>(
                   e, live, [&](int c) { return raw + kb * C::kHalf + offset8k<D>(kt % kBlock, kc + c); },
                   [&](int c) {
@@ -727,7 +745,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
                   });
             } else {
               const bool live = tok < left;
-              const uint32_t e = live ? lds8(exps + vb * 32 + kBlock + exp_place(tok % kBlock)) : (uint32_t)kExpBias;
+              const uint32_t at_e = exps + vb * 32 + kBlock + exp_place(tok % kBlock);
+              const uint32_t e = live ? lds8(at_e) : (uint32_t)kExpBias;
               to_bf16<4>(
                   e, live, [&](int c) { return raw + C::kRawK + vb * (kBlock * 64) + offset8v(tok % kBlock, c); },
                   [&](int c) { return dst + tok * 128 + ((c ^ (tok & 7u)) << 4); });

@@ -312,3 +312,29 @@ def test_one_tile_over_many_keys(kv, fmt, D):
     T = 40
     b = Batch(kv, fmt, 2, 4, D, [(0, T, 40003, 0)] + [(i, 1, 5, 1) for i in range(T)], T, seed=7)
     b.check(*b.run())
+
+
+@pytest.mark.parametrize("fmt,D", [("bf16", 128), ("fp8", 128), ("fp16", 64), ("fp8", 64)])
+def test_tiles_scales_and_values_that_are_not_finite(kv, fmt, D):
+    """The tile kernel: negative and zero scales, a length that ends inside a block, and a NaN or an infinity in a
+    token that every query sees."""
+    import torch
+    T, n = 200, 1001
+    b = Batch(kv, fmt, 2, 4, D, [(0, T, n, 0)], T, seed=17)
+    for scale in (None, -0.3, 0.0):
+        b.check(*b.run(scale=scale), scale=scale)
+    k, v = b.k.clone(), b.v.clone()
+    v[b.slots_of[0][1000], 0, 5] = math.nan
+    v[b.slots_of[0][7], 1, 6] = math.inf
+    b.cache.write(k, v, torch.arange(k.shape[0], device="cuda"))
+    out, _ = b.run()
+    if fmt == "fp8":  # a row with a NaN is NaN whole; an infinity is held as a large number
+        assert torch.isnan(out[:, :4]).all() and torch.isfinite(out[:, 4:]).all()
+    else:
+        assert torch.isnan(out[:, :4, 5]).all() and torch.isposinf(out[:, 4:, 6]).all()
+        keep = torch.ones(D, dtype=torch.bool, device="cuda")
+        keep[[5, 6]] = False
+        assert torch.isfinite(out[:, :, keep]).all()
+    k[b.slots_of[0][300], 1] = math.nan
+    b.cache.write(k, v, torch.arange(k.shape[0], device="cuda"))
+    assert torch.isnan(b.run()[0][:, 4:]).all()
