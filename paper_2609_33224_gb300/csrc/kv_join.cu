@@ -19,13 +19,16 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
   constexpr int kV = D / 32, kAhead = 4;
   constexpr uint32_t kStep = kWide ? 8 : 1, kFull = 0xFFFFFFFFu;
   using Vec = typename std::conditional<kV == 4, float4, float2>::type;
-  wait_for_last();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t row = kWide ? blockIdx.x : blockIdx.x * 8 + warp;
-  if (row >= p.njoin * a.group) return;  // kWide: the whole CTA
-  const JoinEntry en = p.join[row / a.group];
+  // What there is to join is the plan's; the parts are the kernels' before this one.
+  const bool live = row < p.njoin * a.group;  // kWide: the same for the whole CTA
+  const JoinEntry en = live ? p.join[row / a.group] : JoinEntry{};
   const uint32_t gi = row % a.group;
-  if (gi >= en.count) return;  // the same
+  JoinSeg ahead_seg{0, 0, 0};
+  if (lane < min(32u, en.nsegs)) ahead_seg = p.segs[en.seg0 + lane];
+  wait_for_last();
+  if (!live || gi >= en.count) return;
   const uint32_t query = en.query, head = en.head0 + gi;
 
   const float* part = a.part + lane * kV;
@@ -42,8 +45,8 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
   };
   for (uint32_t s0 = 0; s0 < en.nsegs; s0 += 32) {
     const uint32_t ns = min(32u, en.nsegs - s0);
-    JoinSeg sg{0, 0, 0};
-    if (lane < ns) sg = p.segs[en.seg0 + s0 + lane];
+    JoinSeg sg = ahead_seg;
+    if (s0 > 0) sg = lane < ns ? p.segs[en.seg0 + s0 + lane] : JoinSeg{0, 0, 0};
     const uint32_t total = __reduce_add_sync(kFull, sg.nparts);
     for (uint32_t c = kWide ? warp : 0; c < total; c += 32 * kStep) {
       const uint32_t mine = c + lane * kStep;
