@@ -25,10 +25,10 @@ constexpr int tile_ctas_of(int D) { return D == 128 ? 2 : 1; }
 constexpr int tile_rows_of(int D) { return 256 * tile_ctas_of(D); }
 constexpr int kTileKeys = 128;  // keys of one step of the tile kernel
 
-// Workers (warps) of a CTA of the row kernel.  fp8 blocks take as many instructions as 16-bit ones of twice the
-// bytes: 12 warps hide more of their latency (131072 tokens of 5 requests: 182 us, 187 with 8); 16-bit ones are
-// bound by bytes with 8 (64 requests on a prefix: 58 us, 59 with 12, whose shares are shorter).
-constexpr int row_warps_of(int fmt) { return fmt == PS_KV_FP8 ? 12 : 8; }
+// Workers (warps) of a CTA of the row kernel.  12 hide more of a block's latency than 8 (131072 tokens of 5
+// requests, fp8: 182 us, 187; 64 queries on 8192, on 72 SMs: 40.3 and 41.1); 16 leave 128 registers a thread, and
+// spill (223 us).
+constexpr int kRowWarps = 12;
 
 // A piece of work of either attention kernel: a run of key blocks for the rows of one tile and one
 // key/value head.  A span's rows are its queries' heads of the group, row r = (r / g)-th query, head r % g.
@@ -138,11 +138,11 @@ inline int row_sms(const PlanShape& kv, double steps, double blocks, double unit
   return sms;
 }
 
-// A piece of the row kernel joins up to this many tile parts into its rows, where a worker has at least so many
-// units of rows that the time this takes evens out.  192 new tokens on 16384 (4 units a worker, 2 to 3 parts):
-// 456 us, 491 with the join kernel; 256 queries on 32768 (1 unit a worker, 3 parts) 288 and 277 us, 64 on 8192
-// (10 parts) 92 and 60.
-constexpr size_t kFoldMost = 3, kFoldUnits = 3;
+// A piece of the row kernel joins up to this many tile parts into its rows, where an SM has at least so many units
+// of rows that the time this takes evens out.  192 new tokens on 16384 (31 units an SM, 2 to 3 parts): 456 us, 491
+// with the join kernel; 256 queries on 32768 (13 units an SM, 3 parts) 288 and 277 us, 64 on 8192 (10 parts) 92
+// and 60.
+constexpr size_t kFoldMost = 3, kFoldUnits = 24;
 
 // Rows of one tile and one head over a range of key blocks, before it is cut into pieces.
 struct Unit {
@@ -357,7 +357,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     p->nfold = (uint32_t)(o.folds.size() - folds);
     return true;
   };
-  const bool may_fold = o.row_units.size() >= kFoldUnits * (size_t)(pl.sms * row_warps_of(pl.fmt));
+  const bool may_fold = o.row_units.size() >= kFoldUnits * (size_t)pl.sms;
   o.row_sms = pl.sms;
   if (!o.tile_units.empty() && !o.row_units.empty() && !may_fold) {
     double steps = 0, blocks = 0;
@@ -366,7 +366,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     o.row_sms = row_sms(pl, steps, blocks, (double)o.row_units.size());
   }
   const int tile_sms = o.row_sms < pl.sms ? pl.sms - o.row_sms : pl.sms;
-  const uint32_t row_workers = (uint32_t)(o.row_sms * row_warps_of(pl.fmt));
+  const uint32_t row_workers = (uint32_t)(o.row_sms * kRowWarps);
   auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();

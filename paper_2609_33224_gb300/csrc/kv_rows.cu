@@ -102,13 +102,13 @@ __device__ __forceinline__ float value16(uint16_t b) {
 }
 
 template <int D, int FMT>
-__global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
+__global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
   constexpr bool kFp8 = FMT == PS_KV_FP8, kFp16 = FMT == PS_KV_FP16;
   constexpr int kRec = record_bytes(D, FMT), kHalf = half_bytes(D, FMT);
   constexpr int kStages = ring_stages<D, FMT>();
   constexpr int kTiles = D / 8;  // n8 tiles of the output
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ __align__(8) uint64_t bars[row_warps_of(FMT) * kStages];
+  __shared__ __align__(8) uint64_t bars[kRowWarps * kStages];
 
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t worker = warp * p.row_ctas + blockIdx.x;  // neighbours in the plan go to different SMs
@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(row_warps_of(FMT) * 32, 1) rows_kernel(const A
 
 template <int D, int FMT>
 constexpr int smem_bytes() {
-  return row_warps_of(FMT) * ring_stages<D, FMT>() * stage_bytes<D, FMT>();
+  return kRowWarps * ring_stages<D, FMT>() * stage_bytes<D, FMT>();
 }
 
 template <int D, int FMT>
@@ -593,7 +593,7 @@ cudaError_t prepare_one() {
 }
 template <int D, int FMT>
 cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
-  return launch(rows_kernel<D, FMT>, p.row_ctas, row_warps_of(FMT) * 32, smem_bytes<D, FMT>(), 1, overlap, s, a, p);
+  return launch(rows_kernel<D, FMT>, p.row_ctas, kRowWarps * 32, smem_bytes<D, FMT>(), 1, overlap, s, a, p);
 }
 
 }  // namespace

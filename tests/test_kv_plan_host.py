@@ -43,7 +43,7 @@ int main() {
       // side by side, the kernels share the SMs
       CHECK(o.row_sms > 0 && o.row_sms <= (int)sms);
       const unsigned tile_sms = o.row_sms < (int)sms ? sms - o.row_sms : sms;
-      const unsigned workers = kind ? tile_sms / tile_ctas_of(D) : o.row_sms * row_warps_of(fmt);
+      const unsigned workers = kind ? tile_sms / tile_ctas_of(D) : o.row_sms * kRowWarps;
       if (pieces.empty()) { CHECK(off.size() <= 1); continue; }
       CHECK(off.front() == 0 && off.back() == pieces.size() && off.size() - 1 <= workers);
       uint64_t total = 0, most = 0;
