@@ -118,8 +118,9 @@ PS_API ps_status ps_kv_plan_workspace(ps_kv_plan* plan, uint64_t* bytes);
  * kv_heads)), out_i = sum_j e^z_ij v_j / sum_j e^z_ij and lse_i = log sum_j e^z_ij; without a key, zeros
  * and -infinity.  q and out have one 16-bit type: the cache's, or PS_KV_BF16 with PS_KV_FP8.  lse: NULL, or
  * num_queries x q_heads floats.  workspace: device memory, 256-byte aligned, used by this call alone while
- * it runs.  kv may be another cache than the plan's, of the same shape.  Scores, sums and partial results
- * are held in 32 bits, probabilities are rounded to q's type for their product with the values.
+ * it runs.  The stream has to exist until the plan is set again, used on another stream or destroyed.  kv may
+ * be another cache than the plan's, of the same shape.  Scores, sums and partial results are held in 32 bits,
+ * probabilities are rounded to 16 bits for their product with the values.
  * The decode and prefill steps of Eq. 6 and Eq. 7 consist of it; the paper has no counterpart.
  * Errors: PS_ERR_INVALID, PS_ERR_STATE (no batch is set), PS_ERR_CUDA. */
 PS_API ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,

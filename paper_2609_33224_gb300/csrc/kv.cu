@@ -30,9 +30,9 @@ struct ps_kv_plan {
     uint8_t* dev = nullptr;
     uint8_t* host = nullptr;
     size_t cap = 0;
-    cudaEvent_t used = nullptr;  // after the last call that read it
-    bool in_use = false;
-    cudaStream_t last = nullptr;
+    cudaEvent_t used = nullptr;  // after the calls that read it, once recorded
+    bool in_use = false, recorded = false;
+    cudaStream_t last = nullptr;  // of the last such call, which comes after all others
   } buf[2];
   int cur = 0;
   bool set = false, frozen = false;
@@ -126,8 +126,19 @@ size_t place(std::vector<std::pair<const void*, size_t>>* parts, size_t* at, con
   return here;
 }
 
+// Marks the end of the calls that have read a buffer so far.
+cudaError_t mark_used(ps_kv_plan::Buffer& b) {
+  if (!b.in_use || b.recorded) return cudaSuccess;
+  const cudaError_t e = cudaEventRecord(b.used, b.last);
+  b.recorded = e == cudaSuccess;
+  return e;
+}
+
 void release(ps_kv_plan::Buffer& b) {
-  if (b.in_use) cudaEventSynchronize(b.used);
+  if (mark_used(b) != cudaSuccess)
+    cudaDeviceSynchronize();
+  else if (b.in_use)
+    cudaEventSynchronize(b.used);
   if (b.used) cudaEventDestroy(b.used);
   if (b.dev) cudaFree(b.dev);
   if (b.host) cudaFreeHost(b.host);
@@ -190,10 +201,14 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   parts.emplace_back(blocks, n_blocks * sizeof(uint32_t));
   at += n_blocks * sizeof(uint32_t);
 
+  // The calls of the set before keep reading their buffer: their end is marked now, while nothing else has been
+  // queued behind them, and waited for when that buffer's turn comes.
+  KV_CUDA(kv, mark_used(pl->buf[pl->cur]));
   ps_kv_plan::Buffer& b = pl->buf[pl->cur ^ 1];
   if (b.in_use) {
+    KV_CUDA(kv, mark_used(b));
     KV_CUDA(kv, cudaEventSynchronize(b.used));
-    b.in_use = false;
+    b.in_use = b.recorded = false;
   }
   const ps_status st = grow(kv, b, at);
   if (st != PS_OK) return st;
@@ -396,8 +411,10 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   const bool capturing = cap != cudaStreamCaptureStatusNone;
   if (capturing)
     pl->frozen = true;
-  else if (b.in_use && b.last != s)  // so that the last call's event stands for all calls before it
+  else if (b.in_use && b.last != s) {  // so that the last call's stream stands for all calls before it
+    KV_CUDA(kv, mark_used(b));
     KV_CUDA(kv, cudaStreamWaitEvent(s, b.used, 0));
+  }
 
   pskv::AttnArgs a{};
   a.pool = kv->pool;
@@ -421,13 +438,9 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
     e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0, s);
   if (e == cudaSuccess && pl->dev.njoin) e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev, s);
   if (!capturing) {  // also after a failed launch: the ones before it read the buffer
-    const cudaError_t r = cudaEventRecord(b.used, s);
-    if (r == cudaSuccess) {
-      b.in_use = true;
-      b.last = s;
-    } else if (e == cudaSuccess) {
-      e = r;
-    }
+    b.in_use = true;
+    b.recorded = false;
+    b.last = s;
   }
   if (e != cudaSuccess) return fail_cuda(kv, "ps_kv_attend", e);
   return PS_OK;
