@@ -74,6 +74,7 @@ struct AttnArgs {
   float2* part_ml;  // [part row] maximum (of the scores times log2 e) and sum
   uint32_t kv_heads, group;
   float scale_log2;
+  uint32_t rows_first;  // the row kernel is the call's first: it waits for what came before
   uint32_t* err;  // mapped host word
 };
 
@@ -93,7 +94,7 @@ cudaError_t launch_write(int D, int fmt, int type, const StoreArgs& a, int sms, 
 cudaError_t launch_read(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
-cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
+cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
 cudaError_t prepare_tiles(int D, int fmt);
 // ---- PTX ----------------------------------------------------------------------------------------------
@@ -145,8 +146,9 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                "l"(src), "r"(bytes), "r"(bar)
                : "memory");
 }
-// A call's kernels are launched so that the next may start while the last one ends: a kernel lets the next one
-// start at once, and waits for the one before (and with it all earlier ones) where it reads their results, at
+// A call's kernels are launched so that the next may start while the last one ends.  The call's first kernel waits for
+// what came before it in the stream where it first reads or writes anything but the plan, and only then lets the next
+// one start; each later one waits for the one before it (and with it all earlier ones) where it reads its results, at
 // the latest before it ends.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
   const uint32_t gi = row % a.group;
   JoinSeg ahead_seg{0, 0, 0};
   if (lane < min(32u, en.nsegs)) ahead_seg = p.segs[en.seg0 + lane];
+  let_next_start();  // the next call's first kernel, which waits for this one
   wait_for_last();
   if (!live || gi >= en.count) return;
   const uint32_t query = en.query, head = en.head0 + gi;

@@ -87,7 +87,7 @@ __device__ __forceinline__ void sts128_zero(uint32_t addr) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(addr), "r"(0) : "memory");
 }
 
-__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 // Whether one of the two 16-bit floats in w is an infinity or a NaN.
 template <bool FP16>
@@ -112,7 +112,6 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t worker = warp * p.row_ctas + blockIdx.x;  // neighbours in the plan go to different SMs
-  let_next_start();
   if (worker >= p.row_workers) {  // no barrier of the CTA is used
     wait_for_last();
     return;
@@ -127,6 +126,14 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
   const uint32_t piece_end = p.row_off[worker + 1];
   // what is loaded next: block `ahead_i` of piece `ahead`, into stage `ahead_st`
   uint32_t ahead = p.row_off[worker], ahead_i = 0, ahead_st = 0;
+  // The plan is read at once, the cache and the queries after what may have written them; after a tile kernel of the
+  // same call, which has waited for that, at once too.
+  bool waited = a.rows_first != 0;
+  if (waited) {
+    prefetch(p.row_pieces + ahead);
+    wait_for_last();
+  }
+  let_next_start();
   uint32_t ahead_n = 0, ahead_block = 0, ahead_head = 0, ids = 0;
   uint32_t in_flight = 0;
   auto issue = [&]() {
@@ -169,7 +176,6 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
   const uint32_t k_at = kFp8 ? offset8k<D>((mi & 1) * 8 + mr, mi >> 1) : offset16((mi >> 1) * 8 + mr, mi & 1);
   const uint32_t v_at = kHalf + (kFp8 ? offset8v((mi & 1) * 8 + mr, mi >> 1) : offset16((mi & 1) * 8 + mr, mi >> 1));
   uint32_t st = 0, phase = 0;
-  bool waited = false;
 
   for (uint32_t pi = p.row_off[worker]; pi < piece_end; ++pi) {
     const Piece pc = p.row_pieces[pi];
@@ -186,10 +192,10 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
       for (int kc = 0; kc < D / 16; ++kc) {
         // fp8: the key fragment of a 16-byte chunk has this lane's four neighbouring elements
         const int lo = kFp8 ? kc * 16 + t4 * 4 : kc * 16 + t4 * 2, hi = kFp8 ? lo + 2 : lo + 8;
-        qf[kc][0] = va ? *reinterpret_cast<const uint32_t*>(qa + lo) : 0u;
-        qf[kc][1] = vb ? *reinterpret_cast<const uint32_t*>(qb + lo) : 0u;
-        qf[kc][2] = va ? *reinterpret_cast<const uint32_t*>(qa + hi) : 0u;
-        qf[kc][3] = vb ? *reinterpret_cast<const uint32_t*>(qb + hi) : 0u;
+        qf[kc][0] = va ? __ldcg(reinterpret_cast<const uint32_t*>(qa + lo)) : 0u;
+        qf[kc][1] = vb ? __ldcg(reinterpret_cast<const uint32_t*>(qb + lo)) : 0u;
+        qf[kc][2] = va ? __ldcg(reinterpret_cast<const uint32_t*>(qa + hi)) : 0u;
+        qf[kc][3] = vb ? __ldcg(reinterpret_cast<const uint32_t*>(qb + hi)) : 0u;
       }
     }
     // fp8: codes are exact in fp16 and one instruction turns two of them into it, so the products are fp16.
@@ -244,7 +250,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           }
           mbar_wait(bar + st * 8, phase);
         }
-        wait_for_last();
+        if (!waited) wait_for_last();
         return;
       }
       // ---- scores

@@ -270,7 +270,6 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   auto full = [&](uint32_t i) { return smem_u32(&bars.full[i]); };
   auto empty = [&](uint32_t i) { return smem_u32(&bars.empty[i]); };
 
-  let_next_start();
   const uint32_t first = p.tile_off[worker], last = p.tile_off[worker + 1];
   if (warp == 8 && lane == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
@@ -320,6 +319,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     bool alive = true;
     for (uint32_t pi = first; alive && pi < last; ++pi) {
       const Piece pc = p.tile_pieces[pi];
+      if (pi == first) wait_for_last();  // the plan is read before, queries and results' places after
       if (!pc.split && t * C::kRows >= pc.nrows) continue;
       const uint32_t in_tile = (pc.split ? 0 : t * C::kRows) + rank * 128 + r;
       const uint32_t row = pc.row0 + in_tile;
@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           const int from = i * kAt + lane / kLanes;
           const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, from);
           const bool ok = __shfl_sync(0xFFFFFFFFu, (int)valid, from) != 0;
-          w[i] = ok ? *reinterpret_cast<const uint4*>(a.q + at + 8 * c) : make_uint4(0, 0, 0, 0);
+          w[i] = ok ? __ldcg(reinterpret_cast<const uint4*>(a.q + at + 8 * c)) : make_uint4(0, 0, 0, 0);
         }
         if (!here) {
           const uint32_t tmem = all_here();
@@ -532,6 +532,8 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       __syncwarp();
       asm volatile("barrier.cta.arrive 1, %0;" ::"n"(C::kWarps * 32) : "memory");
       arrive_worker<C::kCtas>();
+      wait_for_last();
+      let_next_start();  // the row kernel, which does not wait for what came before this one
       bool alive = true, begun = false;
       for (uint32_t pi = first; alive && pi < last; ++pi) {
         const Piece* pp = p.tile_pieces + pi;
@@ -782,9 +784,9 @@ cudaError_t prepare_one() {
   return cudaFuncSetAttribute(tiles_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, FMT>::kSmem);
 }
 template <int D, int FMT>
-cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   using C = Cfg<D, FMT>;
-  return launch(tiles_kernel<D, FMT>, p.tile_workers * C::kCtas, C::kWarps * 32, C::kSmem, C::kCtas, false, s, a, p);
+  return launch(tiles_kernel<D, FMT>, p.tile_workers * C::kCtas, C::kWarps * 32, C::kSmem, C::kCtas, overlap, s, a, p);
 }
 
 }  // namespace
@@ -799,14 +801,14 @@ cudaError_t prepare_tiles(int D, int fmt) {
                              : prepare_one<64, PS_KV_FP8>();
 }
 
-cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   if (D == 128)
-    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, s)
-           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, s)
-                               : launch_one<128, PS_KV_FP8>(a, p, s);
-  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, s)
-         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, s)
-                             : launch_one<64, PS_KV_FP8>(a, p, s);
+    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, overlap, s)
+           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, overlap, s)
+                               : launch_one<128, PS_KV_FP8>(a, p, overlap, s);
+  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, overlap, s)
+         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, overlap, s)
+                             : launch_one<64, PS_KV_FP8>(a, p, overlap, s);
 }
 
 }  // namespace pskv

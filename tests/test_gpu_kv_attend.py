@@ -338,3 +338,35 @@ def test_tiles_scales_and_values_that_are_not_finite(kv, fmt, D):
     k[b.slots_of[0][300], 1] = math.nan
     b.cache.write(k, v, torch.arange(k.shape[0], device="cuda"))
     assert torch.isnan(b.run()[0][:, 4:]).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_back_to_back_calls(kv, fmt):
+    """Calls queued one behind the other, with the queries, cached tokens and the plan changed in between: each gives
+    what it gives alone."""
+    import torch
+    T = 60
+    spans = [(0, T, 700, 0)] + [(i, 1, 30 + i, 1) for i in range(T)]
+    b = Batch(kv, fmt, 2, 8, 128, spans, T, seed=23)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    n = 25
+    qs = torch.randn(n, *b.q.shape, device="cuda", generator=gen).to(b.q.dtype)
+    sl = b.slots_of[0][:200].contiguous()
+    ks = torch.randn(n, 200, 2, 128, device="cuda", generator=gen).to(b.q.dtype)
+    lens = [700 if i % 3 else 512 for i in range(n)]
+    q = torch.empty_like(b.q)
+
+    def step(i):
+        q.copy_(qs[i])
+        b.cache.write(ks[i], ks[i], sl)
+        b.plan.set(T, [(0, T, lens[i], 0, 0)] + b.spans[1:], b.ids)
+        return b.cache.attend(q, b.plan), b.cache.attend(q, b.plan, scale=0.05)
+
+    torch.cuda.synchronize()
+    got = [step(i) for i in range(n)]
+    b.cache.check()
+    for i in range(n):
+        torch.cuda.synchronize()
+        want = step(i)
+        torch.cuda.synchronize()
+        assert torch.equal(got[i][0], want[0]) and torch.equal(got[i][1], want[1])
