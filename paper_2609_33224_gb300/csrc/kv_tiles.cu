@@ -326,18 +326,21 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       const bool valid = in_tile < pc.nrows;
       const uint32_t query = pc.query0 + row / a.group, head = pc.head * a.group + row % a.group;
       {
-        // a warp's 32 rows, each row's chunks by neighbouring lanes
-        const int64_t mine = (int64_t)query * a.q_tok + (int64_t)head * a.q_head;
+        // a warp's 32 rows, each row's chunks by neighbouring lanes; where the rows are goes through their own places
+        // in shared memory
+        const int64_t mine = valid ? (int64_t)query * a.q_tok + (int64_t)head * a.q_head : INT64_MIN;
         constexpr int kLanes = D / 8, kAt = 32 / kLanes;
-        const uint32_t c = lane % kLanes;
+        const uint32_t c = lane % kLanes, rows_at = q_smem + t * C::kQ + (warp % 4) * (32 * 128);
+        asm volatile("st.shared.b64 [%0], %1;" ::"r"(rows_at + lane * 8), "l"(mine) : "memory");
+        __syncwarp();
         uint4 w[32 / kAt];
 #pragma unroll
         for (int i = 0; i < 32 / kAt; ++i) {
-          const int from = i * kAt + lane / kLanes;
-          const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, from);
-          const bool ok = __shfl_sync(0xFFFFFFFFu, (int)valid, from) != 0;
-          w[i] = ok ? __ldcg(reinterpret_cast<const uint4*>(a.q + at + 8 * c)) : make_uint4(0, 0, 0, 0);
+          int64_t at;
+          asm volatile("ld.shared.b64 %0, [%1];" : "=l"(at) : "r"(rows_at + (i * kAt + lane / kLanes) * 8) : "memory");
+          w[i] = at != INT64_MIN ? __ldcg(reinterpret_cast<const uint4*>(a.q + at + 8 * c)) : make_uint4(0, 0, 0, 0);
         }
+        __syncwarp();
         if (!here) {
           const uint32_t tmem = all_here();
           here = true;
@@ -441,43 +444,56 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       const bool direct = pc.part_row == kDirect;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const uint64_t at = (uint64_t)pc.part_row + t * (pc.split ? pc.split : C::kRows) + rank * 128 + r;
-      // The queries are used up: their rows' shared memory takes the warp's 32 rows, half of their columns at a
-      // time, from which whole rows are stored by neighbouring lanes.
-      const uint32_t stage = q_smem + t * C::kQ + (warp % 4) * (32 * D * 2);
+      // The queries are used up: their shared memory takes the warp's 32 rows, half of their columns at a time, from
+      // which whole rows are stored by neighbouring lanes.  A warp uses the place of its own queries alone, 4 KB in
+      // each panel: the tile's other warps may be at this or already at their next piece's queries.
+      auto stage = [&](uint32_t row_l) {
+        return q_smem + t * C::kQ + (warp % 4) * (32 * 128) +
+               (D == 128 ? (row_l / 16) * (128 * 128) + (row_l % 16) * 256 : row_l * 128);
+      };
       constexpr int kCols = D / 2, kChunks = kCols / 4;  // floats and 16-byte chunks of a row in one round
+      const uint32_t row0 = in_tile - lane, live = min(32u, max(row0, (uint32_t)pc.nrows) - row0);  // of the warp's rows
+      constexpr int kAt = 32 / kChunks;  // rows that the warp stores at once
+      const uint32_t my = lane / kChunks, mc = lane % kChunks;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
+        uint32_t o[kCols / 32][32];
 #pragma unroll
-        for (int c = 0; c < kCols / 16; ++c) {
-          uint32_t o[16];
-          tc_ld16(o, o_addr + half * kCols + 16 * c);
-          tc_wait_ld();
+        for (int c = 0; c < kCols / 32; ++c) tc_ld32(o[c], o_addr + half * kCols + 32 * c);
+        tc_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sts128(stage + lane * (kCols * 4) + (((4 * c + i) ^ (lane & 7u)) << 4), o[4 * i], o[4 * i + 1],
-                   o[4 * i + 2], o[4 * i + 3]);
-        }
+        for (int c = 0; c < kCols / 32; ++c)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            sts128(stage(lane) + (((8 * c + i) ^ (lane & 7u)) << 4), o[c][4 * i], o[c][4 * i + 1],
+                   o[c][4 * i + 2], o[c][4 * i + 3]);
         __syncwarp();
-        constexpr int kAt = 32 / kChunks;  // rows a round of the warp stores
-#pragma unroll 4
-        for (int i = 0; i < 32 / kAt; ++i) {
-          const uint32_t row_l = i * kAt + lane / kChunks, c = lane % kChunks;
-          uint32_t x[4];
+        auto staged = [&](uint32_t row_l, uint32_t (&x)[4]) {
           asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                       : "r"(stage + row_l * (kCols * 4) + ((c ^ (row_l & 7u)) << 4))
+                       : "r"(stage(row_l) + ((mc ^ (row_l & 7u)) << 4))
                        : "memory");
-          const bool ok = __shfl_sync(0xFFFFFFFFu, (int)valid, row_l) != 0;
-          if (direct) {
+        };
+        if (!direct) {
+          float* dst = a.part + (at - lane + my) * D + half * kCols + 4 * mc;
+#pragma unroll
+          for (int i = 0; i < 32 / kAt; ++i) {
+            uint32_t x[4];
+            staged(i * kAt + my, x);
+            if (i * kAt + my < live) *reinterpret_cast<uint4*>(dst + i * kAt * D) = make_uint4(x[0], x[1], x[2], x[3]);
+          }
+        } else {
+#pragma unroll 4
+          for (int i = 0; i < 32 / kAt; ++i) {
+            const uint32_t row_l = i * kAt + my;
+            uint32_t x[4];
+            staged(row_l, x);
             const float f = __shfl_sync(0xFFFFFFFFu, inv, row_l);
             const int64_t to = __shfl_sync(0xFFFFFFFFu, (int64_t)query * a.o_tok + (int64_t)head * a.o_head, row_l);
-            if (ok)
-              *reinterpret_cast<uint2*>(a.out + to + half * kCols + 4 * c) =
+            if (row_l < live)
+              *reinterpret_cast<uint2*>(a.out + to + half * kCols + 4 * mc) =
                   make_uint2(pack2<C::kFp16>(__uint_as_float(x[0]) * f, __uint_as_float(x[1]) * f),
                              pack2<C::kFp16>(__uint_as_float(x[2]) * f, __uint_as_float(x[3]) * f));
-          } else if (ok) {
-            const uint64_t to = at - lane + row_l;
-            *reinterpret_cast<uint4*>(a.part + to * D + half * kCols + 4 * c) = make_uint4(x[0], x[1], x[2], x[3]);
           }
         }
         __syncwarp();

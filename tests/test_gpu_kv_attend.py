@@ -370,3 +370,22 @@ def test_back_to_back_calls(kv, fmt):
         want = step(i)
         torch.cuda.synchronize()
         assert torch.equal(got[i][0], want[0]) and torch.equal(got[i][1], want[1])
+
+
+@pytest.mark.parametrize("fmt,D", [("bf16", 128), ("fp8", 128), ("fp16", 64)])
+def test_many_tiles_per_worker(kv, fmt, D):
+    """Each worker of the tile kernel has several pieces, whose queries and results pass through the same memory, its
+    warps at different pieces."""
+    import random
+    rng = random.Random(5)
+    spans, first = [], 0
+    for _ in range(30):
+        n = rng.choice([64, 64, 33, 50])
+        spans.append((first, n, rng.choice([300, 450, 640]), 0))
+        first += n
+    b = Batch(kv, fmt, 8, 8, D, spans, first, seed=31)
+    out, lse = b.run()
+    b.check(out, lse)
+    for _ in range(10):
+        import torch
+        assert torch.equal(b.run()[0], out)
