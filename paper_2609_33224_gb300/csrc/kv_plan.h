@@ -120,7 +120,7 @@ constexpr uint32_t kSplitSteps = 8;
 // side they take less time than one after the other.  Returns how many SMs the row kernel gets (all: one after the
 // other), by the times above, 3.3 ns of the GPU for a unit's start and end, the bytes at 6.2 TB/s, and what the
 // kernels take whatever their SMs: 6 and 4 us.  64 queries on 8192 shared tokens 55.7 -> 41.8 us, 9 groups under one
-// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 267 -> 260.
+// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 267 -> 260 (245 by now).
 constexpr double kUnitNs = 3.3, kBytesPerNs = 6200.0, kTileFixed = 6000.0, kRowFixed = 4000.0;
 inline int row_sms(const PlanShape& kv, double steps, double blocks, double units) {
   const double tile = step_ns(kv) * steps, work = block_ns(kv) * blocks + kUnitNs * units;

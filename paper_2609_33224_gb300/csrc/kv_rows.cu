@@ -10,9 +10,9 @@
 //
 // Bound by the bytes of the cache: 2 * D elements per key and head for 4 * D * 16 multiply-adds.  mma.sync
 // has the smallest tile (16 rows) and takes operands and results in registers; tcgen05's 128 rows would be
-// 1/8 or less filled here.  5 requests of 65536 to 131072 tokens, fp8, 8 heads, 128 columns, 1.05 GB: 165 us
-// = 6.4 TB/s, 94% of the measured copy; with 48 of the 152 SMs, where memory does not bind it, an fp8 block
-// takes 800 cycles of a scheduler (ALU pipe 63%), a third of them conversions.  As a warp joins nothing with
+// 1/8 or less filled here.  5 requests of 65536 to 131072 tokens, fp8, 8 heads, 128 columns, 1.05 GB: 159 us
+// = 6.6 TB/s, 97% of the measured copy; with 44 of the 152 SMs, where memory does not bind it, an fp8 block
+// takes 770 cycles of a scheduler (ALU pipe 54%).  As a warp joins nothing with
 // its CTA's other warps, a share's partial results cost 4 * D + 8 bytes a row.
 #include "kv_internal.cuh"
 

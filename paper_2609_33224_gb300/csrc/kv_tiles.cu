@@ -25,10 +25,10 @@
 // Bound by the tensor cores for full tiles: 4 * D multiply-adds a row and key, and, near that, the
 // exponentials: one per row and key.  Work is cut into equal shares per worker; each walks its pieces.
 // 9900 rows of 8 heads and 128 columns on 16384 keys, bf16, 665 GFLOP: 393 us = 1.69 PFLOP/s, 98% of what a
-// library product keeps up at the card's power limit (1.72; 1.94 in a burst); fp8, 2048 rows on 32768: 180 us
-// = 1.56 PFLOP/s (the ALU pipe, which the conversions share with the softmax, at half).  A step of 128 keys takes
-// 2400 cycles (2048 at the nominal rate); start and end of a worker take about 12000, the queries' and the
-// first keys' way 7000, the result's 5000.
+// library product keeps up at the card's power limit (1.72; 1.94 in a burst); fp8, 2048 rows on 32768, 282
+// GFLOP: 236 us on 104 SMs, the same rate an SM.  A step of 128 keys takes
+// 2400 cycles (2048 at the nominal rate); start and end of a worker take about 10000: the way of the queries and
+// the first keys, the pipeline's filling, the result's way out.
 #include "kv_internal.cuh"
 
 namespace pskv {
@@ -49,11 +49,13 @@ struct Cfg {
   static constexpr int kRaws = kFp8 ? 4 : 0;
   static constexpr int kSlots = kFp8 ? 6 : 10;
   static constexpr int kWarps = kFp8 ? 16 : 12;
-  static constexpr int kRegSoft = kFp8 ? 192 : 208, kRegRest = kFp8 ? 64 : 88;
+  static constexpr int kRegSoft = kFp8 ? 176 : 200, kRegRest = kFp8 ? 80 : 104;
   static constexpr int kSmem = 2 * kQ + kSlots * kSlot + kRaws * kRaw + 1024;  // 1024: alignment
   static_assert(kSlot == kKeys * D * 2 && kCols == 64, "a slot holds keys or values");
+  // registers a thread at launch (multiples of 8): the split hands out no more than that
+  static_assert(256 * kRegSoft + (kWarps * 32 - 256) * kRegRest <= 65536 / (kWarps * 32) / 8 * 8 * (kWarps * 32),
+                "register split");
 };
-static_assert(192 * 256 + 64 * 256 <= 65536 && 208 * 256 + 88 * 128 <= 384 * 168, "register split");
 
 struct Bars {
   uint64_t full[10], empty[10];  // operand ring
@@ -228,11 +230,12 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, ui
 
 // fp8: the codes of `n` chunks of a row, at `src(c)`, as bf16 with the row's scale applied, to `dst(2 c)` and
 // `dst(2 c + 1)`.
-// value = code * 2^120 * 2^(e - 127); the second factor as a bf16, a NaN for a row with a NaN.
+// Codes to fp16 (one instruction for two), to floats, times the scale, to bf16: two of the ALU pipe's instructions for
+// two elements, where taking the codes' bits apart needs four (256 queries on 32768 tokens: 253 -> 245 us).  The mark of a row with a NaN gives an infinity, whose
+// product with such a row's codes, zeros, is a NaN.
 template <int N, class Src, class Dst>
 __device__ __forceinline__ void to_bf16(uint32_t e, bool live, Src src, Dst dst) {
-  const uint32_t f1 = e == (uint32_t)kExpNan ? 0x7FC0u : e << 7;
-  const uint32_t f = f1 | (f1 << 16);
+  const float f = __uint_as_float(e << 23);
 #pragma unroll 2
   for (int c = 0; c < N; ++c) {
     uint32_t w[4] = {0, 0, 0, 0}, o[8];
@@ -243,11 +246,14 @@ __device__ __forceinline__ void to_bf16(uint32_t e, bool live, Src src, Dst dst)
                    : "memory");
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      o[2 * i] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x1404));
-      o[2 * i + 1] = e4m3_to_bf16x2(__byte_perm(w[i], 0, 0x3424));
-    }
+      uint32_t h[2];
+      e4m3x4_to_f16x2(w[i], h[0], h[1]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o[i]) : "r"(o[i]), "r"(f));
+      for (int k = 0; k < 2; ++k) {
+        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
+        o[2 * i + k] = pack2<false>(x.x * f, x.y * f);
+      }
+    }
     sts128(dst(2 * c), o[0], o[1], o[2], o[3]);
     sts128(dst(2 * c + 1), o[4], o[5], o[6], o[7]);
   }
