@@ -26,7 +26,7 @@
 // exponentials: one per row and key.  Work is cut into equal shares per worker; each walks its pieces.
 // 9900 rows of 8 heads and 128 columns on 16384 keys, bf16, 665 GFLOP: 393 us = 1.69 PFLOP/s, 98% of what a
 // library product keeps up at the card's power limit (1.72; 1.94 in a burst); fp8, 2048 rows on 32768, 282
-// GFLOP: 236 us on 104 SMs, the same rate an SM.  A step of 128 keys takes
+// GFLOP: 236 us on 108 SMs, the same rate an SM.  A step of 128 keys takes
 // 2400 cycles (2048 at the nominal rate); start and end of a worker take about 10000: the way of the queries and
 // the first keys, the pipeline's filling, the result's way out.
 #include "kv_internal.cuh"
