@@ -14,6 +14,8 @@
 // = 6.6 TB/s, 97% of the measured copy; with 44 of the 152 SMs, where memory does not bind it, an fp8 block
 // takes 770 cycles of a scheduler (ALU pipe 54%).  As a warp joins nothing with
 // its CTA's other warps, a share's partial results cost 4 * D + 8 bytes a row.
+#include <type_traits>
+
 #include "kv_internal.cuh"
 
 namespace pskv {
@@ -75,6 +77,16 @@ template <int I>
 __device__ __forceinline__ float exp_byte(uint32_t w) {
   return __uint_as_float((I == 3 ? w >> 1 : w << (23 - 8 * I)) & 0x7F800000u);
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -100,6 +112,8 @@ __device__ __forceinline__ float value16(uint16_t b) {
   if (FP16) return __half2float(__ushort_as_half(b));
   return __uint_as_float((uint32_t)b << 16);
 }
+
+enum Step { kGoOn, kTooFar, kGaveUp };  // what became of a block
 
 template <int D, int FMT>
 __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
@@ -228,7 +242,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         }
       }
     }
-    float v_ref = 0.0f, v_inv = 0.0f;  // fp8: the scale that the output so far is relative to; 2^5 over it
+    // fp8: the scale that the output so far is relative to, 2^5 over it, and the first such scale
+    float v_ref = 0.0f, v_inv = 0.0f, v_first = 0.0f;
     // the last key each of the two rows sees, and the last that all rows of the tile see
     const int32_t last = (int32_t)pc.end - 1;
     const int32_t lim_a = min(last, pc.climit + (int32_t)ta), lim_b = min(last, pc.climit + (int32_t)tb);
@@ -239,20 +254,22 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
     for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
     float ma = -INFINITY, mb = -INFINITY, la = 0.0f, lb = 0.0f;
 
-    for (uint32_t bi = 0; bi < pc.nblocks; ++bi) {
-      const uint32_t rec = ring + st * kStage;
-      if (!mbar_wait_warp(bar + st * 8, phase)) {
-        if (lane == 0) atomicOr_system(a.err, kErrWait);
-        while (--in_flight) {  // the copies behind it write this warp's memory: they are waited for too
-          if (++st == kStages) {
-            st = 0;
-            phase ^= 1u;
-          }
-          mbar_wait(bar + st * 8, phase);
+    auto give_up = [&]() {
+      if (lane == 0) atomicOr_system(a.err, kErrWait);
+      while (--in_flight) {  // the copies behind it write this warp's memory: they are waited for too
+        if (++st == kStages) {
+          st = 0;
+          phase ^= 1u;
         }
-        if (!waited) wait_for_last();
-        return;
+        mbar_wait(bar + st * 8, phase);
       }
+      if (!waited) wait_for_last();
+    };
+    // One block.  Apart (fp8): with value scales that lie far apart.
+    auto step = [&](auto apart, const uint32_t bi) {
+      constexpr bool kApart = decltype(apart)::value;
+      const uint32_t rec = ring + st * kStage;
+      if (!mbar_wait_warp(bar + st * 8, phase)) return kGaveUp;
       // ---- scores
       float s[2][4];
 #pragma unroll
@@ -290,37 +307,73 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         s[1][1] = s[1][1] * qa_scale * k3;
         s[1][2] = s[1][2] * qb_scale * k2;
         s[1][3] = s[1][3] * qb_scale * k3;
-        // The values' scales go into the probabilities, relative to the largest scale so far and times 2^5: with
-        // probabilities of at most 2^8 (below), their products stay below 2^15, and what fp16 holds with fewer
-        // bits is below 2^-27 of what it could hold.
+        // The values' scales go into the probabilities, relative to a reference near the largest and times 2^5: with
+        // probabilities of at most 2^8 (below) and scales of at most twice the reference, their products stay at or
+        // below 2^14.  Scales of at least 2^-10 of it leave a product its 11 bits down to probabilities of 2^-9, and
+        // below that cost at most 2^-20 of the key's own value.  A key further below, beside large rows that a query
+        // does not see or hardly weighs, would lose its bits: from such a block on, the piece's output is relative to
+        // nothing, and the products are of values with their scales, both factors in bf16, whose exponents reach as
+        // far as a float's.
         vs[0] = exp_byte<0>(vx);
         vs[1] = exp_byte<1>(vx);
         vs[2] = exp_byte<2>(vx);
         vs[3] = exp_byte<3>(vx);
-        float top = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        if (top > 2.0f * v_ref) {  // the same for the whole warp; also where a row is marked or past the end
-          const int32_t here = (int32_t)pc.key0 + (int32_t)(bi * kBlock) + (int32_t)t4 * 2;
-          top = 0x1p-110f;
+        if constexpr (kApart) {  // the mark of a NaN stays with the probability
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (vs[i] < 0x1p120f && here + (i & 1) + (i >> 1) * 8 <= last) top = fmaxf(top, vs[i]);
-          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-          if (top > 2.0f * v_ref) {
-            const uint32_t inverse = (254u << 23) - __float_as_uint(top);  // of a power of two
-            const float f = v_ref * __uint_as_float(inverse);
-            v_ref = top;
-            v_inv = __uint_as_float(inverse + (5u << 23));
+          for (int i = 0; i < 4; ++i) vs[i] = vs[i] < 0x1p120f ? 1.0f : vs[i];
+        } else {
+          float rel[4];
 #pragma unroll
-            for (int j = 0; j < kTiles; ++j)
+          for (int i = 0; i < 4; ++i) rel[i] = vs[i] * v_inv;
+          // the same for the whole warp; also where a row is marked, zero or past the end
+          if (__any_sync(0xFFFFFFFFu, max3(fmaxf(rel[0], rel[1]), rel[2], rel[3]) > 0x1p6f ||
+                                          min3(fminf(rel[0], rel[1]), rel[2], rel[3]) < 0x1p-5f)) {
+            const int32_t here = (int32_t)pc.key0 + (int32_t)(bi * kBlock);
+            // Rows of zeros have the smallest scale (or, never written, none) and weigh nothing.
+            uint32_t zeros = 0;  // bit 2 * key
+            if (__any_sync(0xFFFFFFFFu, min3(fminf(vs[0], vs[1]), vs[2], vs[3]) <= 0x1p-110f)) {
+              bool any = false;
+#pragma unroll 1
+              for (uint32_t c = lane & 1; c < D / 16; c += 2) {
+                const uint4 w = lds128(rec + kHalf + offset8v(lane >> 1, c));
+                any |= ((w.x | w.y | w.z | w.w) & 0x7F7F7F7Fu) != 0;
+              }
+              const uint32_t some = __ballot_sync(0xFFFFFFFFu, any);
+              zeros = ~(some | (some >> 1));
+            }
+            float top = 0.0f, low = INFINITY;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t key = t4 * 2 + (i & 1) + (i >> 1) * 8;
+              if (vs[i] < 0x1p120f && here + (int32_t)key <= last && !((zeros >> (2 * key)) & 1u)) {
+                top = fmaxf(top, vs[i]);
+                low = fminf(low, vs[i]);
+              }
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, 2));
+            const float ref = top > 2.0f * v_ref ? top : v_ref;
+            // (the second: the output so far keeps its bits when it is brought to another reference)
+            if (low < 0x1p-10f * ref || (v_first > 0.0f && ref * 0x1p-60f > v_first)) return kTooFar;
+            if (ref > v_ref) {
+              const uint32_t inverse = (254u << 23) - __float_as_uint(ref);  // of a power of two
+              const float f = v_ref * __uint_as_float(inverse);
+              v_ref = ref;
+              v_inv = __uint_as_float(inverse + (5u << 23));
+              if (v_first == 0.0f) v_first = ref;
+#pragma unroll
+              for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rel[i] = vs[i] * v_inv;
           }
-        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) vs[i] *= v_inv;
+          for (int i = 0; i < 4; ++i) vs[i] = rel[i];
+        }
       } else {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
@@ -411,25 +464,42 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           }
       }
       // ---- product with the values
-      constexpr bool kHalfP = kFp16 || kFp8;
-      const uint32_t pf[4] = {pack2<kHalfP>(s[0][0], s[0][1]), pack2<kHalfP>(s[0][2], s[0][3]),
-                              pack2<kHalfP>(s[1][0], s[1][1]), pack2<kHalfP>(s[1][2], s[1][3])};
       if constexpr (kFp8) {
+        const uint32_t pf[4] = {pack2<!kApart>(s[0][0], s[0][1]), pack2<!kApart>(s[0][2], s[0][3]),
+                                pack2<!kApart>(s[1][0], s[1][1]), pack2<!kApart>(s[1][2], s[1][3])};
+        if constexpr (kApart) {  // a marked row's codes are zeros, and stay so
+          const uint32_t vx = lds32(rec + 2 * kHalf + kBlock + t4 * 4);
+          vs[0] = exp_byte<0>(vx);
+          vs[1] = exp_byte<1>(vx);
+          vs[2] = exp_byte<2>(vx);
+          vs[3] = exp_byte<3>(vx);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) vs[i] = vs[i] < 0x1p120f ? vs[i] : 0.0f;
+        }
+        // two codes as the operand that the probabilities' type asks for
+        auto operand = [](uint32_t h, float f0, float f1) {
+          if (!kApart) return h;
+          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h));
+          return pack2<false>(x.x * f0, x.y * f1);
+        };
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
           uint32_t r[4];
           ldsm4<true>(r, (rec + v_at + (c / 4) * (kBlock * 64)) ^ ((c % 4) << 4));
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            // a chunk's 16 columns: tile 2c has the even ones, tile 2c + 1 the odd ones
+            // a chunk's 16 columns: tile 2c has the even ones, tile 2c + 1 the odd ones; the halves of a register are the
+            // keys of vs[0] and vs[1], or of vs[2] and vs[3]
             uint32_t even0, odd0, even1, odd1;
             e4m3x4_to_f16x2(__byte_perm(r[i], 0, 0x3120), even0, odd0);
             e4m3x4_to_f16x2(__byte_perm(r[i + 1], 0, 0x3120), even1, odd1);
-            mma16816<true>(acc[2 * c + i], pf, even0, even1);
-            mma16816<true>(acc[2 * c + i + 1], pf, odd0, odd1);
+            mma16816<!kApart>(acc[2 * c + i], pf, operand(even0, vs[0], vs[1]), operand(even1, vs[2], vs[3]));
+            mma16816<!kApart>(acc[2 * c + i + 1], pf, operand(odd0, vs[0], vs[1]), operand(odd1, vs[2], vs[3]));
           }
         }
       } else {
+        const uint32_t pf[4] = {pack2<kFp16>(s[0][0], s[0][1]), pack2<kFp16>(s[0][2], s[0][3]),
+                                pack2<kFp16>(s[1][0], s[1][1]), pack2<kFp16>(s[1][2], s[1][3])};
 #pragma unroll
         for (int j = 0; j < kTiles; j += 2) {
           uint32_t r[4];
@@ -473,16 +543,28 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         phase ^= 1u;
       }
       issue();
-    }
-
-    // ---- the piece's result
+      return kGoOn;
+    };
+    uint32_t bi = 0;
+    Step did = kGoOn;
+    for (; bi < pc.nblocks; ++bi)
+      if ((did = step(std::false_type(), bi)) != kGoOn) break;
     if constexpr (kFp8) {
       const float f = v_ref * 0x1p-5f;
 #pragma unroll
       for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] *= f;
+      if (did == kTooFar)
+        for (; bi < pc.nblocks; ++bi)
+          if ((did = step(std::true_type(), bi)) != kGoOn) break;
     }
+    if (did == kGaveUp) {
+      give_up();
+      return;
+    }
+
+    // ---- the piece's result
     la += __shfl_xor_sync(0xFFFFFFFFu, la, 1);
     lb += __shfl_xor_sync(0xFFFFFFFFu, lb, 1);
     la += __shfl_xor_sync(0xFFFFFFFFu, la, 2);
