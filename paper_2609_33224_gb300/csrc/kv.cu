@@ -189,7 +189,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
 
   pskv::Layout o;
   pskv::lay_out(pskv::PlanShape{kv->sms, kv->D, kv->fmt, kv->heads, pl->group}, T, spans, n_spans, &o);
-  if (o.part_rows >= 0xFFFFFF00ull || o.groups.size() >= 0xFFFFFF00ull)
+  if (o.part_rows >= 0xFFFFFF00ull || o.groups.size() >= 0xFFFFFF00ull || pskv::join_rows(o) >= 0xFFFFFF00ull)
     return fail(kv, PS_ERR_INVALID, "the batch is too large for one plan");
 
   std::vector<std::pair<const void*, size_t>> parts;
@@ -232,6 +232,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.segs = reinterpret_cast<const pskv::JoinSeg*>(b.dev + sg);
   d.folds = reinterpret_cast<const pskv::Fold*>(b.dev + fd);
   d.njoin = (uint32_t)o.join.size();
+  d.join_stride = o.join_stride;
   d.max_parts = o.max_parts;
   d.blocks = reinterpret_cast<const uint32_t*>(b.dev + bl);
   pl->dev = d;

@@ -58,7 +58,7 @@ struct PlanDev {
   const JoinEntry* join;
   const JoinSeg* segs;
   const Fold* folds;
-  uint32_t njoin;
+  uint32_t njoin, join_stride;  // entries, and rows that each gets
   uint32_t max_parts;
   const uint32_t* blocks;
 };

@@ -22,9 +22,9 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t row = kWide ? blockIdx.x : blockIdx.x * 8 + warp;
   // What there is to join is the plan's; the parts are the kernels' before this one.
-  const bool live = row < p.njoin * a.group;  // kWide: the same for the whole CTA
-  const JoinEntry en = live ? p.join[row / a.group] : JoinEntry{};
-  const uint32_t gi = row % a.group;
+  const bool live = row < p.njoin * p.join_stride;  // < 2^32; kWide: the same for the whole CTA
+  const JoinEntry en = live ? p.join[row / p.join_stride] : JoinEntry{};
+  const uint32_t gi = row % p.join_stride;
   JoinSeg ahead_seg{0, 0, 0};
   if (lane < min(32u, en.nsegs)) ahead_seg = p.segs[en.seg0 + lane];
   let_next_start();  // the next call's first kernel, which waits for this one
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
 
 template <int D, bool FP16>
 cudaError_t go(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
-  const uint32_t rows = p.njoin * a.group;
+  const uint32_t rows = p.njoin * p.join_stride;
   // A CTA a row where there are few: 64 rows of 64 parts 7 us less than a warp a row; 2048 rows of 38 parts 3 us more.
   if (p.max_parts > 4 && rows <= 1024)
     return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, true, s, a, p);

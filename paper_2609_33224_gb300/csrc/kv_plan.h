@@ -51,7 +51,8 @@ constexpr uint32_t kDirect = 0xFFFFFFFFu;
 constexpr int32_t kNoLimit = 0x3FFFFFFF;
 
 // What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments
-// segs[seg0] ..: the i-th row's are the partial rows row + i + k * stride, k < nparts.
+// segs[seg0] ..: the i-th row's are the partial rows row + i + k * stride, k < nparts.  The join kernel gives every entry
+// as many rows as the largest has (Layout::join_stride).
 struct JoinEntry {
   uint32_t query;
   uint16_t head0, count;
@@ -172,8 +173,12 @@ struct Layout {
   std::vector<Fold> folds;
   uint64_t part_rows = 0;
   uint32_t max_parts = 1;
+  uint32_t join_stride = 0;  // the largest entry's count
   int row_sms = 0;  // SMs of the row kernel; fewer than all: beside the tile kernel
 };
+
+// Rows of the join kernel's launch.
+inline uint64_t join_rows(const Layout& o) { return (uint64_t)o.join.size() * o.join_stride; }
 
 // A unit of the layer and group that come last.
 inline Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t from, int64_t end, int step, int32_t climit,
@@ -407,33 +412,47 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   }
 
   // The rows of a query and head that have something to join, or no key at all; cut where one of the query's
-  // layers begins a new tile.
-  for (uint32_t t = 0; t < T; ++t) {
-    const uint32_t* ls = o.tok_layer.data() + o.tok_off[t];
-    const uint32_t nl = o.tok_off[t + 1] - o.tok_off[t];
-    for (uint32_t i = 0, n; i < g; i += n) {
-      n = g - i;
-      for (uint32_t l = 0; l < nl; ++l) {
-        const Layer& ly = o.layers[ls[l]];
-        n = std::min(n, ly.tile_rows - ((t - ly.query0) * g + i) % ly.tile_rows);
-      }
-      for (uint32_t h = 0; h < H; ++h) {
-        const uint32_t seg0 = (uint32_t)o.segs.size();
-        bool direct = false;
+  // layers begins a new tile, and at `most` rows.
+  const size_t fold_segs = o.segs.size();
+  auto join = [&](uint32_t most) {
+    o.segs.resize(fold_segs);
+    o.join.clear();
+    o.join_stride = 0;
+    for (uint32_t t = 0; t < T; ++t) {
+      const uint32_t* ls = o.tok_layer.data() + o.tok_off[t];
+      const uint32_t nl = o.tok_off[t + 1] - o.tok_off[t];
+      for (uint32_t i = 0, n; i < g; i += n) {
+        n = std::min(g - i, most);
         for (uint32_t l = 0; l < nl; ++l) {
           const Layer& ly = o.layers[ls[l]];
-          const uint32_t r = (t - ly.query0) * g + i;
-          const Group& gr = o.groups[ly.group0 + r / ly.tile_rows * H + h];
-          direct = direct || gr.part_row == kDirect;
-          if (gr.nparts) o.segs.push_back(JoinSeg{gr.part_row + r % ly.tile_rows, ly.tile_rows, gr.nparts});
+          n = std::min(n, ly.tile_rows - ((t - ly.query0) * g + i) % ly.tile_rows);
         }
-        if (direct) {
-          o.segs.resize(seg0);
-          continue;
+        for (uint32_t h = 0; h < H; ++h) {
+          const uint32_t seg0 = (uint32_t)o.segs.size();
+          bool direct = false;
+          for (uint32_t l = 0; l < nl; ++l) {
+            const Layer& ly = o.layers[ls[l]];
+            const uint32_t r = (t - ly.query0) * g + i;
+            const Group& gr = o.groups[ly.group0 + r / ly.tile_rows * H + h];
+            direct = direct || gr.part_row == kDirect;
+            if (gr.nparts) o.segs.push_back(JoinSeg{gr.part_row + r % ly.tile_rows, ly.tile_rows, gr.nparts});
+          }
+          if (direct) {
+            o.segs.resize(seg0);
+            continue;
+          }
+          o.join.push_back(JoinEntry{t, (uint16_t)(h * g + i), (uint16_t)n, seg0, (uint32_t)o.segs.size() - seg0});
+          o.join_stride = std::max(o.join_stride, n);
         }
-        o.join.push_back(JoinEntry{t, (uint16_t)(h * g + i), (uint16_t)n, seg0, (uint32_t)o.segs.size() - seg0});
       }
     }
+  };
+  join(g);
+  // A few entries of many rows among many that the row kernel's tiles cut: rows without work are not worth their place.
+  if (o.join_stride > (uint32_t)kSmallRows) {
+    uint64_t cut = 0;
+    for (const JoinEntry& e : o.join) cut += (e.count + kSmallRows - 1) / kSmallRows;
+    if (cut * kSmallRows < join_rows(o)) join(kSmallRows);
   }
 }
 
