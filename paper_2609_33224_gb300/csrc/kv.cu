@@ -173,6 +173,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   if (n_spans > pl->max_spans) return fail(kv, PS_ERR_INVALID, "more spans than max_spans");
   if (n_blocks > pl->max_blocks) return fail(kv, PS_ERR_INVALID, "more block ids than max_blocks");
   if ((n_spans && !spans) || (n_blocks && !blocks)) return fail(kv, PS_ERR_INVALID, "spans or blocks is NULL");
+  uint64_t seen = 0;  // (query, layer) pairs of the layout: a span may become two layers
   for (uint32_t i = 0; i < n_spans; ++i) {
     const ps_kv_span& s = spans[i];
     if (s.causal > 1) return fail(kv, PS_ERR_INVALID, "a span's causal must be 0 or 1");
@@ -182,14 +183,17 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
     const uint64_t nb = (s.length + pskv::kBlock - 1) / pskv::kBlock;
     if (s.first_block > n_blocks || nb > n_blocks - s.first_block)
       return fail(kv, PS_ERR_INVALID, "a span's blocks must lie inside the block array");
+    if (s.length) seen += 2ull * s.num_queries;
   }
+  if (seen >= 0xFFFFFF00ull) return fail(kv, PS_ERR_INVALID, "the batch is too large for one plan");
   uint32_t top = 0;
   for (uint64_t i = 0; i < n_blocks; ++i) top = std::max(top, blocks[i]);
   if (n_blocks && top >= kv->blocks) return fail(kv, PS_ERR_INVALID, "a block id lies outside the cache");
 
   pskv::Layout o;
   pskv::lay_out(pskv::PlanShape{kv->sms, kv->D, kv->fmt, kv->heads, pl->group}, T, spans, n_spans, &o);
-  if (o.part_rows >= 0xFFFFFF00ull || o.groups.size() >= 0xFFFFFF00ull || pskv::join_rows(o) >= 0xFFFFFF00ull)
+  if (o.part_rows >= 0xFFFFFF00ull || o.groups.size() >= 0xFFFFFF00ull || o.segs.size() >= 0xFFFFFF00ull ||
+      pskv::join_rows(o) >= 0xFFFFFF00ull)
     return fail(kv, PS_ERR_INVALID, "the batch is too large for one plan");
 
   std::vector<std::pair<const void*, size_t>> parts;
