@@ -19,6 +19,10 @@
  *     cache, or by ps_kv_check.
  *   - Tensors have their head_dim elements next to each other; token and head strides are free, in
  *     elements.  Base addresses are 16-byte aligned and strides multiples of 16 bytes.
+ *   - Calls may be captured into a CUDA graph.  The graph keeps the cache's blocks and the plan's arrays that its calls
+ *     read, also after ps_kv_destroy and ps_kv_plan_destroy; they are freed by the first ps_kv_create,
+ *     ps_kv_plan_create, ps_kv_plan_destroy or ps_kv_destroy after the graph and its executable graphs are gone.  The
+ *     caller's tensors and the workspace are the caller's to keep.
  *   - One cache or plan must not be used from two threads at once.
  */
 #ifndef PACKSERVE_KV_H
@@ -130,10 +134,12 @@ PS_API ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, 
  * The paper has no counterpart. */
 PS_API const char* ps_kv_last_error(const ps_kv* kv);
 
-/* Release a plan: waits for the calls that read it.  NULL is accepted.  The paper has no counterpart. */
+/* Release a plan: waits for the calls that read it, and leaves its arrays to the graphs that captured one.  NULL is
+ * accepted.  The paper has no counterpart. */
 PS_API void ps_kv_plan_destroy(ps_kv_plan* plan);
 
-/* Release a cache and its memory: waits for the device.  NULL is accepted.  The paper has no counterpart. */
+/* Release a cache and its memory (to the graphs that captured a call on it, where there are any): waits for the
+ * device.  NULL is accepted.  The paper has no counterpart. */
 PS_API void ps_kv_destroy(ps_kv* kv);
 
 #ifdef __cplusplus

@@ -1,6 +1,7 @@
 // C entry points of the serving operators (packserve_kv.h): the block cache, and the plans that lay a
 // batch's spans out for the attention kernels.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -9,12 +10,28 @@
 
 #include "kv_internal.cuh"
 
+namespace {
+
+// Memory of a cache or a plan.  A CUDA graph that has captured a call on it keeps it after its owner is gone: each such
+// graph holds a reference.
+struct Memory {
+  std::atomic<uint32_t> refs{1};
+  int device = 0;
+  uint8_t* dev = nullptr;
+  void* host = nullptr;             // pinned
+  unsigned long long capture = 0;   // the last one whose graph has a reference
+  Memory* next = nullptr;
+};
+
+}  // namespace
+
 struct ps_kv {
   int device = 0;
   int sms = 0;
   uint32_t heads = 0, D = 0;
   int fmt = 0;
   uint64_t blocks = 0;
+  Memory* mem = nullptr;  // the blocks, and the error word
   uint8_t* pool = nullptr;
   uint32_t* err_host = nullptr;  // mapped: kernels set bits, the next call reads them
   uint32_t* err_dev = nullptr;
@@ -27,6 +44,7 @@ struct ps_kv_plan {
   uint64_t max_blocks = 0;
   // Two buffers take turns, so that a set can prepare the next step while calls still read the last one.
   struct Buffer {
+    Memory* mem = nullptr;
     uint8_t* dev = nullptr;
     uint8_t* host = nullptr;
     size_t cap = 0;
@@ -76,6 +94,55 @@ struct OnDevice {
   }
   ~OnDevice() {
     if (was >= 0) cudaSetDevice(was);
+  }
+};
+
+// Memory that nothing refers to any more.  It is freed by a later call: the one that gives up a graph's reference
+// may not call CUDA.
+std::atomic<Memory*> unused{nullptr};
+
+void drop(void* p) {
+  Memory* m = static_cast<Memory*>(p);
+  if (m->refs.fetch_sub(1, std::memory_order_acq_rel) != 1) return;
+  m->next = unused.load(std::memory_order_relaxed);
+  while (!unused.compare_exchange_weak(m->next, m, std::memory_order_release, std::memory_order_relaxed)) {
+  }
+}
+
+void free_unused() {
+  Memory* m = unused.exchange(nullptr, std::memory_order_acquire);
+  while (m) {
+    Memory* next = m->next;
+    OnDevice on(m->device);
+    if (m->dev) cudaFree(m->dev);
+    if (m->host) cudaFreeHost(m->host);
+    delete m;
+    m = next;
+  }
+}
+
+// The graph that a call on the stream is captured into (0: none), and a reference to memory from it.
+struct Capture {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  cudaGraph_t graph = nullptr;
+  cudaError_t look(cudaStream_t s) { return cudaStreamGetCaptureInfo(s, &status, &id, &graph, nullptr, nullptr, nullptr); }
+  bool on() const { return status != cudaStreamCaptureStatusNone; }
+  cudaError_t keep(Memory* m) const {
+    if (status != cudaStreamCaptureStatusActive || m->capture == id) return cudaSuccess;
+    cudaUserObject_t o;
+    m->refs.fetch_add(1, std::memory_order_relaxed);
+    cudaError_t e = cudaUserObjectCreate(&o, m, drop, 1, cudaUserObjectNoDestructorSync);
+    if (e != cudaSuccess) {
+      drop(m);
+      return e;
+    }
+    e = cudaGraphRetainUserObject(graph, o, 1, cudaGraphUserObjectMove);
+    if (e != cudaSuccess)
+      cudaUserObjectRelease(o, 1);  // drops the reference
+    else
+      m->capture = id;
+    return e;
   }
 };
 
@@ -140,8 +207,7 @@ void release(ps_kv_plan::Buffer& b) {
   else if (b.in_use)
     cudaEventSynchronize(b.used);
   if (b.used) cudaEventDestroy(b.used);
-  if (b.dev) cudaFree(b.dev);
-  if (b.host) cudaFreeHost(b.host);
+  if (b.mem) drop(b.mem);
   b = ps_kv_plan::Buffer{};
 }
 
@@ -149,18 +215,25 @@ ps_status grow(ps_kv* kv, ps_kv_plan::Buffer& b, size_t need) {
   if (need <= b.cap) return PS_OK;
   size_t cap = std::max<size_t>(b.cap * 2, 1 << 16);
   while (cap < need) cap *= 2;
-  if (b.dev) cudaFree(b.dev);
-  if (b.host) cudaFreeHost(b.host);
+  if (b.mem) drop(b.mem);
+  b.mem = nullptr;
   b.dev = b.host = nullptr;
   b.cap = 0;
-  cudaError_t e = cudaMalloc(&b.dev, cap);
-  if (e == cudaSuccess) e = cudaHostAlloc(&b.host, cap, cudaHostAllocDefault);
+  free_unused();
+  Memory* m = new (std::nothrow) Memory;
+  if (!m) return fail(kv, PS_ERR_OOM, "no host memory for a plan");
+  m->device = kv->device;
+  cudaError_t e = cudaMalloc(&m->dev, cap);
+  if (e == cudaSuccess) e = cudaHostAlloc(&m->host, cap, cudaHostAllocDefault);
   if (e != cudaSuccess) {
     cudaGetLastError();
-    if (b.dev) cudaFree(b.dev);
-    b.dev = b.host = nullptr;
+    drop(m);
+    free_unused();
     return fail(kv, e == cudaErrorMemoryAllocation ? PS_ERR_OOM : PS_ERR_CUDA, "plan buffers could not be allocated");
   }
+  b.mem = m;
+  b.dev = m->dev;
+  b.host = static_cast<uint8_t*>(m->host);
   b.cap = cap;
   return PS_OK;
 }
@@ -270,8 +343,12 @@ ps_status ps_kv_create(const ps_kv_config* cfg, ps_kv** out) {
   }
   if (cfg->device < 0 || cfg->device >= count) return PS_ERR_INVALID;
   ps_kv* kv = new (std::nothrow) ps_kv;
-  if (!kv) return PS_ERR_OOM;
-  kv->device = cfg->device;
+  if (kv) kv->mem = new (std::nothrow) Memory;
+  if (!kv || !kv->mem) {
+    delete kv;
+    return PS_ERR_OOM;
+  }
+  kv->device = kv->mem->device = cfg->device;
   kv->heads = cfg->kv_heads;
   kv->D = cfg->head_dim;
   kv->fmt = cfg->format;
@@ -279,11 +356,14 @@ ps_status ps_kv_create(const ps_kv_config* cfg, ps_kv** out) {
   OnDevice on(kv->device);
   const uint64_t bytes = kv->blocks * kv->heads * (uint64_t)pskv::record_bytes((int)kv->D, kv->fmt);
   void* dev = nullptr;
+  free_unused();
   cudaError_t e = cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, kv->device);
-  if (e == cudaSuccess) e = cudaMalloc(&kv->pool, bytes);
-  if (e == cudaSuccess) e = cudaMemset(kv->pool, 0, bytes);
-  if (e == cudaSuccess) e = cudaHostAlloc(&kv->err_host, 64, cudaHostAllocMapped);
+  if (e == cudaSuccess) e = cudaMalloc(&kv->mem->dev, bytes);
+  if (e == cudaSuccess) e = cudaMemset(kv->mem->dev, 0, bytes);
+  if (e == cudaSuccess) e = cudaHostAlloc(&kv->mem->host, 64, cudaHostAllocMapped);
+  kv->pool = kv->mem->dev;
   if (e == cudaSuccess) {
+    kv->err_host = static_cast<uint32_t*>(kv->mem->host);
     std::memset(kv->err_host, 0, 64);
     e = cudaHostGetDevicePointer(&dev, kv->err_host, 0);
   }
@@ -309,6 +389,9 @@ ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const
   st = store_args(kv, k, v, slots, n, &a);
   if (st != PS_OK || n == 0) return st;
   OnDevice on(kv->device);
+  Capture cap;
+  KV_CUDA(kv, cap.look(static_cast<cudaStream_t>(stream)));
+  KV_CUDA(kv, cap.keep(kv->mem));
   KV_CUDA(kv, pskv::launch_write((int)kv->D, kv->fmt, k->type, a, kv->sms, static_cast<cudaStream_t>(stream)));
   return PS_OK;
 }
@@ -322,6 +405,9 @@ ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_ro
   st = store_args(kv, k, v, slots, n, &a);
   if (st != PS_OK || n == 0) return st;
   OnDevice on(kv->device);
+  Capture cap;
+  KV_CUDA(kv, cap.look(static_cast<cudaStream_t>(stream)));
+  KV_CUDA(kv, cap.keep(kv->mem));
   KV_CUDA(kv, pskv::launch_read((int)kv->D, kv->fmt, k->type, a, kv->sms, static_cast<cudaStream_t>(stream)));
   return PS_OK;
 }
@@ -410,13 +496,15 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   if (T == 0) return PS_OK;
   OnDevice on(kv->device);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-  KV_CUDA(kv, cudaStreamIsCapturing(s, &cap));
+  Capture cap;
+  KV_CUDA(kv, cap.look(s));
   ps_kv_plan::Buffer& b = pl->buf[pl->cur];
-  const bool capturing = cap != cudaStreamCaptureStatusNone;
-  if (capturing)
+  const bool capturing = cap.on();
+  if (capturing) {
     pl->frozen = true;
-  else if (b.in_use && b.last != s) {  // so that the last call's stream stands for all calls before it
+    KV_CUDA(kv, cap.keep(kv->mem));
+    KV_CUDA(kv, cap.keep(b.mem));
+  } else if (b.in_use && b.last != s) {  // so that the last call's stream stands for all calls before it
     KV_CUDA(kv, mark_used(b));
     KV_CUDA(kv, cudaStreamWaitEvent(s, b.used, 0));
   }
@@ -461,6 +549,7 @@ void ps_kv_plan_destroy(ps_kv_plan* pl) {
   release(pl->buf[0]);
   release(pl->buf[1]);
   if (pl->copy) cudaStreamDestroy(pl->copy);
+  free_unused();
   delete pl;
 }
 
@@ -468,8 +557,8 @@ void ps_kv_destroy(ps_kv* kv) {
   if (!kv) return;
   OnDevice on(kv->device);
   cudaDeviceSynchronize();
-  if (kv->pool) cudaFree(kv->pool);
-  if (kv->err_host) cudaFreeHost(kv->err_host);
+  drop(kv->mem);
+  free_unused();
   delete kv;
 }
 

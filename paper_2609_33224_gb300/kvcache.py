@@ -62,7 +62,8 @@ class KVCache:
             raise PSError(s, self._lib.ps_kv_last_error(self._h).decode())
 
     def close(self):
-        """Release the cache's memory, and the plans made for it."""
+        """Release the cache's memory, and the plans made for it.  What a CUDA graph's captured calls read is kept for the
+        graph, and freed with the next cache or plan made or closed after it."""
         if getattr(self, "_h", None):
             for p in list(self._plans):
                 p.close()
