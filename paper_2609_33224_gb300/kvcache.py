@@ -15,7 +15,7 @@ import weakref
 import numpy as np
 import torch
 
-from . import PS_OK, PSError, PsKvConfig, PsKvRows, lib
+from . import PS_ERR_STATE, PS_OK, PSError, PsKvConfig, PsKvRows, lib
 
 FORMATS = {"bf16": 0, "fp16": 1, "fp8": 2}
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 3}
@@ -223,9 +223,11 @@ class AttentionPlan:
         b = np.ascontiguousarray(b)
         if not 0 <= int(num_queries) < 1 << 32:
             raise ValueError("num_queries must be in 0..2^32-1")
-        self.num_queries = self.workspace_bytes = 0
-        self.cache._check(L.ps_kv_plan_set(h, int(num_queries), spans.ctypes.data if spans.size else None, spans.size,
-                                           b.ctypes.data if b.size else None, b.size))
+        s = L.ps_kv_plan_set(h, int(num_queries), spans.ctypes.data if spans.size else None, spans.size,
+                             b.ctypes.data if b.size else None, b.size)
+        if s != PS_ERR_STATE:  # a plan that a CUDA graph holds stays as it is
+            self.num_queries = self.workspace_bytes = 0
+        self.cache._check(s)
         n = ctypes.c_uint64()
         self.cache._check(L.ps_kv_plan_workspace(h, ctypes.byref(n)))
         self.num_queries, self.workspace_bytes = int(num_queries), n.value

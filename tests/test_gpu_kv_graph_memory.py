@@ -96,3 +96,16 @@ def test_memory_is_freed_with_the_graph(kv):
             break
         time.sleep(0.05)
     assert free() > before - size // 2
+
+
+def test_a_captured_plan_stays_as_it_is(kv):
+    """A refused set leaves the plan's batch in place, for eager calls and for replays."""
+    import paper_2609_33224_gb300 as P
+    graph, inputs, got, want, cache, plan = _captured(kv)
+    with pytest.raises(P.PSError, match="PS_ERR_STATE"):
+        plan.set(1, [(0, 1, 5, 0, 0)], [0])
+    assert torch.equal(cache.attend(inputs[3], plan), want[0])
+    got[0].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0])
