@@ -526,12 +526,15 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   a.err = kv->err_dev;
   const int D = (int)kv->D;
   cudaError_t e = cudaSuccess;
-  // In a graph the first kernel follows whatever node it has to: it takes the plain dependency.
+  // In a graph the first kernel, the join of a batch without a key too, follows whatever node it has to: it takes the
+  // plain dependency.
   a.rows_first = pl->dev.tile_workers == 0;
   if (pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, !capturing, s);
   if (e == cudaSuccess && pl->dev.row_workers)
     e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0 || !capturing, s);
-  if (e == cudaSuccess && pl->dev.njoin) e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev, s);
+  if (e == cudaSuccess && pl->dev.njoin)
+    e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev,
+                          pl->dev.tile_workers || pl->dev.row_workers || !capturing, s);
   if (!capturing) {  // also after a failed launch: the ones before it read the buffer
     b.in_use = true;
     b.recorded = false;

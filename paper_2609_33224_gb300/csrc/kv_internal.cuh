@@ -93,7 +93,7 @@ struct StoreArgs {
 cudaError_t launch_write(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_read(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
-cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, cudaStream_t s);
+cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
 cudaError_t prepare_tiles(int D, int fmt);

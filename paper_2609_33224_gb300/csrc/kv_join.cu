@@ -130,19 +130,19 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
 }
 
 template <int D, bool FP16>
-cudaError_t go(const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
+cudaError_t go(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   const uint32_t rows = p.njoin * p.join_stride;
   // A CTA a row where there are few: 64 rows of 64 parts 7 us less than a warp a row; 2048 rows of 38 parts 3 us more.
   if (p.max_parts > 4 && rows <= 1024)
-    return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, true, s, a, p);
-  return launch(join_kernel<D, FP16, false>, (rows + 7) / 8, 256, 0, 1, true, s, a, p);
+    return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, overlap, s, a, p);
+  return launch(join_kernel<D, FP16, false>, (rows + 7) / 8, 256, 0, 1, overlap, s, a, p);
 }
 
 }  // namespace
 
-cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, cudaStream_t s) {
-  if (D == 128) return fp16 ? go<128, true>(a, p, s) : go<128, false>(a, p, s);
-  return fp16 ? go<64, true>(a, p, s) : go<64, false>(a, p, s);
+cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
+  if (D == 128) return fp16 ? go<128, true>(a, p, overlap, s) : go<128, false>(a, p, overlap, s);
+  return fp16 ? go<64, true>(a, p, overlap, s) : go<64, false>(a, p, overlap, s);
 }
 
 }  // namespace pskv
