@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "kv_internal.cuh"
+#include "kv_ring.h"
 
 namespace pskv {
 namespace {
@@ -256,13 +257,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 
     auto give_up = [&]() {
       if (lane == 0) atomicOr_system(a.err, kErrWait);
-      while (--in_flight) {  // the copies behind it write this warp's memory: they are waited for too
-        if (++st == kStages) {
-          st = 0;
-          phase ^= 1u;
-        }
-        mbar_wait(bar + st * 8, phase);
-      }
+      // the copies under way write this warp's memory: they are waited for, each as long again
+      drain_ring<kStages>(st, phase, in_flight, [&](uint32_t i, uint32_t parity) { mbar_wait(bar + i * 8, parity); });
       if (!waited) wait_for_last();
     };
     // One block.  Apart (fp8): with value scales that lie far apart.
