@@ -62,6 +62,7 @@ struct Bars {
   uint64_t raw_full[4], raw_empty[4];
   uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], tail_here, tail_done, drain;
   uint32_t tmem;
+  uint32_t gave_up;  // by the warp that arrives on tail_here, before its last arrival
 };
 
 // ---- tcgen05
@@ -297,6 +298,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     mbar_init(smem_u32(&bars.tail_here), 1);
     mbar_init(smem_u32(&bars.tail_done), 1);
     mbar_init(smem_u32(&bars.drain), 1);
+    bars.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) tc_alloc<C::kCtas>(smem_u32(&bars.tmem), 512);
@@ -678,6 +680,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       alive = mbar_wait(smem_u32(&bars.drain), 0) && alive;  // nothing is in flight when tensor memory is freed
       if (!alive) {
         atomicOr_system(a.err, kErrWait);
+        *static_cast<volatile uint32_t*>(&bars.gave_up) = 1;
         mbar_arrive(smem_u32(&bars.tail_here));  // releases the warp that waits for it
       }
     } else if (warp == 9 && rank == 1 && !C::kFp8 && elect_one()) {
@@ -700,6 +703,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       }
       if (!alive) {
         atomicOr_system(a.err, kErrWait);
+        *static_cast<volatile uint32_t*>(&bars.gave_up) = 1;
         mbar_arrive(smem_u32(&bars.tail_here));
       }
     } else if (warp == 10 && !C::kFp8) {
@@ -717,6 +721,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
           alive = false;
           break;
         }
+        if (*static_cast<volatile uint32_t*>(&bars.gave_up)) break;  // no step comes any more
         const uint32_t v = ring + (n - 1) % C::kSlots * C::kSlot;  // the last step's values
         for (uint32_t i = left * 8 + lane; i < kTileKeys * 8; i += 32)
           sts128(v + (i / 8) * 128 + (i % 8) * 16, 0, 0, 0, 0);

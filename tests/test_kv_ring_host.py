@@ -39,3 +39,15 @@ def test_the_row_kernel_uses_it():
     with open(os.path.join(CSRC, "kv_rows.cu")) as f:
         text = f.read()
     assert text.count("drain_ring<kStages>(st, phase, in_flight,") == 1 and "while (--in_flight)" not in text
+
+
+def test_the_tile_kernel_ends_its_long_wait():
+    """The warp that zeroes partial steps waits long for each; the threads it waits for say that they have given up
+    before their last arrival, and it asks after each wait, before it goes on."""
+    with open(os.path.join(CSRC, "kv_tiles.cu")) as f:
+        text = f.read()
+    told = "*static_cast<volatile uint32_t*>(&bars.gave_up) = 1;\n        mbar_arrive(smem_u32(&bars.tail_here));"
+    assert text.count("bars.gave_up = 0;") == 1 and text.count(told) == 2
+    assert text.count("mbar_arrive(smem_u32(&bars.tail_here));") == 4  # two a step, two when given up
+    wait = text.index("60000000000ull")
+    assert wait < text.index("if (*static_cast<volatile uint32_t*>(&bars.gave_up)) break;") < text.index("- 1) % C::kSlots * C::kSlot;")
