@@ -18,7 +18,8 @@
  *     finds wrong (a slot outside the cache, a wait that gave up) is reported by the next call on the
  *     cache, or by ps_kv_check.
  *   - Tensors have their head_dim elements next to each other; token and head strides are free, in
- *     elements.  Base addresses are 16-byte aligned and strides multiples of 16 bytes.
+ *     elements.  Base addresses are 16-byte aligned and strides multiples of 16 bytes.  Rows of a result do not
+ *     overlap (rows that are read may: a stride of 0 repeats one).
  *   - Calls may be captured into a CUDA graph.  The graph keeps the cache's blocks and the plan's arrays that its calls
  *     read, also after ps_kv_destroy and ps_kv_plan_destroy; they are freed by the first ps_kv_create,
  *     ps_kv_plan_create, ps_kv_plan_destroy or ps_kv_destroy after the graph and its executable graphs are gone.  The

@@ -170,14 +170,38 @@ const char* rows_error(const ps_kv_rows* r, uint32_t heads, uint64_t n) {
   return nullptr;
 }
 
+// Whether some two of n x heads rows of D elements overlap, which a result's must not.
+bool rows_overlap(const ps_kv_rows* r, uint64_t n, uint32_t heads, uint32_t D) {
+  using Wide = unsigned __int128;
+  const auto size = [](int64_t x) { return x < 0 ? 0 - (uint64_t)x : (uint64_t)x; };
+  if (n == 0) return false;
+  uint64_t s0 = n > 1 ? size(r->token_stride) : 0, s1 = heads > 1 ? size(r->head_stride) : 0, c0 = n, c1 = heads;
+  if (n > 1 && s0 < D) return true;
+  if (heads > 1 && s1 < D) return true;
+  if (n == 1 || heads == 1) return false;
+  if (s0 > s1) {
+    std::swap(s0, s1);
+    std::swap(c0, c1);
+  }
+  // i rows of the wider stride on, the nearest of the narrower: none where all of those lie before the first of them
+  const Wide extent = (Wide)(c0 - 1) * s0 + D;
+  for (uint64_t i = 1; i < c1 && (Wide)i * s1 < extent; ++i) {
+    const Wide j = (Wide)i * s1 / s0, rest = (Wide)i * s1 % s0;
+    if ((j < c0 && rest < D) || (j + 1 < c0 && s0 - rest < D)) return true;
+  }
+  return false;
+}
+
 ps_status store_args(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const int64_t* slots, uint64_t n,
-                     pskv::StoreArgs* a) {
+                     bool results, pskv::StoreArgs* a) {
   const char* m = rows_error(k, kv->heads, n);
   if (!m) m = rows_error(v, kv->heads, n);
   if (!m && k->type != v->type) m = "k and v must have one element type";
   if (!m && n > 0 && !slots) m = "slots is NULL";
   if (!m && n > 0 && reinterpret_cast<uintptr_t>(slots) % 8) m = "slots must start on an 8-byte boundary";
   if (!m && n > (1ull << 40)) m = "too many tokens";
+  if (!m && results && (rows_overlap(k, n, kv->heads, kv->D) || rows_overlap(v, n, kv->heads, kv->D)))
+    m = "rows of a result overlap";
   if (m) return fail(kv, PS_ERR_INVALID, m);
   *a = pskv::StoreArgs{kv->pool,         slots,          n,
                        kv->blocks * pskv::kBlock, kv->heads, k->data, v->data, k->token_stride, k->head_stride,
@@ -386,7 +410,7 @@ ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const
   ps_status st = reported(kv);
   if (st != PS_OK) return st;
   pskv::StoreArgs a;
-  st = store_args(kv, k, v, slots, n, &a);
+  st = store_args(kv, k, v, slots, n, false, &a);
   if (st != PS_OK || n == 0) return st;
   OnDevice on(kv->device);
   Capture cap;
@@ -402,7 +426,7 @@ ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_ro
   ps_status st = reported(kv);
   if (st != PS_OK) return st;
   pskv::StoreArgs a;
-  st = store_args(kv, k, v, slots, n, &a);
+  st = store_args(kv, k, v, slots, n, true, &a);
   if (st != PS_OK || n == 0) return st;
   OnDevice on(kv->device);
   Capture cap;
@@ -487,6 +511,7 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   if (!m) m = rows_error(out, pl->q_heads, T);
   const int want = kv->fmt == PS_KV_FP16 ? PS_KV_FP16 : PS_KV_BF16;
   if (!m && (q->type != want || out->type != want)) m = "q and out must have the cache's 16-bit type (bf16 with fp8)";
+  if (!m && rows_overlap(out, T, pl->q_heads, kv->D)) m = "rows of a result overlap";
   if (!m && lse && reinterpret_cast<uintptr_t>(lse) % 4) m = "lse must start on a 4-byte boundary";
   if (!m && !std::isfinite(scale)) m = "scale must be finite";
   const uint64_t need = workspace_bytes(pl);
