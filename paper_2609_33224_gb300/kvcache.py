@@ -23,6 +23,16 @@ BLOCK_TOKENS = 16
 _ROWS = struct.Struct("@Pqqi4x")  # ps_kv_rows
 assert _ROWS.size == ctypes.sizeof(PsKvRows)
 _stream = torch._C._cuda_getCurrentRawStream  # torch's current stream of a device, as a number
+
+
+def _capturing(device: int) -> bool:
+    """Whether torch's current stream of the device, which need not be the current one, is captured into a graph."""
+    if torch._C._cuda_getDevice() == device:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.device(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
 # ps_kv_span: a run of cached tokens (their blocks start at first_block of the plan's block array) and the
 # queries that see it; causal: the last num_queries tokens are the queries' own
 SPAN_DTYPE = np.dtype([("first_query", np.uint32), ("num_queries", np.uint32), ("length", np.uint64),
@@ -197,7 +207,7 @@ class AttentionPlan:
         return self._h
 
     def _workspace(self, stream: int, nbytes: int):
-        if torch.cuda.is_current_stream_capturing():  # a graph's own: it may run beside other calls
+        if _capturing(self.cache.device):  # a graph's own: it may run beside other calls
             return torch.empty(nbytes, dtype=torch.uint8, device=self.cache._device)
         ws = self._spaces.get(stream)
         if ws is None or ws.numel() < nbytes:
