@@ -78,6 +78,12 @@ template <int I>
 __device__ __forceinline__ float exp_byte(uint32_t w) {
   return __uint_as_float((I == 3 ? w >> 1 : w << (23 - 8 * I)) & 0x7F800000u);
 }
+// The same of the byte at an address.
+__device__ __forceinline__ float exp_of(uint32_t addr) {
+  uint16_t b;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=h"(b) : "r"(addr) : "memory");
+  return __uint_as_float((uint32_t)b << 23);
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -114,41 +120,30 @@ __device__ __forceinline__ float value16(uint16_t b) {
   return __uint_as_float((uint32_t)b << 16);
 }
 
-enum Step { kGoOn, kTooFar, kGaveUp };  // what became of a block
+// Where a worker is: its next piece and the end of its pieces, its ring's next stage and that barrier's phase; whether it has
+// waited for the kernel before this one.
+struct Place {
+  uint32_t piece, end, st, phase;
+  bool waited;
+};
+enum Step { kDone, kTooFar, kGaveUp };
 
-template <int D, int FMT>
-__global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
+// A worker's pieces from `pl` on.  kApart (fp8): the form for queries or value scales whose magnitudes lie far apart, with
+// keys, values, queries and probabilities in bf16, whose exponents reach as far as a float's; the other form leaves it a
+// piece (kTooFar), with nothing of it written, and the pieces after it.  5 requests of 131072 tokens, 256 queries on 32768:
+// 257 and 357 us, 166 and 248 by the other form.  The two are separate instances: as branches of a block they cost the
+// common form registers (178 and 260 us).
+template <int D, int FMT, bool kApart>
+__device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, const uint32_t ring, const uint32_t bar,
+                                           Place& pl) {
   constexpr bool kFp8 = FMT == PS_KV_FP8, kFp16 = FMT == PS_KV_FP16;
   constexpr int kRec = record_bytes(D, FMT), kHalf = half_bytes(D, FMT);
-  constexpr int kStages = ring_stages<D, FMT>();
+  constexpr int kStages = ring_stages<D, FMT>(), kStage = stage_bytes<D, FMT>();
   constexpr int kTiles = D / 8;  // n8 tiles of the output
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ __align__(8) uint64_t bars[kRowWarps * kStages];
-
-  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const uint32_t worker = warp * p.row_ctas + blockIdx.x;  // neighbours in the plan go to different SMs
-  if (worker >= p.row_workers) {  // no barrier of the CTA is used
-    wait_for_last();
-    return;
-  }
-  constexpr int kStage = stage_bytes<D, FMT>();
-  const uint32_t ring = smem_u32(smem) + warp * kStages * kStage;
-  const uint32_t bar = smem_u32(bars) + warp * kStages * 8;
-  if (lane < kStages) mbar_init(bar + lane * 8, 1);
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  __syncwarp();
-
-  const uint32_t piece_end = p.row_off[worker + 1];
+  const uint32_t lane = threadIdx.x % 32;
+  const uint32_t piece_end = pl.end;
   // what is loaded next: block `ahead_i` of piece `ahead`, into stage `ahead_st`
-  uint32_t ahead = p.row_off[worker], ahead_i = 0, ahead_st = 0;
-  // The plan is read at once, the cache and the queries after what may have written them; after a tile kernel of the
-  // same call, which has waited for that, at once too.
-  bool waited = a.rows_first != 0;
-  if (waited) {
-    prefetch(p.row_pieces + ahead);
-    wait_for_last();
-  }
-  let_next_start();
+  uint32_t ahead = pl.piece, ahead_i = 0, ahead_st = pl.st;
   uint32_t ahead_n = 0, ahead_block = 0, ahead_head = 0, ids = 0;
   uint32_t in_flight = 0;
   auto issue = [&]() {
@@ -190,9 +185,22 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
   // then keys 8-15.  Values: keys 0-7 and 8-15 of a chunk, then of the next.
   const uint32_t k_at = kFp8 ? offset8k<D>((mi & 1) * 8 + mr, mi >> 1) : offset16((mi >> 1) * 8 + mr, mi & 1);
   const uint32_t v_at = kHalf + (kFp8 ? offset8v((mi & 1) * 8 + mr, mi >> 1) : offset16((mi & 1) * 8 + mr, mi >> 1));
-  uint32_t st = 0, phase = 0;
+  uint32_t st = pl.st, phase = pl.phase;
+  // The copies under way write this warp's memory: they are waited for, each as long as the one that is given up.
+  auto leave = [&](Step how, uint32_t piece) {
+    bool all = true;
+    drain_ring<kStages>(st, phase, in_flight, [&](uint32_t i, uint32_t parity) { all &= mbar_wait_warp(bar + i * 8, parity); });
+    if (how == kGaveUp || !all) {
+      if (lane == 0) atomicOr_system(a.err, kErrWait);
+      return kGaveUp;
+    }
+    pl.piece = piece;
+    pl.st = ahead_st;
+    pl.phase = st + in_flight >= kStages ? phase ^ 1u : phase;
+    return how;
+  };
 
-  for (uint32_t pi = p.row_off[worker]; pi < piece_end; ++pi) {
+  for (uint32_t pi = pl.piece; pi < piece_end; ++pi) {
     const Piece pc = p.row_pieces[pi];
     // ---- the rows of the tile
     const uint32_t ra = pc.row0 + quad, rb = ra + 8;
@@ -215,9 +223,10 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
     }
     // fp8: codes are exact in fp16 and one instruction turns two of them into it, so the products are fp16.
     // The queries are first scaled by a power of two per row, which brings the largest element just below
-    // 2^15: all but elements 2^-32 of it keep their 8 bits.
+    // 2^15: all but elements 2^-32 of it keep their 8 bits.  Rows with such elements, or so large that a product might
+    // overflow before the key's scale brings it back, are for the other form.
     float qa_scale = a.scale_log2, qb_scale = a.scale_log2;
-    if constexpr (kFp8) {
+    if constexpr (kFp8 && !kApart) {
       float x = 0.0f, y = 0.0f;
 #pragma unroll
       for (int kc = 0; kc < D / 16; ++kc) {
@@ -234,14 +243,18 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
       const float ua = __uint_as_float((uint32_t)(127 + ea) << 23), ub = __uint_as_float((uint32_t)(127 + eb) << 23);
       qa_scale *= __uint_as_float((uint32_t)(127 - ea) << 23);
       qb_scale *= __uint_as_float((uint32_t)(127 - eb) << 23);
+      bool lost = fmaxf(fabsf(qa_scale), fabsf(qb_scale)) > 0x1p90f;
 #pragma unroll
       for (int kc = 0; kc < D / 16; ++kc) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float u = (i & 1) ? ub : ua;
-          qf[kc][i] = pack2<true>(bf16_lo(qf[kc][i]) * u, bf16_hi(qf[kc][i]) * u);
+          const float u = (i & 1) ? ub : ua, lo = bf16_lo(qf[kc][i]) * u, hi = bf16_hi(qf[kc][i]) * u;
+          qf[kc][i] = pack2<true>(lo, hi);
+          const float2 got = __half22float2(*reinterpret_cast<const __half2*>(&qf[kc][i]));
+          lost |= got.x != lo || got.y != hi;
         }
       }
+      if (__any_sync(0xFFFFFFFFu, lost)) return leave(kTooFar, pi);
     }
     // fp8: the scale that the output so far is relative to, 2^5 over it, and the first such scale
     float v_ref = 0.0f, v_inv = 0.0f, v_first = 0.0f;
@@ -255,22 +268,22 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
     for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
     float ma = -INFINITY, mb = -INFINITY, la = 0.0f, lb = 0.0f;
 
-    auto give_up = [&]() {
-      if (lane == 0) atomicOr_system(a.err, kErrWait);
-      // the copies under way write this warp's memory: they are waited for, each as long again
-      drain_ring<kStages>(st, phase, in_flight, [&](uint32_t i, uint32_t parity) { mbar_wait(bar + i * 8, parity); });
-      if (!waited) wait_for_last();
-    };
-    // One block.  Apart (fp8): with value scales that lie far apart.
-    auto step = [&](auto apart, const uint32_t bi) {
-      constexpr bool kApart = decltype(apart)::value;
+    for (uint32_t bi = 0; bi < pc.nblocks; ++bi) {
       const uint32_t rec = ring + st * kStage;
-      if (!mbar_wait_warp(bar + st * 8, phase)) return kGaveUp;
+      if (!mbar_wait_warp(bar + st * 8, phase)) return leave(kGaveUp, pi);
       // ---- scores
       float s[2][4];
 #pragma unroll
       for (int n = 0; n < 2; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+      // two codes as a bf16 operand, with their scales
+      auto scaled = [](uint32_t h, float f0, float f1) {
+        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        return pack2<false>(x.x * f0, x.y * f1);
+      };
       if constexpr (kFp8) {
+        // apart: the scales of this lane's keys of the fragments; the mark of a NaN gives one
+        const float kf[2] = {kApart ? exp_of(rec + 2 * kHalf + exp_place(quad)) : 1.0f,
+                             kApart ? exp_of(rec + 2 * kHalf + exp_place(quad + 8)) : 1.0f};
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
           uint32_t r[4];
@@ -279,7 +292,11 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
           for (int i = 0; i < 4; ++i) {
             uint32_t b0, b1;
             e4m3x4_to_f16x2(r[i], b0, b1);
-            mma16816<true>(s[i & 1], qf[c + (i >> 1)], b0, b1);
+            if (kApart) {
+              b0 = scaled(b0, kf[i & 1], kf[i & 1]);
+              b1 = scaled(b1, kf[i & 1], kf[i & 1]);
+            }
+            mma16816<!kApart>(s[i & 1], qf[c + (i >> 1)], b0, b1);
           }
         }
       } else {
@@ -294,7 +311,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
       float vs[4];  // fp8: the value rows' scales of this lane's keys
       if constexpr (kFp8) {
         const uint32_t ke = lds32(rec + 2 * kHalf + t4 * 4), vx = lds32(rec + 2 * kHalf + kBlock + t4 * 4);
-        const float k0 = exp_byte<0>(ke), k1 = exp_byte<1>(ke), k2 = exp_byte<2>(ke), k3 = exp_byte<3>(ke);
+        const float k0 = kApart ? 1.0f : exp_byte<0>(ke), k1 = kApart ? 1.0f : exp_byte<1>(ke);
+        const float k2 = kApart ? 1.0f : exp_byte<2>(ke), k3 = kApart ? 1.0f : exp_byte<3>(ke);
         s[0][0] = s[0][0] * qa_scale * k0;
         s[0][1] = s[0][1] * qa_scale * k1;
         s[0][2] = s[0][2] * qb_scale * k0;
@@ -307,9 +325,8 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         // probabilities of at most 2^8 (below) and scales of at most twice the reference, their products stay at or
         // below 2^14.  Scales of at least 2^-10 of it leave a product its 11 bits down to probabilities of 2^-9, and
         // below that cost at most 2^-20 of the key's own value.  A key further below, beside large rows that a query
-        // does not see or hardly weighs, would lose its bits: from such a block on, the piece's output is relative to
-        // nothing, and the products are of values with their scales, both factors in bf16, whose exponents reach as
-        // far as a float's.
+        // does not see or hardly weighs, would lose its bits: such a piece is for the other form, whose values have their
+        // scales and whose output is relative to nothing.
         vs[0] = exp_byte<0>(vx);
         vs[1] = exp_byte<1>(vx);
         vs[2] = exp_byte<2>(vx);
@@ -352,7 +369,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
             low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, 2));
             const float ref = top > 2.0f * v_ref ? top : v_ref;
             // (the second: the output so far keeps its bits when it is brought to another reference)
-            if (low < 0x1p-10f * ref || (v_first > 0.0f && ref * 0x1p-60f > v_first)) return kTooFar;
+            if (low < 0x1p-10f * ref || (v_first > 0.0f && ref * 0x1p-60f > v_first)) return leave(kTooFar, pi);
             if (ref > v_ref) {
               const uint32_t inverse = (254u << 23) - __float_as_uint(ref);  // of a power of two
               const float f = v_ref * __uint_as_float(inverse);
@@ -472,12 +489,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
 #pragma unroll
           for (int i = 0; i < 4; ++i) vs[i] = vs[i] < 0x1p120f ? vs[i] : 0.0f;
         }
-        // two codes as the operand that the probabilities' type asks for
-        auto operand = [](uint32_t h, float f0, float f1) {
-          if (!kApart) return h;
-          const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&h));
-          return pack2<false>(x.x * f0, x.y * f1);
-        };
+        auto operand = [&](uint32_t h, float f0, float f1) { return kApart ? scaled(h, f0, f1) : h; };
 #pragma unroll
         for (int c = 0; c < D / 16; c += 2) {
           uint32_t r[4];
@@ -539,28 +551,16 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
         phase ^= 1u;
       }
       issue();
-      return kGoOn;
-    };
-    uint32_t bi = 0;
-    Step did = kGoOn;
-    for (; bi < pc.nblocks; ++bi)
-      if ((did = step(std::false_type(), bi)) != kGoOn) break;
-    if constexpr (kFp8) {
+    }
+
+    // ---- the piece's result
+    if constexpr (kFp8 && !kApart) {
       const float f = v_ref * 0x1p-5f;
 #pragma unroll
       for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][i] *= f;
-      if (did == kTooFar)
-        for (; bi < pc.nblocks; ++bi)
-          if ((did = step(std::true_type(), bi)) != kGoOn) break;
     }
-    if (did == kGaveUp) {
-      give_up();
-      return;
-    }
-
-    // ---- the piece's result
     la += __shfl_xor_sync(0xFFFFFFFFu, la, 1);
     lb += __shfl_xor_sync(0xFFFFFFFFu, lb, 1);
     la += __shfl_xor_sync(0xFFFFFFFFu, la, 2);
@@ -597,9 +597,9 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
     } else {
       // The tile kernel's parts of these rows (the prefix that they share) are joined in here, which saves the
       // write and the read of this part and, mostly, the join kernel.
-      if (pc.nfold && !waited) {
+      if (pc.nfold && !pl.waited) {
         wait_for_last();
-        waited = true;
+        pl.waited = true;
       }
       for (uint32_t fi = 0; fi < pc.nfold; ++fi) {
         const Fold fo = p.folds[pc.fold0 + fi];
@@ -663,7 +663,39 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
       }
     }
   }
-  if (!waited) wait_for_last();
+  return kDone;
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
+  constexpr int kStages = ring_stages<D, FMT>(), kStage = stage_bytes<D, FMT>();
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[kRowWarps * kStages];
+
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t worker = warp * p.row_ctas + blockIdx.x;  // neighbours in the plan go to different SMs
+  if (worker >= p.row_workers) {  // no barrier of the CTA is used
+    wait_for_last();
+    return;
+  }
+  const uint32_t ring = smem_u32(smem) + warp * kStages * kStage;
+  const uint32_t bar = smem_u32(bars) + warp * kStages * 8;
+  if (lane < kStages) mbar_init(bar + lane * 8, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
+
+  // The plan is read at once, the cache and the queries after what may have written them; after a tile kernel of the
+  // same call, which has waited for that, at once too.
+  Place pl{p.row_off[worker], p.row_off[worker + 1], 0, 0, a.rows_first != 0};
+  if (pl.waited) {
+    prefetch(p.row_pieces + pl.piece);
+    wait_for_last();
+  }
+  let_next_start();
+  const Step how = run_pieces<D, FMT, false>(a, p, ring, bar, pl);
+  if constexpr (FMT == PS_KV_FP8)
+    if (how == kTooFar) run_pieces<D, FMT, true>(a, p, ring, bar, pl);
+  if (!pl.waited) wait_for_last();
 }
 
 template <int D, int FMT>
