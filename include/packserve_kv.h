@@ -108,8 +108,8 @@ PS_API ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_que
  * call returns).  A query that no span covers, or none with a key, gets zeros.  Spans may share blocks and
  * overlap; a query's softmax runs over the tokens of all its spans (a token listed twice counts twice).
  * The call may follow calls that still run: the arrays of the last set but one are overwritten, after
- * waiting for the calls that read them.  PS_ERR_STATE if a call on this plan was captured into a CUDA
- * graph: the graph reads the plan's arrays, so such a plan stays as it is.  The paper has no counterpart.
+ * waiting for the calls that read them.  PS_ERR_STATE while there is a CUDA graph that has captured a call on this
+ * plan: the graph reads the plan's arrays, so such a plan stays as it is.  The paper has no counterpart.
  * Errors: PS_ERR_INVALID (the plan is left without a batch), PS_ERR_STATE, PS_ERR_OOM, PS_ERR_CUDA. */
 PS_API ps_status ps_kv_plan_set(ps_kv_plan* plan, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
                                 const uint32_t* blocks, uint64_t num_blocks);

@@ -53,7 +53,7 @@ struct ps_kv_plan {
     cudaStream_t last = nullptr;  // of the last such call, which comes after all others
   } buf[2];
   int cur = 0;
-  bool set = false, frozen = false;
+  bool set = false;
   cudaStream_t copy = nullptr;
   pskv::PlanDev dev{};
   uint32_t queries = 0;
@@ -236,7 +236,7 @@ void release(ps_kv_plan::Buffer& b) {
 }
 
 ps_status grow(ps_kv* kv, ps_kv_plan::Buffer& b, size_t need) {
-  if (need <= b.cap) return PS_OK;
+  if (b.mem && need <= b.cap) return PS_OK;
   size_t cap = std::max<size_t>(b.cap * 2, 1 << 16);
   while (cap < need) cap *= 2;
   if (b.mem) drop(b.mem);
@@ -478,7 +478,8 @@ ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_queries, u
 ps_status ps_kv_plan_set(ps_kv_plan* pl, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
                          const uint32_t* blocks, uint64_t num_blocks) {
   if (!pl) return PS_ERR_INVALID;
-  if (pl->frozen) return fail(pl->kv, PS_ERR_STATE, "a CUDA graph holds this plan's arrays: make another plan");
+  if (pl->buf[pl->cur].mem->refs.load(std::memory_order_acquire) > 1)  // the other buffer was last set before this one
+    return fail(pl->kv, PS_ERR_STATE, "a CUDA graph holds this plan's arrays: make another plan");
   OnDevice on(pl->kv->device);
   try {
     return plan_set(pl, num_queries, spans, num_spans, blocks, num_blocks);
@@ -526,7 +527,6 @@ ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_
   ps_kv_plan::Buffer& b = pl->buf[pl->cur];
   const bool capturing = cap.on();
   if (capturing) {
-    pl->frozen = true;
     KV_CUDA(kv, cap.keep(kv->mem));
     KV_CUDA(kv, cap.keep(b.mem));
   } else if (b.in_use && b.last != s) {  // so that the last call's stream stands for all calls before it

@@ -109,3 +109,35 @@ def test_a_captured_plan_stays_as_it_is(kv):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0])
+
+
+def test_a_plan_is_free_again_after_its_graph(kv):
+    import paper_2609_33224_gb300 as P
+    graph, inputs, got, want, cache, plan = _captured(kv)
+    span = [(0, T, 700, 0, 0)]
+    with pytest.raises(P.PSError, match="PS_ERR_STATE"):
+        plan.set(T, span, list(range(BLOCKS)))
+    graph.replay()
+    torch.cuda.synchronize()
+    graph.reset()
+    for _ in range(100):  # the driver gives the reference up on a thread of its own
+        try:
+            plan.set(T, span, list(range(BLOCKS)))
+            break
+        except P.PSError:
+            time.sleep(0.05)
+    other = kv.AttentionPlan(cache, HQ, T, 1, BLOCKS)
+    other.set(T, span, list(range(BLOCKS)))
+    assert torch.equal(cache.attend(inputs[3], plan), cache.attend(inputs[3], other))
+    cache.check()
+
+
+def test_a_plan_without_spans(kv):
+    """Limits of zero: a batch without a key."""
+    with kv.KVCache(4, H, D) as c:
+        plan = kv.AttentionPlan(c, HQ, T, 0, 0)
+        for n in (0, T, 0, 1):
+            plan.set(n, [], [])
+            q = torch.ones(n, HQ, D, device="cuda").bfloat16()
+            assert not c.attend(q, plan).any()
+        c.check()
