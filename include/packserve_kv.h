@@ -125,7 +125,9 @@ PS_API ps_status ps_kv_plan_workspace(ps_kv_plan* plan, uint64_t* bytes);
  * num_queries x q_heads floats.  workspace: device memory, 256-byte aligned, used by this call alone while
  * it runs.  The stream has to exist until the plan is set again, used on another stream or destroyed.  kv may
  * be another cache than the plan's, of the same shape.  Scores, sums and partial results are held in 32 bits,
- * probabilities are rounded to 16 bits for their product with the values.
+ * probabilities are rounded to 16 bits for their product with the values: bf16 ones to 8 bits whatever their size; fp16
+ * ones (PS_KV_FP16, and PS_KV_FP8 where few rows see the keys) to 11 bits, but where the largest of a row counts 1,
+ * those below 2^-14 (PS_KV_FP8: 2^-9) are off by up to 2^-25 (2^-20).
  * The decode and prefill steps of Eq. 6 and Eq. 7 consist of it; the paper has no counterpart.
  * Errors: PS_ERR_INVALID, PS_ERR_STATE (no batch is set), PS_ERR_CUDA. */
 PS_API ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,

@@ -25,9 +25,9 @@ constexpr int tile_ctas_of(int D) { return D == 128 ? 2 : 1; }
 constexpr int tile_rows_of(int D) { return 256 * tile_ctas_of(D); }
 constexpr int kTileKeys = 128;  // keys of one step of the tile kernel
 
-// Workers (warps) of a CTA of the row kernel.  12 hide more of a block's latency than 8 (131072 tokens of 5
-// requests, fp8: 182 us, 187; 64 queries on 8192, on 72 SMs: 40.3 and 41.1); 16 leave 128 registers a thread, and
-// spill (223 us).
+// Workers (warps) of a CTA of the row kernel.  12 hide more of a block's latency than 8 where instructions bind it (131072
+// tokens of 5 requests, fp8: 166 us, 183; 256 queries on 32768: 249 and 274; 16-bit ones are bound by bytes: 64 queries
+// on 8192 39.2 and 37.9); 16 would leave 128 registers a thread, and spill.
 constexpr int kRowWarps = 12;
 
 // A piece of work of either attention kernel: a run of key blocks for the rows of one tile and one
@@ -121,7 +121,8 @@ constexpr uint32_t kSplitSteps = 8;
 // side they take less time than one after the other.  Returns how many SMs the row kernel gets (all: one after the
 // other), by the times above, 3.3 ns of the GPU for a unit's start and end, the bytes at 6.2 TB/s, and what the
 // kernels take whatever their SMs: 6 and 4 us.  64 queries on 8192 shared tokens 55.7 -> 41.8 us, 9 groups under one
-// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 267 -> 260 (245 by now).
+// prompt with head_dim 64 24.6 -> 20.4, 256 queries on 32768 (fp8) 267 -> 260, with the kernels of then (39.2, 17.8 and
+// 248 now).
 constexpr double kUnitNs = 3.3, kBytesPerNs = 6200.0, kTileFixed = 6000.0, kRowFixed = 4000.0;
 inline int row_sms(const PlanShape& kv, double steps, double blocks, double units) {
   const double tile = step_ns(kv) * steps, work = block_ns(kv) * blocks + kUnitNs * units;

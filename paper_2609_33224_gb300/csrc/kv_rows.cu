@@ -10,10 +10,10 @@
 //
 // Bound by the bytes of the cache: 2 * D elements per key and head for 4 * D * 16 multiply-adds.  mma.sync
 // has the smallest tile (16 rows) and takes operands and results in registers; tcgen05's 128 rows would be
-// 1/8 or less filled here.  5 requests of 65536 to 131072 tokens, fp8, 8 heads, 128 columns, 1.05 GB: 159 us
-// = 6.6 TB/s, 97% of the measured copy; with 44 of the 152 SMs, where memory does not bind it, an fp8 block
-// takes 770 cycles of a scheduler (ALU pipe 54%).  As a warp joins nothing with
-// its CTA's other warps, a share's partial results cost 4 * D + 8 bytes a row.
+// 1/8 or less filled here.  5 requests of 65536 to 131072 tokens, fp8, 8 heads, 128 columns, 1.05 GB: 166 us a pass,
+// the join included, = 6.3 TB/s, 93% of the measured copy; with 44 of the 152 SMs, where memory does not bind it, it is
+// bound by its instructions (ALU pipe 56%).  As a warp joins nothing with its CTA's other warps, a share's partial
+// results cost 4 * D + 8 bytes a row.
 #include <type_traits>
 
 #include "kv_internal.cuh"
@@ -22,8 +22,8 @@
 namespace pskv {
 namespace {
 
-// Ring of one warp: two to four records of 128 columns.  More of them (28 KB) measured the same or 2% slower:
-// the memory then only answers later.
+// Ring of one warp: with 128 columns two records of 16 bits or three of fp8, with 64 four or seven.  More of them
+// (28 KB) measured the same or 2% slower: the memory then only answers later.
 constexpr int kRingBytes = 16640;
 
 // A stage starts on a multiple of 128 bytes, so that a swizzled address is an exclusive or with a constant.
@@ -120,19 +120,19 @@ __device__ __forceinline__ float value16(uint16_t b) {
   return __uint_as_float((uint32_t)b << 16);
 }
 
-// Where a worker is: its next piece and the end of its pieces, its ring's next stage and that barrier's phase; whether it has
-// waited for the kernel before this one.
+// Where a worker is: its next piece and the end of its pieces, its ring's next stage and that barrier's phase; whether
+// it has waited for the kernel before this one.
 struct Place {
   uint32_t piece, end, st, phase;
   bool waited;
 };
 enum Step { kDone, kTooFar, kGaveUp };
 
-// A worker's pieces from `pl` on.  kApart (fp8): the form for queries or value scales whose magnitudes lie far apart, with
-// keys, values, queries and probabilities in bf16, whose exponents reach as far as a float's; the other form leaves it a
-// piece (kTooFar), with nothing of it written, and the pieces after it.  5 requests of 131072 tokens, 256 queries on 32768:
-// 257 and 357 us, 166 and 248 by the other form.  The two are separate instances: as branches of a block they cost the
-// common form registers (178 and 260 us).
+// A worker's pieces from `pl` on.  kApart (fp8): the form for queries or value scales whose magnitudes lie far apart,
+// with keys, values, queries and probabilities in bf16, whose exponents reach as far as a float's; the other form leaves
+// it a piece (kTooFar), with nothing of it written, and the pieces after it.  5 requests of 131072 tokens, 256 queries on
+// 32768: 257 and 357 us, 166 and 248 by the other form.  The two are separate instances: as branches of a block they
+// cost the common form registers (178 and 260 us).
 template <int D, int FMT, bool kApart>
 __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, const uint32_t ring, const uint32_t bar,
                                            Place& pl) {
@@ -189,7 +189,8 @@ __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, 
   // The copies under way write this warp's memory: they are waited for, each as long as the one that is given up.
   auto leave = [&](Step how, uint32_t piece) {
     bool all = true;
-    drain_ring<kStages>(st, phase, in_flight, [&](uint32_t i, uint32_t parity) { all &= mbar_wait_warp(bar + i * 8, parity); });
+    drain_ring<kStages>(st, phase, in_flight,
+                        [&](uint32_t i, uint32_t parity) { all &= mbar_wait_warp(bar + i * 8, parity); });
     if (how == kGaveUp || !all) {
       if (lane == 0) atomicOr_system(a.err, kErrWait);
       return kGaveUp;

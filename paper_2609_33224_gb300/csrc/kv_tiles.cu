@@ -232,8 +232,8 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, ui
 // fp8: the codes of `n` chunks of a row, at `src(c)`, as bf16 with the row's scale applied, to `dst(2 c)` and
 // `dst(2 c + 1)`.
 // Codes to fp16 (one instruction for two), to floats, times the scale, to bf16: two of the ALU pipe's instructions for
-// two elements, where taking the codes' bits apart needs four (256 queries on 32768 tokens: 253 -> 245 us).  The mark of a row with a NaN gives an infinity, whose
-// product with such a row's codes, zeros, is a NaN.
+// two elements, where taking the codes' bits apart needs four (256 queries on 32768 tokens: 8 us of 253).  The mark of a
+// row with a NaN gives an infinity, whose product with such a row's codes, zeros, is a NaN.
 template <int N, class Src, class Dst>
 __device__ __forceinline__ void to_bf16(uint32_t e, bool live, Src src, Dst dst) {
   const float f = __uint_as_float(e << 23);

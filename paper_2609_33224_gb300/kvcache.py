@@ -4,7 +4,8 @@
 ``KVCache`` holds the keys and values of one layer: ``write`` stores new tokens (rounding them to the
 cache's format), ``read`` gives back what the cache holds, ``attend`` computes attention of a batch that an
 ``AttentionPlan`` describes.  All three run on torch's current stream of the cache's device and return
-without waiting for it; what a kernel finds wrong raises ``PSError`` from the next call, or from ``check``.
+without waiting for it; what a kernel finds wrong raises ``PSError`` from the next call, or from ``check``.  They are
+operators of serving: no gradient goes through them, and their results are not part of autograd's graph.
 """
 from __future__ import annotations
 
@@ -187,7 +188,9 @@ class AttentionPlan:
 
     ``set(num_queries, spans, blocks)``: ``spans`` is an array of ``SPAN_DTYPE`` (or rows of its five fields),
     ``blocks`` the uint32 block ids that they index.  A prefix shared by a range of queries is one span over
-    all of them, a request's own tokens a (causal) span of its own.
+    all of them, a request's own tokens a (causal) span of its own.  ``set`` works on the host (27 us for one request,
+    0.1 ms for 256 on a prefix, 2.5 ms for 8192 new tokens of 64 heads) and waits for its copy to the device.  While a
+    CUDA graph holds a captured call on the plan, ``set`` is refused and the plan stays as it is.
     """
 
     def __init__(self, cache: KVCache, q_heads: int, max_queries: int, max_spans: int, max_blocks: int):
