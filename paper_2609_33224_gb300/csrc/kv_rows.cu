@@ -36,9 +36,6 @@ constexpr int ring_stages() {
   return kRingBytes / stage_bytes<D, FMT>();
 }
 
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
 __device__ __forceinline__ float abs_max2(uint32_t w) { return fmaxf(fabsf(bf16_lo(w)), fabsf(bf16_hi(w))); }
 
 template <bool FP16>
@@ -83,11 +80,6 @@ __device__ __forceinline__ float exp_of(uint32_t addr) {
   uint16_t b;
   asm volatile("ld.shared.u8 %0, [%1];" : "=h"(b) : "r"(addr) : "memory");
   return __uint_as_float((uint32_t)b << 23);
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
 }
 __device__ __forceinline__ float min3(float a, float b, float c) {
   float r;

@@ -21,9 +21,6 @@ struct Elem<PS_KV_FP32> {
   static constexpr int kSize = 4;
 };
 
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
 // N consecutive elements as 16-byte loads, then as floats
 template <int TYPE, int N>
 struct Row {

@@ -204,11 +204,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 
 // Shared-memory operand descriptor, 128-byte swizzle, groups of 8 rows (keys and queries, K-major; values,
 // MN-major, one panel of 64 columns) 1024 bytes apart.
