@@ -12,7 +12,8 @@
  *
  * Conventions:
  *   - Every call returns a ps_status; on failure ps_kv_last_error() describes it.
- *   - ps_kv_write, ps_kv_read and ps_kv_attend only enqueue work on the given stream (a cudaStream_t, NULL
+ *   - ps_kv_write, ps_kv_write_rotated, ps_kv_read, ps_kv_move, ps_kv_copy_blocks, ps_kv_tree_mask, ps_kv_attend and
+ *     ps_kv_attend_masked only enqueue work on the given stream (a cudaStream_t, NULL
  *     for the default stream) and return.  Their tensors are device memory of the cache's device, which
  *     must stay valid until that work is done; ordering between streams is the caller's.  What a kernel
  *     finds wrong (a slot outside the cache, a wait that gave up) is reported by the next call on the
@@ -86,11 +87,67 @@ PS_API ps_status ps_kv_create(const ps_kv_config* cfg, ps_kv** out);
 PS_API ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v, const int64_t* slots, uint64_t n,
                              void* stream);
 
+/* Rotary positions.  Of a head's elements the first dims (a multiple of 16, at most head_dim) are taken in dims / 2
+ * pairs (a, b): elements i and i + dims / 2, or with `interleaved` 2 i and 2 i + 1.  At position p pair i turns by
+ * p * frequency[i] radians: (a, b) becomes magnitude * (a cos - b sin, b cos + a sin); the other elements stay.  A
+ * frequency is held as a 64-bit fraction of a turn, and its product with the position wraps at a whole turn, so that
+ * angles are as exact at a position of millions as at 1 (to p * 2^-52 of frequency[i], at least 2^-25 of a turn). */
+typedef struct {
+  uint32_t dims;
+  uint32_t interleaved; /* 0 or 1 */
+  float magnitude;
+  double frequency[64];
+} ps_kv_rotary;
+
+/* ps_kv_write of keys that are first rotated by positions[t] (device array of n int64, negative ones too), and the same
+ * rotation of queries: row t of q (q_heads heads) goes to row t of q_out.  Rotation is in 32 bits, and what is stored is
+ * rounded once.  q, k and v have one element type; q_out the type that ps_kv_attend takes.  q and q_out: both NULL (and
+ * q_heads 0) for keys alone; q_out may be q itself, and must not overlap it or k or v otherwise.  Queries of tokens
+ * whose slot is negative or outside the cache are rotated all the same.  The paper has no counterpart.
+ * Errors: as ps_kv_write. */
+PS_API ps_status ps_kv_write_rotated(ps_kv* kv, const ps_kv_rotary* rotary, const int64_t* positions, const ps_kv_rows* q,
+                                     const ps_kv_rows* q_out, uint32_t q_heads, const ps_kv_rows* k, const ps_kv_rows* v,
+                                     const int64_t* slots, uint64_t n, void* stream);
+
 /* Read n tokens back: k and v (of one type, rounded to it) receive the values that the cache holds at
  * slots[t]; a negative slot gives zeros, a slot past the cache zeros and a report.
  * The paper has no counterpart.  Errors: as ps_kv_write. */
 PS_API ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_rows* k, const ps_kv_rows* v,
                             void* stream);
+
+/* Move n tokens inside the cache: the keys and values at slot src[i] go to slot dst[i], as they are held, all heads.  It is
+ * as if every source were read before any slot is written: an accepted path of drafted tokens moves to the front of its
+ * blocks, and slots may change places.  src, dst: device arrays of n int64.  A negative dst[i] skips the move, a
+ * negative src[i] clears dst[i] to zeros; where either lies past the cache, the move is skipped and reported.  Slots of
+ * dst must be different.  workspace: as ps_kv_attend's, of the bytes that ps_kv_move_workspace gives (0 possible).
+ * The paper has no counterpart.  Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+PS_API ps_status ps_kv_move(ps_kv* kv, const int64_t* src, const int64_t* dst, uint64_t n, void* workspace,
+                            uint64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that ps_kv_move needs for n tokens.  The paper has no counterpart. */
+PS_API ps_status ps_kv_move_workspace(ps_kv* kv, uint64_t n, uint64_t* bytes);
+
+/* Copy n whole blocks of `from` (which may be kv, or another cache of the same device, heads, head_dim and format) to
+ * blocks of kv: src[i] to dst[i] (device arrays of n int64).  A request is forked so at its open block, or a chain is
+ * handed to another cache.  A negative src[i] clears dst[i] to zeros, a negative dst[i] skips the copy; a block past its
+ * cache skips it and is reported by kv.  A block may be copied to many places.  Blocks of dst must be different, and where
+ * from is kv, none of them may be another copy's source.  The paper has no counterpart.
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+PS_API ps_status ps_kv_copy_blocks(ps_kv* kv, ps_kv* from, const int64_t* src, const int64_t* dst, uint64_t n, void* stream);
+
+/* Masks and positions of trees of drafted tokens, for ps_kv_attend_masked and ps_kv_write_rotated.  Tree b's nodes are
+ * rows offsets[b] .. offsets[b + 1] - 1 of num_nodes (device array of num_trees + 1 int64, rising), or with offsets NULL
+ * each tree has num_nodes / num_trees of them.  parents[t] (int32): the number in its tree, below t's own, of node t's
+ * parent; -1: t is a root, a child of the request's context; less: t is no node.  mask row t (`words` 32-bit words,
+ * mask_stride words apart): bit j is set where node j of the tree is t itself or an ancestor of it; none for no node.
+ * positions (NULL, or num_nodes int64): the node's depth, 0 for a root, plus start[b] (device array of num_trees int64,
+ * or NULL for 0).  A tree has at most 32 * words nodes, words at most 256.  Rows of no tree stay as they are.  A parent
+ * that is not below its node, or offsets that do not rise within num_nodes or give a tree too many nodes, are reported
+ * (such a node counts as a root, such a tree is skipped).  The paper has no counterpart.
+ * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
+PS_API ps_status ps_kv_tree_mask(ps_kv* kv, const int32_t* parents, uint64_t num_nodes, const int64_t* offsets,
+                                 uint32_t num_trees, const int64_t* start, uint32_t* mask, int64_t mask_stride,
+                                 uint32_t words, int64_t* positions, void* stream);
 
 /* Waits for the stream and returns what the kernels reported since the last report: PS_OK,
  * PS_ERR_INVALID (a slot outside the cache) or PS_ERR_TIMEOUT (a bounded wait of the attention gave up;
@@ -114,6 +171,13 @@ PS_API ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_que
 PS_API ps_status ps_kv_plan_set(ps_kv_plan* plan, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
                                 const uint32_t* blocks, uint64_t num_blocks);
 
+/* ps_kv_plan_set for a batch in which spans may also have causal = 2: masked.  Such a span's last num_queries tokens
+ * (it has at least so many) are its queries' own, as a causal one's; the tokens before them are seen by all its queries,
+ * and which of its own a query sees is a row of the mask that ps_kv_attend_masked takes: a tree of drafted tokens.
+ * The paper has no counterpart.  Errors: as ps_kv_plan_set. */
+PS_API ps_status ps_kv_plan_set_masked(ps_kv_plan* plan, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
+                                       const uint32_t* blocks, uint64_t num_blocks);
+
 /* Bytes of workspace that ps_kv_attend needs for the batch that is set (0 possible).
  * The paper has no counterpart. */
 PS_API ps_status ps_kv_plan_workspace(ps_kv_plan* plan, uint64_t* bytes);
@@ -132,6 +196,16 @@ PS_API ps_status ps_kv_plan_workspace(ps_kv_plan* plan, uint64_t* bytes);
  * Errors: PS_ERR_INVALID, PS_ERR_STATE (no batch is set), PS_ERR_CUDA. */
 PS_API ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,
                               float scale, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* ps_kv_attend of a batch with masked spans.  mask: device memory, a row of mask_words 32-bit words per query of the batch,
+ * rows mask_stride words apart (4-byte aligned): bit j of query i's row (bit j % 32 of word j / 32) is set where i sees
+ * token j of its masked span's own ones, the span's length - num_queries + j-th.  Bits past the span's queries and rows of
+ * queries without a masked span are not looked at; 32 * mask_words is at least the queries of the longest masked span.
+ * Any mask will do: a query need not see itself, nor anything.  The paper has no counterpart.
+ * Errors: as ps_kv_attend, which refuses such a batch. */
+PS_API ps_status ps_kv_attend_masked(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,
+                                     float scale, const uint32_t* mask, int64_t mask_stride, uint32_t mask_words,
+                                     void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Text of the last error of this cache's calls, its plans' among them ("" if none).
  * The paper has no counterpart. */

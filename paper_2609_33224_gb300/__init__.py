@@ -29,8 +29,10 @@ ABI_FUNCTIONS = ("ps_create", "ps_load_instances", "ps_get_instances", "ps_get_p
                  "ps_schedule_window", "ps_commit_window", "ps_last_timings", "ps_last_probe_stats", "ps_last_error",
                  "ps_destroy", "ps_score_window_noalloc", "ps_load_requests", "ps_advance_window",
                  "ps_shard_wmin", "ps_shard_pick",
-                 "ps_kv_create", "ps_kv_write", "ps_kv_read", "ps_kv_check", "ps_kv_plan_create", "ps_kv_plan_set",
-                 "ps_kv_plan_workspace", "ps_kv_attend", "ps_kv_last_error", "ps_kv_plan_destroy", "ps_kv_destroy")
+                 "ps_kv_create", "ps_kv_write", "ps_kv_write_rotated", "ps_kv_read", "ps_kv_move", "ps_kv_move_workspace",
+                 "ps_kv_copy_blocks", "ps_kv_tree_mask", "ps_kv_check", "ps_kv_plan_create", "ps_kv_plan_set",
+                 "ps_kv_plan_set_masked", "ps_kv_plan_workspace", "ps_kv_attend", "ps_kv_attend_masked",
+                 "ps_kv_last_error", "ps_kv_plan_destroy", "ps_kv_destroy")
 
 
 class PsModel(ctypes.Structure):
@@ -103,6 +105,11 @@ class PsKvConfig(ctypes.Structure):
                 ("head_dim", ctypes.c_uint32), ("format", ctypes.c_int32)]
 
 
+class PsKvRotary(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_uint32), ("interleaved", ctypes.c_uint32), ("magnitude", ctypes.c_float),
+                ("frequency", ctypes.c_double * 64)]
+
+
 class PsKvRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
                 ("type", ctypes.c_int32)]
@@ -153,11 +160,18 @@ def lib() -> ctypes.CDLL:
             "ps_kv_create": [ctypes.POINTER(PsKvConfig), ctypes.POINTER(vp)],
             "ps_kv_write": [vp, vp, vp, vp, u64, vp],  # the two ps_kv_rows by address
             "ps_kv_read": [vp, vp, u64, vp, vp, vp],
+            "ps_kv_write_rotated": [vp, vp, vp, vp, vp, u32, vp, vp, vp, u64, vp],
+            "ps_kv_move": [vp, vp, vp, u64, vp, u64, vp],
+            "ps_kv_move_workspace": [vp, u64, ctypes.POINTER(u64)],
+            "ps_kv_copy_blocks": [vp, vp, vp, vp, u64, vp],
+            "ps_kv_tree_mask": [vp, vp, u64, vp, u32, vp, vp, ctypes.c_int64, u32, vp, vp],
             "ps_kv_check": [vp, vp],
             "ps_kv_plan_create": [vp, u32, u32, u32, u64, ctypes.POINTER(vp)],
             "ps_kv_plan_set": [vp, u32, vp, u32, vp, u64],
+            "ps_kv_plan_set_masked": [vp, u32, vp, u32, vp, u64],
             "ps_kv_plan_workspace": [vp, ctypes.POINTER(u64)],
             "ps_kv_attend": [vp, vp, vp, vp, vp, ctypes.c_float, vp, u64, vp],
+            "ps_kv_attend_masked": [vp, vp, vp, vp, vp, ctypes.c_float, vp, ctypes.c_int64, u32, vp, u64, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)

@@ -59,6 +59,7 @@ struct ps_kv_plan {
   uint32_t queries = 0;
   uint64_t part_rows = 0;
   uint32_t top_block = 0;
+  uint32_t masked = 0;  // queries of the longest masked span
 };
 
 namespace {
@@ -152,7 +153,8 @@ ps_status reported(ps_kv* kv) {
   const uint32_t e = __atomic_exchange_n(kv->err_host, 0u, __ATOMIC_ACQ_REL);
   if (e & pskv::kErrWait)
     return fail(kv, PS_ERR_TIMEOUT, "a bounded device-side wait of an earlier attention call gave up");
-  return fail(kv, PS_ERR_INVALID, "an earlier write or read named a slot outside the cache");
+  if (e & pskv::kErrSlot) return fail(kv, PS_ERR_INVALID, "an earlier call named a slot or block outside the cache");
+  return fail(kv, PS_ERR_INVALID, "an earlier call's trees had a parent that is no node before its child, or wrong offsets");
 }
 
 size_t elem_size(int type) { return type == PS_KV_FP32 ? 4 : 2; }
@@ -263,17 +265,19 @@ ps_status grow(ps_kv* kv, ps_kv_plan::Buffer& b, size_t need) {
 }
 
 ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t n_spans, const uint32_t* blocks,
-                   uint64_t n_blocks) {
+                   uint64_t n_blocks, bool may_mask) {
   ps_kv* kv = pl->kv;
   pl->set = false;
   if (T > pl->max_queries) return fail(kv, PS_ERR_INVALID, "more queries than max_queries");
   if (n_spans > pl->max_spans) return fail(kv, PS_ERR_INVALID, "more spans than max_spans");
   if (n_blocks > pl->max_blocks) return fail(kv, PS_ERR_INVALID, "more block ids than max_blocks");
   if ((n_spans && !spans) || (n_blocks && !blocks)) return fail(kv, PS_ERR_INVALID, "spans or blocks is NULL");
+  uint32_t masked = 0;
   uint64_t seen = 0;  // (query, layer) pairs of the layout: a span may become two layers
   for (uint32_t i = 0; i < n_spans; ++i) {
     const ps_kv_span& s = spans[i];
-    if (s.causal > 1) return fail(kv, PS_ERR_INVALID, "a span's causal must be 0 or 1");
+    if (s.causal > 1 && !(may_mask && s.causal == pskv::kMasked))
+      return fail(kv, PS_ERR_INVALID, may_mask ? "a span's causal must be 0, 1 or 2" : "a span's causal must be 0 or 1");
     if (s.first_query > T || s.num_queries > T - s.first_query)
       return fail(kv, PS_ERR_INVALID, "a span's queries must lie inside the batch");
     if (s.length >= (1ull << 30)) return fail(kv, PS_ERR_INVALID, "a span's length must be < 2^30");
@@ -281,6 +285,10 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
     if (s.first_block > n_blocks || nb > n_blocks - s.first_block)
       return fail(kv, PS_ERR_INVALID, "a span's blocks must lie inside the block array");
     if (s.length) seen += 2ull * s.num_queries;
+    if (s.causal == pskv::kMasked) {
+      if (s.length < s.num_queries) return fail(kv, PS_ERR_INVALID, "a masked span has its queries' tokens at least");
+      masked = std::max(masked, s.num_queries);
+    }
   }
   if (seen >= 0xFFFFFF00ull) return fail(kv, PS_ERR_INVALID, "the batch is too large for one plan");
   uint32_t top = 0;
@@ -341,6 +349,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   pl->queries = T;
   pl->part_rows = o.part_rows;
   pl->top_block = n_blocks ? top : 0;
+  pl->masked = masked;
   pl->set = true;
   return PS_OK;
 }
@@ -348,6 +357,121 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
 uint64_t workspace_bytes(const ps_kv_plan* pl) {
   const uint64_t ml = (pl->part_rows * sizeof(float2) + 255) / 256 * 256;
   return ml + pl->part_rows * pl->kv->D * sizeof(float);
+}
+
+ps_status set_plan(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t n_spans, const uint32_t* blocks,
+                   uint64_t n_blocks, bool may_mask) {
+  if (!pl) return PS_ERR_INVALID;
+  if (pl->buf[pl->cur].mem->refs.load(std::memory_order_acquire) > 1)  // the other buffer was last set before this one
+    return fail(pl->kv, PS_ERR_STATE, "a CUDA graph holds this plan's arrays: make another plan");
+  OnDevice on(pl->kv->device);
+  try {
+    return plan_set(pl, T, spans, n_spans, blocks, n_blocks, may_mask);
+  } catch (...) {
+    pl->set = false;
+    return fail(pl->kv, PS_ERR_OOM, "no host memory for the plan");
+  }
+}
+
+ps_status attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_kv_rows* out, float* lse, float scale,
+                 const uint32_t* mask, int64_t mask_stride, uint32_t mask_words, void* workspace, uint64_t bytes,
+                 void* stream) {
+  if (!kv) return PS_ERR_INVALID;
+  ps_status st = reported(kv);
+  if (st != PS_OK) return st;
+  if (!pl) return fail(kv, PS_ERR_INVALID, "plan is NULL");
+  if (!pl->set) return fail(kv, PS_ERR_STATE, "no batch is set");
+  if (kv != pl->kv && (kv->device != pl->kv->device || kv->heads != pl->kv->heads || kv->D != pl->kv->D ||
+                       kv->fmt != pl->kv->fmt || kv->blocks <= pl->top_block))
+    return fail(kv, PS_ERR_INVALID, "the plan was made for a cache of another shape");
+  const uint32_t T = pl->queries;
+  const char* m = rows_error(q, pl->q_heads, T);
+  if (!m) m = rows_error(out, pl->q_heads, T);
+  const int want = kv->fmt == PS_KV_FP16 ? PS_KV_FP16 : PS_KV_BF16;
+  if (!m && (q->type != want || out->type != want)) m = "q and out must have the cache's 16-bit type (bf16 with fp8)";
+  if (!m && rows_overlap(out, T, pl->q_heads, kv->D)) m = "rows of a result overlap";
+  if (!m && lse && reinterpret_cast<uintptr_t>(lse) % 4) m = "lse must start on a 4-byte boundary";
+  if (!m && !std::isfinite(scale)) m = "scale must be finite";
+  if (!m && pl->masked && !mask) m = "the batch has masked spans: it needs a mask";
+  if (!m && pl->masked && reinterpret_cast<uintptr_t>(mask) % 4) m = "the mask must start on a 4-byte boundary";
+  if (!m && pl->masked > 32ull * mask_words) m = "the mask's rows are shorter than a masked span's queries";
+  const uint64_t need = workspace_bytes(pl);
+  if (!m && need && (!workspace || bytes < need)) m = "the workspace is smaller than ps_kv_plan_workspace says";
+  if (!m && need && reinterpret_cast<uintptr_t>(workspace) % 256) m = "the workspace must start on a 256-byte boundary";
+  if (m) return fail(kv, PS_ERR_INVALID, m);
+  if (T == 0) return PS_OK;
+  OnDevice on(kv->device);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  Capture cap;
+  KV_CUDA(kv, cap.look(s));
+  ps_kv_plan::Buffer& b = pl->buf[pl->cur];
+  const bool capturing = cap.on();
+  if (capturing) {
+    KV_CUDA(kv, cap.keep(kv->mem));
+    KV_CUDA(kv, cap.keep(b.mem));
+  } else if (b.in_use && b.last != s) {  // so that the last call's stream stands for all calls before it
+    KV_CUDA(kv, mark_used(b));
+    KV_CUDA(kv, cudaStreamWaitEvent(s, b.used, 0));
+  }
+
+  pskv::AttnArgs a{};
+  a.pool = kv->pool;
+  a.q = static_cast<const uint16_t*>(q->data);
+  a.q_tok = q->token_stride;
+  a.q_head = q->head_stride;
+  a.out = static_cast<uint16_t*>(out->data);
+  a.o_tok = out->token_stride;
+  a.o_head = out->head_stride;
+  a.lse = lse;
+  a.part_ml = static_cast<float2*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (need - pl->part_rows * kv->D * sizeof(float)));
+  a.kv_heads = kv->heads;
+  a.group = pl->group;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.err = kv->err_dev;
+  a.mask = mask;
+  a.mask_stride = mask_stride;
+  const int D = (int)kv->D;
+  cudaError_t e = cudaSuccess;
+  // In a graph the first kernel, the join of a batch without a key too, follows whatever node it has to: it takes the
+  // plain dependency.
+  a.rows_first = pl->dev.tile_workers == 0;
+  if (pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, !capturing, s);
+  if (e == cudaSuccess && pl->dev.row_workers)
+    e = pskv::launch_rows(D, kv->fmt, pl->masked != 0, a, pl->dev, pl->dev.tile_workers != 0 || !capturing, s);
+  if (e == cudaSuccess && pl->dev.njoin)
+    e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev,
+                          pl->dev.tile_workers || pl->dev.row_workers || !capturing, s);
+  if (!capturing) {  // also after a failed launch: the ones before it read the buffer
+    b.in_use = true;
+    b.recorded = false;
+    b.last = s;
+  }
+  if (e != cudaSuccess) return fail_cuda(kv, "ps_kv_attend", e);
+  return PS_OK;
+}
+
+// What a call on the cache does before its kernels: the reports of earlier ones, and a graph's reference to its memory.
+ps_status begin(ps_kv* kv, cudaStream_t s, Memory* also = nullptr) {
+  Capture cap;
+  KV_CUDA(kv, cap.look(s));
+  KV_CUDA(kv, cap.keep(kv->mem));
+  if (also && also != kv->mem) KV_CUDA(kv, cap.keep(also));
+  return PS_OK;
+}
+
+const char* vector_error(const void* p, uint64_t n, const char* null, const char* odd, size_t align = 8) {
+  if (n > 0 && !p) return null;
+  return n > 0 && reinterpret_cast<uintptr_t>(p) % align ? odd : nullptr;
+}
+
+// A frequency as turns per position, in 2^-64 of a turn.
+uint64_t turns_of(double frequency) {
+  double t = frequency / 6.283185307179586476925;
+  t -= std::floor(t);  // [0, 1], as exact as t
+  const double hi = std::floor(std::ldexp(t, 32)), lo = std::ldexp(std::ldexp(t, 32) - hi, 32);
+  // parts that round up to 2^32 carry, and a whole turn is none
+  return ((uint64_t)hi << 32) + (uint64_t)std::nearbyint(lo);
 }
 
 }  // namespace
@@ -436,6 +560,139 @@ ps_status ps_kv_read(ps_kv* kv, const int64_t* slots, uint64_t n, const ps_kv_ro
   return PS_OK;
 }
 
+ps_status ps_kv_write_rotated(ps_kv* kv, const ps_kv_rotary* ro, const int64_t* positions, const ps_kv_rows* q,
+                              const ps_kv_rows* q_out, uint32_t q_heads, const ps_kv_rows* k, const ps_kv_rows* v,
+                              const int64_t* slots, uint64_t n, void* stream) {
+  if (!kv) return PS_ERR_INVALID;
+  ps_status st = reported(kv);
+  if (st != PS_OK) return st;
+  const char* m = nullptr;
+  if (!ro) m = "rotary is NULL";
+  if (!m && (ro->dims < 16 || ro->dims % 16 || ro->dims > kv->D)) m = "dims must be a multiple of 16, at most head_dim";
+  if (!m && ro->interleaved > 1) m = "interleaved must be 0 or 1";
+  if (!m && !std::isfinite(ro->magnitude)) m = "magnitude must be finite";
+  for (uint32_t i = 0; !m && i < ro->dims / 2; ++i)
+    if (!std::isfinite(ro->frequency[i])) m = "frequencies must be finite";
+  if (!m) m = vector_error(positions, n, "positions is NULL", "positions must start on an 8-byte boundary");
+  if (!m && (!q != !q_out || !q != !q_heads)) m = "q, q_out and q_heads come together";
+  if (!m && q_heads > 65535) m = "q_heads must be at most 65535";
+  if (!m && q) m = rows_error(q, q_heads, n);
+  if (!m && q) m = rows_error(q_out, q_heads, n);
+  const int want = kv->fmt == PS_KV_FP16 ? PS_KV_FP16 : PS_KV_BF16;
+  if (!m && q && q_out->type != want) m = "q_out must have the cache's 16-bit type (bf16 with fp8)";
+  if (!m && q && rows_overlap(q_out, n, q_heads, kv->D)) m = "rows of a result overlap";
+  if (m) return fail(kv, PS_ERR_INVALID, m);
+  pskv::RotateArgs a{};
+  st = store_args(kv, k, v, slots, n, false, &a.s);
+  if (st != PS_OK) return st;
+  if (q && q->type != k->type) return fail(kv, PS_ERR_INVALID, "q, k and v must have one element type");
+  if (n == 0) return PS_OK;
+  if (q) {
+    a.q = q->data;
+    a.q_tok = q->token_stride;
+    a.q_head = q->head_stride;
+    a.q_out = q_out->data;
+    a.o_tok = q_out->token_stride;
+    a.o_head = q_out->head_stride;
+    a.q_heads = q_heads;
+  }
+  a.positions = positions;
+  a.dims = ro->dims;
+  a.interleaved = ro->interleaved;
+  a.magnitude = ro->magnitude;
+  for (uint32_t i = 0; i < ro->dims / 2; ++i) a.turns[i] = turns_of(ro->frequency[i]);
+  OnDevice on(kv->device);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  st = begin(kv, s);
+  if (st != PS_OK) return st;
+  KV_CUDA(kv, pskv::launch_write_rotated((int)kv->D, kv->fmt, k->type, a, kv->sms, s));
+  return PS_OK;
+}
+
+ps_status ps_kv_move_workspace(ps_kv* kv, uint64_t n, uint64_t* bytes) {
+  if (!kv) return PS_ERR_INVALID;
+  if (!bytes) return fail(kv, PS_ERR_INVALID, "bytes is NULL");
+  if (n > (1ull << 40)) return fail(kv, PS_ERR_INVALID, "too many tokens");
+  *bytes = pskv::move_space((int)kv->D, kv->fmt, kv->heads, n);
+  return PS_OK;
+}
+
+ps_status ps_kv_move(ps_kv* kv, const int64_t* src, const int64_t* dst, uint64_t n, void* workspace, uint64_t bytes,
+                     void* stream) {
+  if (!kv) return PS_ERR_INVALID;
+  ps_status st = reported(kv);
+  if (st != PS_OK) return st;
+  const char* m = vector_error(src, n, "src is NULL", "src must start on an 8-byte boundary");
+  if (!m) m = vector_error(dst, n, "dst is NULL", "dst must start on an 8-byte boundary");
+  if (!m && n > (1ull << 40)) m = "too many tokens";
+  const uint64_t need = m ? 0 : pskv::move_space((int)kv->D, kv->fmt, kv->heads, n);
+  if (!m && need && (!workspace || bytes < need)) m = "the workspace is smaller than ps_kv_move_workspace says";
+  if (!m && need && reinterpret_cast<uintptr_t>(workspace) % 256) m = "the workspace must start on a 256-byte boundary";
+  if (m) return fail(kv, PS_ERR_INVALID, m);
+  if (n == 0) return PS_OK;
+  OnDevice on(kv->device);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  st = begin(kv, s);
+  if (st != PS_OK) return st;
+  const pskv::MoveArgs a{kv->pool, src, dst, n, kv->blocks * pskv::kBlock, kv->heads, static_cast<uint4*>(workspace),
+                         kv->err_dev};
+  KV_CUDA(kv, pskv::launch_move((int)kv->D, kv->fmt, a, kv->sms, s));
+  return PS_OK;
+}
+
+ps_status ps_kv_copy_blocks(ps_kv* kv, ps_kv* from, const int64_t* src, const int64_t* dst, uint64_t n, void* stream) {
+  if (!kv) return PS_ERR_INVALID;
+  ps_status st = reported(kv);
+  if (st != PS_OK) return st;
+  const char* m = vector_error(src, n, "src is NULL", "src must start on an 8-byte boundary");
+  if (!m) m = vector_error(dst, n, "dst is NULL", "dst must start on an 8-byte boundary");
+  if (!m && n > (1ull << 40)) m = "too many blocks";
+  if (!m && !from) m = "from is NULL";
+  if (!m && (from->device != kv->device || from->heads != kv->heads || from->D != kv->D || from->fmt != kv->fmt))
+    m = "blocks are copied between caches of one device, heads, head_dim and format";
+  if (m) return fail(kv, PS_ERR_INVALID, m);
+  if (n == 0) return PS_OK;
+  OnDevice on(kv->device);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  st = begin(kv, s, from->mem);
+  if (st != PS_OK) return st;
+  const uint32_t chunks = kv->heads * (uint32_t)pskv::record_bytes((int)kv->D, kv->fmt) / 16;
+  const pskv::CopyArgs a{kv->pool, from->pool, src, dst, n, kv->blocks, from->blocks, chunks, 1, kv->err_dev};
+  KV_CUDA(kv, pskv::launch_copy(a, kv->sms, s));
+  return PS_OK;
+}
+
+ps_status ps_kv_tree_mask(ps_kv* kv, const int32_t* parents, uint64_t num_nodes, const int64_t* offsets, uint32_t num_trees,
+                          const int64_t* start, uint32_t* mask, int64_t mask_stride, uint32_t words, int64_t* positions,
+                          void* stream) {
+  if (!kv) return PS_ERR_INVALID;
+  ps_status st = reported(kv);
+  if (st != PS_OK) return st;
+  const char* m = vector_error(parents, num_nodes, "parents is NULL", "parents must start on a 4-byte boundary", 4);
+  if (!m) m = vector_error(mask, num_nodes, "mask is NULL", "mask must start on a 4-byte boundary", 4);
+  if (!m && reinterpret_cast<uintptr_t>(offsets) % 8) m = "offsets must start on an 8-byte boundary";
+  if (!m && reinterpret_cast<uintptr_t>(start) % 8) m = "start must start on an 8-byte boundary";
+  if (!m && reinterpret_cast<uintptr_t>(positions) % 8) m = "positions must start on an 8-byte boundary";
+  if (!m && (words < 1 || words > 256)) m = "words must be in 1..256";
+  if (!m && num_nodes > (1ull << 40)) m = "too many nodes";
+  if (!m && num_trees >= (1u << 31)) m = "too many trees";
+  if (!m && num_nodes > 0 && num_trees == 0) m = "nodes without a tree";
+  if (!m && !offsets && num_trees && num_nodes % num_trees) m = "without offsets all trees have the same number of nodes";
+  if (!m && !offsets && num_trees && num_nodes / num_trees > 32ull * words) m = "the trees have more than 32 * words nodes";
+  if (!m && num_nodes > 1 && (mask_stride < 0 ? 0 - (uint64_t)mask_stride : (uint64_t)mask_stride) < words)
+    m = "rows of a result overlap";
+  if (m) return fail(kv, PS_ERR_INVALID, m);
+  if (num_nodes == 0) return PS_OK;
+  OnDevice on(kv->device);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  st = begin(kv, s);
+  if (st != PS_OK) return st;
+  const pskv::TreeArgs a{parents, offsets, start, mask, positions, mask_stride, num_nodes, num_nodes / num_trees, words,
+                         kv->err_dev};
+  KV_CUDA(kv, pskv::launch_tree(a, num_trees, s));
+  return PS_OK;
+}
+
 ps_status ps_kv_check(ps_kv* kv, void* stream) {
   if (!kv) return PS_ERR_INVALID;
   OnDevice on(kv->device);
@@ -477,16 +734,12 @@ ps_status ps_kv_plan_create(ps_kv* kv, uint32_t q_heads, uint32_t max_queries, u
 
 ps_status ps_kv_plan_set(ps_kv_plan* pl, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
                          const uint32_t* blocks, uint64_t num_blocks) {
-  if (!pl) return PS_ERR_INVALID;
-  if (pl->buf[pl->cur].mem->refs.load(std::memory_order_acquire) > 1)  // the other buffer was last set before this one
-    return fail(pl->kv, PS_ERR_STATE, "a CUDA graph holds this plan's arrays: make another plan");
-  OnDevice on(pl->kv->device);
-  try {
-    return plan_set(pl, num_queries, spans, num_spans, blocks, num_blocks);
-  } catch (...) {
-    pl->set = false;
-    return fail(pl->kv, PS_ERR_OOM, "no host memory for the plan");
-  }
+  return set_plan(pl, num_queries, spans, num_spans, blocks, num_blocks, false);
+}
+
+ps_status ps_kv_plan_set_masked(ps_kv_plan* pl, uint32_t num_queries, const ps_kv_span* spans, uint32_t num_spans,
+                                const uint32_t* blocks, uint64_t num_blocks) {
+  return set_plan(pl, num_queries, spans, num_spans, blocks, num_blocks, true);
 }
 
 ps_status ps_kv_plan_workspace(ps_kv_plan* pl, uint64_t* bytes) {
@@ -499,74 +752,13 @@ ps_status ps_kv_plan_workspace(ps_kv_plan* pl, uint64_t* bytes) {
 
 ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_kv_rows* out, float* lse, float scale,
                        void* workspace, uint64_t bytes, void* stream) {
-  if (!kv) return PS_ERR_INVALID;
-  ps_status st = reported(kv);
-  if (st != PS_OK) return st;
-  if (!pl) return fail(kv, PS_ERR_INVALID, "plan is NULL");
-  if (!pl->set) return fail(kv, PS_ERR_STATE, "no batch is set");
-  if (kv != pl->kv && (kv->device != pl->kv->device || kv->heads != pl->kv->heads || kv->D != pl->kv->D ||
-                       kv->fmt != pl->kv->fmt || kv->blocks <= pl->top_block))
-    return fail(kv, PS_ERR_INVALID, "the plan was made for a cache of another shape");
-  const uint32_t T = pl->queries;
-  const char* m = rows_error(q, pl->q_heads, T);
-  if (!m) m = rows_error(out, pl->q_heads, T);
-  const int want = kv->fmt == PS_KV_FP16 ? PS_KV_FP16 : PS_KV_BF16;
-  if (!m && (q->type != want || out->type != want)) m = "q and out must have the cache's 16-bit type (bf16 with fp8)";
-  if (!m && rows_overlap(out, T, pl->q_heads, kv->D)) m = "rows of a result overlap";
-  if (!m && lse && reinterpret_cast<uintptr_t>(lse) % 4) m = "lse must start on a 4-byte boundary";
-  if (!m && !std::isfinite(scale)) m = "scale must be finite";
-  const uint64_t need = workspace_bytes(pl);
-  if (!m && need && (!workspace || bytes < need)) m = "the workspace is smaller than ps_kv_plan_workspace says";
-  if (!m && need && reinterpret_cast<uintptr_t>(workspace) % 256) m = "the workspace must start on a 256-byte boundary";
-  if (m) return fail(kv, PS_ERR_INVALID, m);
-  if (T == 0) return PS_OK;
-  OnDevice on(kv->device);
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  Capture cap;
-  KV_CUDA(kv, cap.look(s));
-  ps_kv_plan::Buffer& b = pl->buf[pl->cur];
-  const bool capturing = cap.on();
-  if (capturing) {
-    KV_CUDA(kv, cap.keep(kv->mem));
-    KV_CUDA(kv, cap.keep(b.mem));
-  } else if (b.in_use && b.last != s) {  // so that the last call's stream stands for all calls before it
-    KV_CUDA(kv, mark_used(b));
-    KV_CUDA(kv, cudaStreamWaitEvent(s, b.used, 0));
-  }
+  return attend(kv, pl, q, out, lse, scale, nullptr, 0, 0, workspace, bytes, stream);
+}
 
-  pskv::AttnArgs a{};
-  a.pool = kv->pool;
-  a.q = static_cast<const uint16_t*>(q->data);
-  a.q_tok = q->token_stride;
-  a.q_head = q->head_stride;
-  a.out = static_cast<uint16_t*>(out->data);
-  a.o_tok = out->token_stride;
-  a.o_head = out->head_stride;
-  a.lse = lse;
-  a.part_ml = static_cast<float2*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (need - pl->part_rows * kv->D * sizeof(float)));
-  a.kv_heads = kv->heads;
-  a.group = pl->group;
-  a.scale_log2 = scale * 1.4426950408889634f;
-  a.err = kv->err_dev;
-  const int D = (int)kv->D;
-  cudaError_t e = cudaSuccess;
-  // In a graph the first kernel, the join of a batch without a key too, follows whatever node it has to: it takes the
-  // plain dependency.
-  a.rows_first = pl->dev.tile_workers == 0;
-  if (pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, !capturing, s);
-  if (e == cudaSuccess && pl->dev.row_workers)
-    e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0 || !capturing, s);
-  if (e == cudaSuccess && pl->dev.njoin)
-    e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev,
-                          pl->dev.tile_workers || pl->dev.row_workers || !capturing, s);
-  if (!capturing) {  // also after a failed launch: the ones before it read the buffer
-    b.in_use = true;
-    b.recorded = false;
-    b.last = s;
-  }
-  if (e != cudaSuccess) return fail_cuda(kv, "ps_kv_attend", e);
-  return PS_OK;
+ps_status ps_kv_attend_masked(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,
+                              float scale, const uint32_t* mask, int64_t mask_stride, uint32_t mask_words, void* workspace,
+                              uint64_t bytes, void* stream) {
+  return attend(kv, pl, q, out, lse, scale, mask, mask_stride, mask_words, workspace, bytes, stream);
 }
 
 const char* ps_kv_last_error(const ps_kv* kv) { return kv ? kv->err.c_str() : ""; }

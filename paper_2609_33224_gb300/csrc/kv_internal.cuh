@@ -26,7 +26,7 @@ namespace pskv {
 constexpr int kExpBias = 127;
 constexpr int kExpMin = -110, kExpMax = 119, kExpNan = 255;
 
-enum : uint32_t { kErrSlot = 1u, kErrWait = 2u };
+enum : uint32_t { kErrSlot = 1u, kErrWait = 2u, kErrTree = 4u };
 
 __host__ __device__ constexpr int record_bytes(int D, int fmt) {
   return fmt == PS_KV_FP8 ? 2 * kBlock * D + 2 * kBlock : 2 * kBlock * D * 2;
@@ -74,6 +74,8 @@ struct AttnArgs {
   float2* part_ml;  // [part row] maximum (of the scores times log2 e) and sum
   uint32_t kv_heads, group;
   float scale_log2;
+  const uint32_t* mask;  // [query][mask_stride]: which of their own tokens the queries of masked spans see
+  int64_t mask_stride;
   uint32_t rows_first;  // the row kernel is the call's first: it waits for what came before
   uint32_t* err;  // mapped host word
 };
@@ -90,9 +92,62 @@ struct StoreArgs {
   uint32_t* err;
 };
 
+struct RotateArgs {
+  StoreArgs s;
+  const void* q;
+  void* q_out;
+  int64_t q_tok, q_head, o_tok, o_head;
+  uint32_t q_heads;
+  uint32_t dims, interleaved;
+  float magnitude;
+  uint32_t shares;  // warps of a token
+  const int64_t* positions;
+  uint64_t turns[64];  // a pair's turns per position, in 2^-64
+};
+
+struct MoveArgs {
+  uint8_t* pool;
+  const int64_t* src;
+  const int64_t* dst;
+  uint64_t n;
+  uint64_t num_slots;
+  uint32_t kv_heads;
+  uint4* space;
+  uint32_t* err;
+};
+
+struct CopyArgs {
+  uint8_t* pool;
+  const uint8_t* from;
+  const int64_t* src;
+  const int64_t* dst;
+  uint64_t n;
+  uint64_t num_blocks, from_blocks;
+  uint32_t chunks;  // 16-byte chunks of a block
+  uint32_t parts;   // that a block is copied in
+  uint32_t* err;
+};
+
+struct TreeArgs {
+  const int32_t* parents;
+  const int64_t* offsets;
+  const int64_t* start;
+  uint32_t* mask;
+  int64_t* positions;
+  int64_t stride;
+  uint64_t nodes, each;
+  uint32_t words;
+  uint32_t* err;
+};
+
 cudaError_t launch_write(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_read(int D, int fmt, int type, const StoreArgs& a, int sms, cudaStream_t s);
-cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
+cudaError_t launch_write_rotated(int D, int fmt, int type, const RotateArgs& a, int sms, cudaStream_t s);
+uint64_t move_space(int D, int fmt, uint32_t heads, uint64_t n);  // bytes of workspace
+cudaError_t launch_move(int D, int fmt, const MoveArgs& a, int sms, cudaStream_t s);
+cudaError_t launch_copy(CopyArgs a, int sms, cudaStream_t s);
+cudaError_t launch_tree(const TreeArgs& a, uint32_t trees, cudaStream_t s);
+cudaError_t launch_rows(int D, int fmt, bool masked, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);

@@ -44,11 +44,12 @@ struct alignas(16) Piece {
   uint16_t nrows;
   uint16_t head;
   uint32_t fold0, nfold;  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in
-  uint32_t split;  // tile kernel: not 0: its even steps in tile 0, its odd ones in tile 1, so many rows behind
+  uint32_t split;  // row kernel: 1: of a masked span, own tokens from climit on; tile kernel: not 0: its even steps in tile 0, its odd ones in tile 1, so many rows behind
 };
 static_assert(sizeof(Piece) == 48, "Piece layout");
 constexpr uint32_t kDirect = 0xFFFFFFFFu;
 constexpr int32_t kNoLimit = 0x3FFFFFFF;
+constexpr uint32_t kMasked = 2;  // ps_kv_span.causal of a masked span
 
 // What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments
 // segs[seg0] ..: the i-th row's are the partial rows row + i + k * stride, k < nparts.  The join kernel gives every entry
@@ -245,7 +246,8 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   // The keys that all rows of a tile see, where the tile kernel is the one to take them (else 0).
   auto cut_of = [&](const ps_kv_span& s, uint32_t r0, uint32_t nr) -> int64_t {
     int64_t c = (int64_t)s.length;
-    if (s.causal) c = std::max<int64_t>(0, c - (int64_t)s.num_queries + r0 / g + 1) / kBlock * kBlock;
+    if (s.causal == 1) c = std::max<int64_t>(0, c - (int64_t)s.num_queries + r0 / g + 1) / kBlock * kBlock;
+    if (s.causal == kMasked) c = (c - (int64_t)s.num_queries) / kBlock * kBlock;
     return tile_saves(pl, nr, c, s.causal != 0) > 0 ? c : 0;
   };
   auto tiles_save = [&](const ps_kv_span& s) {
@@ -289,9 +291,12 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     for (uint32_t r0 = 0; r0 < rows; r0 += kSmallRows) {
       const uint32_t nr = std::min<uint32_t>(rows - r0, kSmallRows);
       const int64_t from = cut.empty() ? 0 : cut[r0 / tile_rows];
-      const int64_t end = s.causal ? std::min<int64_t>(len, (int64_t)climit + (r0 + nr - 1) / g + 1) : len;
+      const int64_t end = s.causal == 1 ? std::min<int64_t>(len, (int64_t)climit + (r0 + nr - 1) / g + 1) : len;
       for (uint32_t h = 0; h < H; ++h) {
-        if (end > from) o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, o));
+        if (end > from) {
+          o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, o));
+          o.row_units.back().p.split = s.causal == kMasked;
+        }
         o.groups.push_back(Group{0, 0});
       }
     }
@@ -382,7 +387,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
       for (uint32_t k = a; k < b; ++k) {
         if (!rows && pl.D == 128 && p.nrows <= tile_rows_of(128) / 2 && pieces[k].nblocks >= kSplitSteps)
           pieces[k].split = units[i].tile_rows;
-        nparts += pieces[k].split ? 2 : 1;
+        nparts += !rows && pieces[k].split ? 2 : 1;
       }
       bool direct = nparts == 1;
       for (uint32_t q = p.row0 / g; direct && q <= (p.row0 + p.nrows - 1) / g; ++q) direct = alone[p.query0 + q];
@@ -397,7 +402,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
       o.max_parts = std::max(o.max_parts, nparts);
       for (uint32_t k = a; k < b; ++k) {
         pieces[k].part_row = (uint32_t)o.part_rows;
-        o.part_rows += units[i].tile_rows * (pieces[k].split ? 2 : 1);
+        o.part_rows += units[i].tile_rows * (!rows && pieces[k].split ? 2 : 1);
       }
     }
   };

@@ -120,12 +120,21 @@ struct Place {
 };
 enum Step { kDone, kTooFar, kGaveUp };
 
-// A worker's pieces from `pl` on.  kApart (fp8): the form for queries or value scales whose magnitudes lie far apart,
+// Bits `at` .. `at` + 15 of a mask row, which has bits 0 .. bits - 1, bits > at; those below 0 are set.
+__device__ __forceinline__ uint32_t mask16(const uint32_t* row, int32_t at, int32_t bits) {
+  if (at <= -(int32_t)kBlock) return 0xFFFFu;
+  if (at < 0) return (~(0xFFFFFFFFu << -at) | __ldg(row) << -at) & 0xFFFFu;
+  const uint32_t w = (uint32_t)at / 32;
+  const uint32_t lo = __ldg(row + w), hi = at % 32 > 16 && (int32_t)(w + 1) * 32 < bits ? __ldg(row + w + 1) : 0u;
+  return __funnelshift_r(lo, hi, (uint32_t)at % 32) & 0xFFFFu;
+}
+
+// A worker's pieces from `pl` on.  kMask: some are of masked spans.  kApart (fp8): the form for queries or value scales whose magnitudes lie far apart,
 // with keys, values, queries and probabilities in bf16, whose exponents reach as far as a float's; the other form leaves
 // it a piece (kTooFar), with nothing of it written, and the pieces after it.  5 requests of 131072 tokens, 256 queries on
 // 32768: 257 and 357 us, 166 and 248 by the other form.  The two are separate instances: as branches of a block they
 // cost the common form registers (178 and 260 us).
-template <int D, int FMT, bool kApart>
+template <int D, int FMT, bool kApart, bool kMask>
 __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, const uint32_t ring, const uint32_t bar,
                                            Place& pl) {
   constexpr bool kFp8 = FMT == PS_KV_FP8, kFp16 = FMT == PS_KV_FP16;
@@ -254,7 +263,8 @@ __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, 
     // the last key each of the two rows sees, and the last that all rows of the tile see
     const int32_t last = (int32_t)pc.end - 1;
     const int32_t lim_a = min(last, pc.climit + (int32_t)ta), lim_b = min(last, pc.climit + (int32_t)tb);
-    const int32_t lim_all = min(last, pc.climit + (int32_t)(pc.row0 / a.group));
+    const bool masked = kMask && pc.split != 0;
+    const int32_t lim_all = min(last, masked ? pc.climit - 1 : pc.climit + (int32_t)(pc.row0 / a.group));
 
     float acc[kTiles][4];
 #pragma unroll
@@ -390,14 +400,24 @@ __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, 
       const int32_t key0 = (int32_t)(pc.key0 + bi * kBlock);
       const bool edge = key0 + kBlock - 1 > lim_all;  // the same for the whole warp
       uint32_t bad = 0;                               // 16-bit formats: keys whose values are not all finite
+      uint32_t see_a = 0, see_b = 0;                  // masked: the block's keys that each row sees
+      if (kMask && masked && edge) {
+        const int32_t at = key0 - pc.climit, bits = last + 1 - pc.climit;
+        const uint32_t here = 0xFFFFu >> max(0, kBlock - 1 - (last - key0));
+        const uint32_t* mask = a.mask + (int64_t)pc.query0 * a.mask_stride;
+        if (va) see_a = mask16(mask + ta * a.mask_stride, at, bits) & here;
+        if (vb) see_b = mask16(mask + tb * a.mask_stride, at, bits) & here;
+      }
+      auto sees_a = [&](int32_t j) { return kMask && masked ? ((see_a >> (j - key0)) & 1u) != 0 : j <= lim_a; };
+      auto sees_b = [&](int32_t j) { return kMask && masked ? ((see_b >> (j - key0)) & 1u) != 0 : j <= lim_b; };
       if (edge) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int32_t j = key0 + n * 8 + (int32_t)t4 * 2 + i;
-            if (j > lim_a) s[n][i] = -INFINITY;
-            if (j > lim_b) s[n][2 + i] = -INFINITY;
+            if (!sees_a(j)) s[n][i] = -INFINITY;
+            if (!sees_b(j)) s[n][2 + i] = -INFINITY;
           }
         if constexpr (!kFp8) {
           // A masked key's probability is 0, but 0 times an infinity or a NaN is not: value rows past the
@@ -462,8 +482,8 @@ __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, 
             float fa = vs[2 * n + i], fb = fa;
             if (edge) {  // the scale of a masked row may be the mark of a NaN
               const int32_t j = key0 + n * 8 + (int32_t)t4 * 2 + i;
-              if (j > lim_a) fa = 0.0f;
-              if (j > lim_b) fb = 0.0f;
+              if (!sees_a(j)) fa = 0.0f;
+              if (!sees_b(j)) fb = 0.0f;
             }
             s[n][i] *= fa;
             s[n][2 + i] *= fb;
@@ -518,7 +538,7 @@ __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, 
               const float c0 = kk < 8 ? ((kk & 1) ? s[0][1] : s[0][0]) : ((kk & 1) ? s[1][1] : s[1][0]);
               const float c1 = kk < 8 ? ((kk & 1) ? s[0][3] : s[0][2]) : ((kk & 1) ? s[1][3] : s[1][2]);
               const float pa = __shfl_sync(0xFFFFFFFFu, c0, from), pb = __shfl_sync(0xFFFFFFFFu, c1, from);
-              const bool sa = key0 + (int32_t)kk <= lim_a, sb = key0 + (int32_t)kk <= lim_b;
+              const bool sa = sees_a(key0 + (int32_t)kk), sb = sees_b(key0 + (int32_t)kk);
 #pragma unroll
               for (int j = 0; j < kTiles; ++j) {
                 const uint32_t w = *reinterpret_cast<const uint32_t*>(vals + offset16(kk, j) + t4 * 4);
@@ -659,7 +679,7 @@ __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, 
   return kDone;
 }
 
-template <int D, int FMT>
+template <int D, int FMT, bool kMask>
 __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs a, const PlanDev p) {
   constexpr int kStages = ring_stages<D, FMT>(), kStage = stage_bytes<D, FMT>();
   extern __shared__ __align__(128) uint8_t smem[];
@@ -685,9 +705,9 @@ __global__ void __launch_bounds__(kRowWarps * 32, 1) rows_kernel(const AttnArgs 
     wait_for_last();
   }
   let_next_start();
-  const Step how = run_pieces<D, FMT, false>(a, p, ring, bar, pl);
+  const Step how = run_pieces<D, FMT, false, kMask>(a, p, ring, bar, pl);
   if constexpr (FMT == PS_KV_FP8)
-    if (how == kTooFar) run_pieces<D, FMT, true>(a, p, ring, bar, pl);
+    if (how == kTooFar) run_pieces<D, FMT, true, kMask>(a, p, ring, bar, pl);
   if (!pl.waited) wait_for_last();
 }
 
@@ -698,11 +718,15 @@ constexpr int smem_bytes() {
 
 template <int D, int FMT>
 cudaError_t prepare_one() {
-  return cudaFuncSetAttribute(rows_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FMT>());
+  const cudaError_t e =
+      cudaFuncSetAttribute(rows_kernel<D, FMT, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FMT>());
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(rows_kernel<D, FMT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FMT>());
 }
 template <int D, int FMT>
-cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
-  return launch(rows_kernel<D, FMT>, p.row_ctas, kRowWarps * 32, smem_bytes<D, FMT>(), 1, overlap, s, a, p);
+cudaError_t launch_one(bool masked, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
+  return launch(masked ? rows_kernel<D, FMT, true> : rows_kernel<D, FMT, false>, p.row_ctas, kRowWarps * 32,
+                smem_bytes<D, FMT>(), 1, overlap, s, a, p);
 }
 
 }  // namespace
@@ -717,14 +741,14 @@ cudaError_t prepare_rows(int D, int fmt) {
                              : prepare_one<64, PS_KV_FP8>();
 }
 
-cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
+cudaError_t launch_rows(int D, int fmt, bool masked, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   if (D == 128)
-    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, overlap, s)
-           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, overlap, s)
-                               : launch_one<128, PS_KV_FP8>(a, p, overlap, s);
-  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, overlap, s)
-         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, overlap, s)
-                             : launch_one<64, PS_KV_FP8>(a, p, overlap, s);
+    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(masked, a, p, overlap, s)
+           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(masked, a, p, overlap, s)
+                               : launch_one<128, PS_KV_FP8>(masked, a, p, overlap, s);
+  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(masked, a, p, overlap, s)
+         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(masked, a, p, overlap, s)
+                             : launch_one<64, PS_KV_FP8>(masked, a, p, overlap, s);
 }
 
 }  // namespace pskv
