@@ -343,6 +343,9 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.njoin = (uint32_t)o.join.size();
   d.join_stride = o.join_stride;
   d.max_parts = o.max_parts;
+  d.join_parts = o.join_parts;
+  d.mask_rows = o.mask_rows;
+  d.mask_tiles = o.mask_tiles;
   d.blocks = reinterpret_cast<const uint32_t*>(b.dev + bl);
   pl->dev = d;
   pl->cur ^= 1;
@@ -438,7 +441,7 @@ ps_status attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_kv_row
   a.rows_first = pl->dev.tile_workers == 0;
   if (pl->dev.tile_workers) e = pskv::launch_tiles(D, kv->fmt, a, pl->dev, !capturing, s);
   if (e == cudaSuccess && pl->dev.row_workers)
-    e = pskv::launch_rows(D, kv->fmt, pl->masked != 0, a, pl->dev, pl->dev.tile_workers != 0 || !capturing, s);
+    e = pskv::launch_rows(D, kv->fmt, a, pl->dev, pl->dev.tile_workers != 0 || !capturing, s);
   if (e == cudaSuccess && pl->dev.njoin)
     e = pskv::launch_join(D, kv->fmt == PS_KV_FP16, a, pl->dev,
                           pl->dev.tile_workers || pl->dev.row_workers || !capturing, s);
@@ -469,7 +472,7 @@ const char* vector_error(const void* p, uint64_t n, const char* null, const char
 uint64_t turns_of(double frequency) {
   double t = frequency / 6.283185307179586476925;
   t -= std::floor(t);  // [0, 1], as exact as t
-  const double hi = std::floor(std::ldexp(t, 32)), lo = std::ldexp(std::ldexp(t, 32) - hi, 32);
+  const double hi = std::floor(t * 0x1p32), lo = (t * 0x1p32 - hi) * 0x1p32;
   // parts that round up to 2^32 carry, and a whole turn is none
   return ((uint64_t)hi << 32) + (uint64_t)std::nearbyint(lo);
 }

@@ -59,7 +59,9 @@ struct PlanDev {
   const JoinSeg* segs;
   const Fold* folds;
   uint32_t njoin, join_stride;  // entries, and rows that each gets
-  uint32_t max_parts;
+  uint32_t max_parts;   // of a span's rows
+  uint32_t join_parts;  // of an entry, at most
+  uint32_t mask_rows, mask_tiles;  // whether a kernel has pieces with own tokens of masked spans
   const uint32_t* blocks;
 };
 
@@ -147,7 +149,7 @@ uint64_t move_space(int D, int fmt, uint32_t heads, uint64_t n);  // bytes of wo
 cudaError_t launch_move(int D, int fmt, const MoveArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_copy(CopyArgs a, int sms, cudaStream_t s);
 cudaError_t launch_tree(const TreeArgs& a, uint32_t trees, cudaStream_t s);
-cudaError_t launch_rows(int D, int fmt, bool masked, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
+cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_join(int D, bool fp16, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t launch_tiles(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s);
 cudaError_t prepare_rows(int D, int fmt);
@@ -250,6 +252,22 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // Two bf16 as floats.
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Whether one of the two 16-bit floats in w is an infinity or a NaN.
+template <bool FP16>
+__device__ __forceinline__ bool not_finite2(uint32_t w) {
+  constexpr uint32_t m = FP16 ? 0x7C00u : 0x7F80u;
+  return (w & m) == m || ((w >> 16) & m) == m;
+}
+template <bool FP16>
+__device__ __forceinline__ bool not_finite4(const uint4& w) {
+  return not_finite2<FP16>(w.x) || not_finite2<FP16>(w.y) || not_finite2<FP16>(w.z) || not_finite2<FP16>(w.w);
+}
+template <bool FP16>
+__device__ __forceinline__ float value16(uint16_t b) {
+  if (FP16) return __half2float(__ushort_as_half(b));
+  return __uint_as_float((uint32_t)b << 16);
+}
 
 // The scale of an fp8 row as a float; the mark of a row with a NaN gives a NaN.
 __device__ __forceinline__ float exp_value(uint32_t e) {

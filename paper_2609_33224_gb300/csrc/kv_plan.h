@@ -37,19 +37,22 @@ struct alignas(16) Piece {
   uint32_t nblocks;   // blocks (row kernel) or key tiles of 8 blocks (tile kernel; the last may be partial)
   uint32_t key0;      // index in the span of the first key
   uint32_t end;       // keys end before this index
-  int32_t climit;     // the span's i-th query sees keys j <= climit + i
+  int32_t climit;     // the span's i-th query sees keys j <= climit + i; masked: the first of the own tokens
   uint32_t query0;    // the span's first query
   uint32_t row0;      // the tile's first row
   uint32_t part_row;  // first row of the partial result, or kDirect: the output is written
   uint16_t nrows;
   uint16_t head;
   uint32_t fold0, nfold;  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in
-  uint32_t split;  // row kernel: 1: of a masked span, own tokens from climit on; tile kernel: not 0: its even steps in tile 0, its odd ones in tile 1, so many rows behind
+  // row kernel: 1: masked; tile kernel (masked where climit is a limit): not 0: its even steps in tile 0, its odd ones in
+  // tile 1, so many rows behind
+  uint32_t split;
 };
 static_assert(sizeof(Piece) == 48, "Piece layout");
 constexpr uint32_t kDirect = 0xFFFFFFFFu;
 constexpr int32_t kNoLimit = 0x3FFFFFFF;
 constexpr uint32_t kMasked = 2;  // ps_kv_span.causal of a masked span
+constexpr uint32_t kTileOwn = 256;  // own tokens of a masked span that the tile kernel takes, at most
 
 // What is to be joined: the rows head0 .. head0 + count - 1 of a query, whose parts are the segments
 // segs[seg0] ..: the i-th row's are the partial rows row + i + k * stride, k < nparts.  The join kernel gives every entry
@@ -111,6 +114,19 @@ inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool 
   if (row_tiles > 2 && (double)keys * token_bytes(kv) * kv.heads > 96e6)
     by_rows = std::max(by_rows, row_tiles / 2.0 * (double)keys * token_bytes(kv) / 5000.0);
   return by_rows - step_ns(kv) * (double)((keys + kTileKeys - 1) / kTileKeys + kPieceSteps);
+}
+
+// The same for all keys of a masked span.  By rows they cost about twice as much as a plain span's, in pieces that end with
+// masked blocks (32 drafts of 32 nodes on 300 to 500 tokens, 4 query heads a key/value head: 44 us by tiles, 51 by rows; 16
+// of 8 nodes on 1500 to 2000 45 and 53; 60 of 4 nodes on 2000 to 3000, fp8, 187 and 127).  Where the rows have a prefix
+// too, the tile kernel's results are to be joined with the prefix's, which the row kernel can do as it goes: 32 drafts
+// of 48 nodes on 30 tokens or less and 8000 shared ones 343 by tiles, 292 by rows; 60 of 8 to 12 nodes on 50 to 300 and
+// 4000, fp8, 117 and 110; 60 of up to 31 on up to 700 and 16384, fp8, 441 with all of them that the first rule would
+// give to tiles and 426 with this one.
+constexpr double kMaskedRows = 2.0, kJoinRow = 0.25;
+inline double masked_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool prefix) {
+  const double tile = step_ns(kv) * (double)((keys + kTileKeys - 1) / kTileKeys + kPieceSteps);
+  return kMaskedRows * (tile_saves(kv, rows, keys, false) + tile) - tile - (prefix ? kJoinRow * rows * kv.D / 128 : 0.0);
 }
 
 // From so many steps on, a piece of one tile of rows runs as two.  64 rows on 65536 tokens: 65 us, 79 as one; on
@@ -176,6 +192,8 @@ struct Layout {
   uint64_t part_rows = 0;
   uint32_t max_parts = 1;
   uint32_t join_stride = 0;  // the largest entry's count
+  uint32_t join_parts = 0;   // and number of parts
+  bool mask_rows = false, mask_tiles = false;  // pieces with own tokens of masked spans
   int row_sms = 0;  // SMs of the row kernel; fewer than all: beside the tile kernel
 };
 
@@ -243,12 +261,29 @@ inline void share_out(const std::vector<Unit>& units, uint32_t most, uint32_t ex
 inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, uint32_t n_spans, Layout* out) {
   Layout& o = *out;
   const uint32_t H = pl.heads, g = pl.group;
-  // The keys that all rows of a tile see, where the tile kernel is the one to take them (else 0).
+  // spans that cover a query: how many more than the one before
+  std::vector<int32_t> over((size_t)T + 1, 0);
+  bool any_masked = false;
+  for (uint32_t si = 0; si < n_spans; ++si) {
+    any_masked = any_masked || spans[si].causal == kMasked;
+    if (spans[si].num_queries == 0 || spans[si].length == 0) continue;
+    ++over[spans[si].first_query];
+    --over[spans[si].first_query + spans[si].num_queries];
+  }
+  if (any_masked)
+    for (uint32_t t = 1; t < T; ++t) over[t] += over[t - 1];
+  // The time that the tile kernel saves for the keys c of a tile's rows.
+  auto saves = [&](const ps_kv_span& s, uint32_t nr, int64_t c) {
+    if (s.causal == kMasked && c == (int64_t)s.length) return masked_saves(pl, nr, c, over[s.first_query] > 1);
+    return tile_saves(pl, nr, c, s.causal != 0);
+  };
+  // The keys that all rows of a tile see, where the tile kernel is the one to take them (else 0); a masked span's own
+  // ones too, unless they are too many.
   auto cut_of = [&](const ps_kv_span& s, uint32_t r0, uint32_t nr) -> int64_t {
     int64_t c = (int64_t)s.length;
     if (s.causal == 1) c = std::max<int64_t>(0, c - (int64_t)s.num_queries + r0 / g + 1) / kBlock * kBlock;
-    if (s.causal == kMasked) c = (c - (int64_t)s.num_queries) / kBlock * kBlock;
-    return tile_saves(pl, nr, c, s.causal != 0) > 0 ? c : 0;
+    if (s.causal == kMasked && s.num_queries > kTileOwn) c = (c - (int64_t)s.num_queries) / kBlock * kBlock;
+    return saves(s, nr, c) > 0 ? c : 0;
   };
   auto tiles_save = [&](const ps_kv_span& s) {
     double sum = 0;
@@ -256,7 +291,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     for (uint32_t r0 = 0; r0 < rows; r0 += tr) {
       const uint32_t nr = std::min(rows - r0, tr);
       const int64_t c = cut_of(s, r0, nr);
-      if (c > 0) sum += tile_saves(pl, nr, c, s.causal != 0) * H;
+      if (c > 0) sum += saves(s, nr, c) * H;
     }
     return sum;
   };
@@ -281,7 +316,9 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
         const int64_t c = cut_of(s, r0, nr);
         cut.push_back(c);
         for (uint32_t h = 0; h < H; ++h) {
-          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, kNoLimit, tile_rows, o));
+          const bool own = s.causal == kMasked && c == len;
+          if (c > 0) o.tile_units.push_back(unit(s, r0, nr, h, 0, c, kTileKeys, own ? climit : kNoLimit, tile_rows, o));
+          if (c > 0 && own) o.mask_tiles = true;
           o.groups.push_back(Group{0, 0});
         }
       }
@@ -295,7 +332,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
       for (uint32_t h = 0; h < H; ++h) {
         if (end > from) {
           o.row_units.push_back(unit(s, r0, nr, h, from, end, kBlock, climit, kSmallRows, o));
-          o.row_units.back().p.split = s.causal == kMasked;
+          if (s.causal == kMasked) o.mask_rows = o.row_units.back().p.split = 1;
         }
         o.groups.push_back(Group{0, 0});
       }
@@ -435,6 +472,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
         }
         for (uint32_t h = 0; h < H; ++h) {
           const uint32_t seg0 = (uint32_t)o.segs.size();
+          uint32_t parts = 0;
           bool direct = false;
           for (uint32_t l = 0; l < nl; ++l) {
             const Layer& ly = o.layers[ls[l]];
@@ -442,6 +480,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
             const Group& gr = o.groups[ly.group0 + r / ly.tile_rows * H + h];
             direct = direct || gr.part_row == kDirect;
             if (gr.nparts) o.segs.push_back(JoinSeg{gr.part_row + r % ly.tile_rows, ly.tile_rows, gr.nparts});
+            parts += gr.nparts;
           }
           if (direct) {
             o.segs.resize(seg0);
@@ -449,6 +488,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
           }
           o.join.push_back(JoinEntry{t, (uint16_t)(h * g + i), (uint16_t)n, seg0, (uint32_t)o.segs.size() - seg0});
           o.join_stride = std::max(o.join_stride, n);
+          o.join_parts = std::max(o.join_parts, parts);
         }
       }
     }

@@ -33,7 +33,7 @@ __device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
 // A warp takes a token and a share of its rows (queries' heads, then keys' heads), D / 16 lanes a row.  Its lanes first
 // work out the token's cosines and sines, a pair of elements each, which every row then uses: the angle is
 // position * (turns per position), as 64-bit fractions of a turn, so the integer product wraps at whole turns and no
-// position is too far; the upper 32 bits, as a float, go to sincospif.  A lane has two groups of 8 elements that its
+// position is too far; its upper 32 bits, less the nearest quarter turn, go to sincospif.  A lane has two groups of 8 elements that its
 // pairs lie in: half a rotated part apart, or next to each other.
 // Bound by bytes: reads q, k and v and writes the rotated queries and the cache's rows, each once.
 template <int D, int FMT, int TYPE>
@@ -68,10 +68,18 @@ __global__ void __launch_bounds__(256, TYPE == PS_KV_FP32 ? 3 : 4) rotate_kernel
     const uint64_t p = (uint64_t)a.positions[t];
     __syncwarp();
     for (uint32_t i = lane; i < a.dims / 2; i += 32) {
-      const int32_t part = (int32_t)((p * a.turns[i]) >> 32);  // of a turn, in 2^-32
+      const uint32_t part = (uint32_t)((p * a.turns[i]) >> 32);  // of a turn, in 2^-32
+      // to within an eighth of a turn of a quarter: what is left has as many bits as a float keeps
+      const uint32_t quarter = (part + (1u << 29)) >> 30;
       float s, co;
-      sincospif((float)part * 0x1p-31f, &s, &co);
-      turns[warp][i] = make_float2(co * a.magnitude, s * a.magnitude);
+      sincospif((float)(int32_t)(part - (quarter << 30)) * 0x1p-31f, &s, &co);
+      if (quarter & 1u) {
+        const float x = co;
+        co = -s;
+        s = x;
+      }
+      const float m = quarter & 2u ? -a.magnitude : a.magnitude;
+      turns[warp][i] = make_float2(co * m, s * m);
     }
     __syncwarp();
     float2 cs[8];

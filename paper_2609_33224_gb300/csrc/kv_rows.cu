@@ -100,18 +100,6 @@ __device__ __forceinline__ void sts128_zero(uint32_t addr) {
 
 __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// Whether one of the two 16-bit floats in w is an infinity or a NaN.
-template <bool FP16>
-__device__ __forceinline__ bool not_finite2(uint32_t w) {
-  constexpr uint32_t m = FP16 ? 0x7C00u : 0x7F80u;
-  return (w & m) == m || ((w >> 16) & m) == m;
-}
-template <bool FP16>
-__device__ __forceinline__ float value16(uint16_t b) {
-  if (FP16) return __half2float(__ushort_as_half(b));
-  return __uint_as_float((uint32_t)b << 16);
-}
-
 // Where a worker is: its next piece and the end of its pieces, its ring's next stage and that barrier's phase; whether
 // it has waited for the kernel before this one.
 struct Place {
@@ -724,8 +712,8 @@ cudaError_t prepare_one() {
   return cudaFuncSetAttribute(rows_kernel<D, FMT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FMT>());
 }
 template <int D, int FMT>
-cudaError_t launch_one(bool masked, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
-  return launch(masked ? rows_kernel<D, FMT, true> : rows_kernel<D, FMT, false>, p.row_ctas, kRowWarps * 32,
+cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
+  return launch(p.mask_rows ? rows_kernel<D, FMT, true> : rows_kernel<D, FMT, false>, p.row_ctas, kRowWarps * 32,
                 smem_bytes<D, FMT>(), 1, overlap, s, a, p);
 }
 
@@ -741,14 +729,14 @@ cudaError_t prepare_rows(int D, int fmt) {
                              : prepare_one<64, PS_KV_FP8>();
 }
 
-cudaError_t launch_rows(int D, int fmt, bool masked, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
+cudaError_t launch_rows(int D, int fmt, const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   if (D == 128)
-    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(masked, a, p, overlap, s)
-           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(masked, a, p, overlap, s)
-                               : launch_one<128, PS_KV_FP8>(masked, a, p, overlap, s);
-  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(masked, a, p, overlap, s)
-         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(masked, a, p, overlap, s)
-                             : launch_one<64, PS_KV_FP8>(masked, a, p, overlap, s);
+    return fmt == PS_KV_BF16   ? launch_one<128, PS_KV_BF16>(a, p, overlap, s)
+           : fmt == PS_KV_FP16 ? launch_one<128, PS_KV_FP16>(a, p, overlap, s)
+                               : launch_one<128, PS_KV_FP8>(a, p, overlap, s);
+  return fmt == PS_KV_BF16   ? launch_one<64, PS_KV_BF16>(a, p, overlap, s)
+         : fmt == PS_KV_FP16 ? launch_one<64, PS_KV_FP16>(a, p, overlap, s)
+                             : launch_one<64, PS_KV_FP8>(a, p, overlap, s);
 }
 
 }  // namespace pskv

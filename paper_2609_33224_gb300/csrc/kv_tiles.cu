@@ -61,6 +61,7 @@ struct Bars {
   uint64_t full[10], empty[10];  // operand ring
   uint64_t raw_full[4], raw_empty[4];
   uint64_t q_ready[2], s_full[2], p_ready[2][2], o_done[2], tail_here, tail_done, drain;
+  uint32_t odd;  // a value row of an own token was taken out of a product so far
   uint32_t tmem;
   uint32_t gave_up;  // by the warp that arrives on tail_here, before its last arrival
 };
@@ -260,7 +261,49 @@ __device__ __forceinline__ uint32_t lds8(uint32_t addr) {
   return b;
 }
 
+// Bits `at` .. `at` + 127 of a mask row, which has bits 0 .. bits - 1; those below 0 are set, those past the end are not.
+// The loads wait for nothing but their place.
+__device__ __forceinline__ void mask128(uint32_t (&sees)[4], const uint32_t* row, int32_t at, int32_t bits) {
+  uint32_t w[5];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) {
+    const int32_t x = (at >> 5) + i;  // rounds down
+    w[i] = x < 0 ? 0xFFFFFFFFu : 0u;
+    if (x >= 0 && x * 32 < bits) w[i] = __ldg(row + x);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sees[i] = __funnelshift_r(w[i], w[i + 1], (uint32_t)at & 31u);
+}
+// The first step of a piece that has own tokens of a masked span, or one past all steps.
+__device__ __forceinline__ uint32_t first_masked(const Piece& p) {
+  if (p.climit == kNoLimit) return 0xFFFFFFFFu;
+  return p.climit >= (int32_t)p.key0 ? (uint32_t)(p.climit - (int32_t)p.key0) / kTileKeys : 0;
+}
+
+// Which panels of 64 columns of token `tok`'s value row hold a value that is not finite (bits), by a whole warp.
 template <int D, int FMT>
+__device__ __forceinline__ uint32_t odd_panels(const uint8_t* rec, uint32_t tok, uint32_t lane) {
+  constexpr int kHalf = half_bytes(D, FMT);
+  if constexpr (FMT == PS_KV_FP8) return rec[2 * kHalf + kBlock + exp_place(tok)] == kExpNan ? (1u << D / 64) - 1 : 0u;
+  uint4 w = make_uint4(0, 0, 0, 0);
+  if (lane < D / 8) w = __ldcg(reinterpret_cast<const uint4*>(rec + kHalf + offset16(tok, lane)));
+  const uint32_t odd = __ballot_sync(0xFFFFFFFFu, not_finite4<FMT == PS_KV_FP16>(w));
+  return (odd & 0xFFu ? 1u : 0u) | (odd >> 8 ? 2u : 0u);
+}
+// Sets a word of this CTA's shared memory and, in a pair, the other CTA's, and waits until both are.
+template <int CTAS>
+__device__ __forceinline__ void set_in_both(uint32_t addr) {
+  asm volatile("st.shared::cta.u32 [%0], %1;" ::"r"(addr), "r"(1) : "memory");
+  if (CTAS == 2) {
+    asm volatile(
+        "{\n .reg .b32 r, a;\n mov.u32 r, %%cluster_ctarank;\n xor.b32 r, r, 1;\n mapa.shared::cluster.u32 a, %0, r;\n"
+        " st.shared::cluster.u32 [a], %1;\n fence.acq_rel.cluster;\n}\n" ::"r"(addr),
+        "r"(1)
+        : "memory");
+  }
+}
+
+template <int D, int FMT, bool kMask>
 __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(const AttnArgs a, const PlanDev p) {
   using C = Cfg<D, FMT>;
   extern __shared__ uint8_t smem_raw[];
@@ -293,7 +336,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     mbar_init(smem_u32(&bars.tail_here), 1);
     mbar_init(smem_u32(&bars.tail_done), 1);
     mbar_init(smem_u32(&bars.drain), 1);
-    bars.gave_up = 0;
+    bars.odd = bars.gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) tc_alloc<C::kCtas>(smem_u32(&bars.tmem), 512);
@@ -323,6 +366,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     for (uint32_t pi = first; alive && pi < last; ++pi) {
       const Piece pc = p.tile_pieces[pi];
       if (pi == first) wait_for_last();  // the plan is read before, queries and results' places after
+      const uint32_t masked0 = kMask ? first_masked(pc) : 0;
       if (!pc.split && t * C::kRows >= pc.nrows) continue;
       const uint32_t in_tile = (pc.split ? 0 : t * C::kRows) + rank * 128 + r;
       const uint32_t row = pc.row0 + in_tile;
@@ -364,6 +408,11 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       float m = -INFINITY, l = 0.0f;
       const uint32_t j0 = pc.split ? t : 0, dj = pc.split ? 2 : 1;
       for (uint32_t j = j0; j < pc.nblocks; j += dj) {
+        uint32_t sees[4];  // masked: the step's keys that this row sees
+        if (kMask && j >= masked0) {
+          const int32_t at = (int32_t)(pc.key0 + j * kTileKeys) - pc.climit, bits = (int32_t)pc.end - pc.climit;
+          mask128(sees, a.mask + (int64_t)query * a.mask_stride, at, valid ? bits : 0);
+        }
         if (!mbar_wait_warp(smem_u32(&bars.s_full[t]), steps & 1)) {
           alive = false;
           break;
@@ -381,6 +430,13 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if ((uint32_t)(32 * c + i) >= left) s[c][i] = 0xFF800000u;
+        }
+        if (kMask && j >= masked0) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!((sees[c] >> i) & 1u)) s[c][i] = 0xFF800000u;
         }
         float x4[4];
 #pragma unroll
@@ -444,6 +500,46 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       }
       ++done;
       tc_fence_after();
+      if (kMask && masked0 < pc.nblocks && *static_cast<volatile uint32_t*>(&bars.odd)) {
+        // The panels of value rows that were taken out (the mark was set before their step's product, or by another
+        // piece's), token by token, for the rows that see it.  They are found again in the cache; the warp's lanes go
+        // together, as tensor memory is read and written by all of them.
+        const float u = m == -INFINITY ? 0.0f : m;
+        const uint32_t end = min(pc.end, pc.key0 + pc.nblocks * kTileKeys);
+        for (uint32_t key = max((uint32_t)max(pc.climit, 0), pc.key0); key < end; ++key) {
+          if (pc.split && ((key - pc.key0) / kTileKeys & 1u) != t) continue;
+          const uint8_t* rec = a.pool + ((uint64_t)p.blocks[pc.block + (key - pc.key0) / kBlock] * a.kv_heads + pc.head) * C::kRec;
+          const uint32_t tok = key % kBlock, panels = odd_panels<D, FMT>(rec, tok, lane);
+          if (!panels) continue;
+          const uint32_t own = key - (uint32_t)pc.climit;
+          const bool seen = valid && ((a.mask[(int64_t)query * a.mask_stride + own / 32] >> (own % 32)) & 1u);
+          float w = NAN;  // the token's weight (fp8: its value is a NaN)
+          if (!C::kFp8 && seen) {
+            const uint16_t* q = a.q + (int64_t)query * a.q_tok + (int64_t)head * a.q_head;
+            w = 0.0f;
+            for (uint32_t d = 0; d < D; ++d)
+              w += value16<C::kFp16>(q[d]) *
+                   value16<C::kFp16>(*reinterpret_cast<const uint16_t*>(rec + offset16(tok, d / 8) + d % 8 * 2));
+            w = ex2(w * a.scale_log2 - u);
+          }
+#pragma unroll 1
+          for (uint32_t c = 0; c < D / 16; ++c) {
+            if (!((panels >> (c / 4)) & 1u)) continue;
+            uint32_t o[16];
+            tc_ld16(o, o_addr + 16 * c);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float v = 1.0f;
+              if constexpr (!C::kFp8)
+                v = value16<C::kFp16>(*reinterpret_cast<const uint16_t*>(rec + C::kHalf + offset16(tok, 2 * c + i / 8) + i % 8 * 2));
+              if (seen) o[i] = __float_as_uint(__uint_as_float(o[i]) + w * v);
+            }
+            tc_st16(o_addr + 16 * c, o);
+            tc_wait_st();
+          }
+        }
+      }
       const bool direct = pc.part_row == kDirect;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const uint64_t at = (uint64_t)pc.part_row + t * (pc.split ? pc.split : C::kRows) + rank * 128 + r;
@@ -619,6 +715,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         const Piece* pp = p.tile_pieces + pi;
         const uint32_t steps = pp->nblocks, keys = pp->end - pp->key0;
         const uint32_t tiles = pp->nrows > C::kRows ? 2 : 1;
+        const uint32_t masked0 = kMask ? first_masked(*pp) : 0;
         // ring order: keys 0, values 0, keys 1, values 1, ...: step j's keys are slot n0 + 2j, values n0 + 2j + 1
         const uint32_t n0 = n;
         auto slot = [&](uint32_t i) { return (n0 + i) % C::kSlots; };
@@ -654,7 +751,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         }
         for (uint32_t j = 0; alive && j < steps; ++j) {
           if (!here(2 * j + 1)) break;
-          if (!C::kFp8 && keys - j * kTileKeys < (uint32_t)kTileKeys) {
+          if (!C::kFp8 && (keys - j * kTileKeys < (uint32_t)kTileKeys || (kMask && j >= masked0))) {
             mbar_arrive(smem_u32(&bars.tail_here));
             if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
           }
@@ -686,10 +783,11 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         const Piece* pp = p.tile_pieces + pi;
         const uint32_t slots = 2 * pp->nblocks;
         const bool partial = pp->end - pp->key0 < pp->nblocks * kTileKeys;
+        const uint32_t masked0 = kMask ? first_masked(*pp) : 0;
         for (uint32_t i = 0; alive && i < slots; ++i, ++n) {
           const uint32_t at = n % C::kSlots;
           alive = mbar_wait(full(at), (n / C::kSlots) & 1);
-          if (alive && partial && i == slots - 1) {
+          if (alive && ((partial && i == slots - 1) || (kMask && i % 2 == 1 && i / 2 >= masked0))) {
             mbar_arrive(smem_u32(&bars.tail_here));
             alive = mbar_wait(smem_u32(&bars.tail_done), tails++ & 1);
           }
@@ -701,7 +799,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         *static_cast<volatile uint32_t*>(&bars.gave_up) = 1;
         mbar_arrive(smem_u32(&bars.tail_here));
       }
-    } else if (warp == 10 && !C::kFp8) {
+    } else if (warp == 10 && !C::kFp8 && !kMask) {
       // ================= partial steps: value rows past the end hold other tokens or earlier steps =================
       uint32_t n = 0, tails = 0;
       bool alive = true;
@@ -723,6 +821,57 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         fence_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&bars.tail_done));
+      }
+      if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
+    } else if (warp == 10 && !C::kFp8) {
+      // ================= masked pieces: values of own tokens, and partial steps as above =================
+      // A token that a row does not see has a probability of 0 there, but 0 times an infinity or a NaN is not: an own
+      // token's values (here: this CTA's panel of them) are taken out of the product where one of them is not finite, and
+      // rows that see the token add them at the piece's end.
+      uint32_t n = 0, tails = 0;
+      bool alive = true;
+      for (uint32_t pi = first; alive && pi < last; ++pi) {
+        const Piece* pp = p.tile_pieces + pi;
+        const uint32_t n0 = n, steps = pp->nblocks, key0 = pp->key0, end = pp->end, masked0 = first_masked(*pp);
+        const uint32_t own = masked0 < steps ? (uint32_t)pp->climit : end;
+        n += 2 * steps;
+        for (uint32_t j = min(masked0, end - key0 < steps * kTileKeys ? steps - 1 : steps); j < steps; ++j) {
+          if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars.tail_here), tails++ & 1, 60000000000ull))) {
+            alive = false;
+            break;
+          }
+          if (*static_cast<volatile uint32_t*>(&bars.gave_up)) {  // no step comes any more
+            pi = last;
+            break;
+          }
+          const uint32_t v = ring + (n0 + 2 * j + 1) % C::kSlots * C::kSlot;
+          bool any = false;
+#pragma unroll 1
+          for (uint32_t i = lane; i < kTileKeys; i += 32) {
+            const uint32_t key = key0 + j * kTileKeys + i, row = v + i * 128;
+            bool odd = false;
+            if (key >= own && key < end) {
+#pragma unroll
+              for (uint32_t c = 0; c < 8; ++c) {
+                uint4 w;
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                             : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                             : "r"(row + ((c ^ (i & 7u)) << 4))
+                             : "memory");
+                odd |= not_finite4<C::kFp16>(w);
+              }
+            }
+            if (odd || key >= end) {
+#pragma unroll
+              for (uint32_t c = 0; c < 8; ++c) sts128(row + ((c ^ (i & 7u)) << 4), 0, 0, 0, 0);
+            }
+            any |= odd;
+          }
+          if (__any_sync(0xFFFFFFFFu, any) && lane == 0) set_in_both<C::kCtas>(smem_u32(&bars.odd));
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars.tail_done));
+        }
       }
       if (!alive && lane == 0) atomicOr_system(a.err, kErrWait);
     }
@@ -770,7 +919,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             } else {
               const bool live = tok < left;
               const uint32_t at_e = exps + vb * 32 + kBlock + exp_place(tok % kBlock);
-              const uint32_t e = live ? lds8(at_e) : (uint32_t)kExpBias;
+              uint32_t e = live ? lds8(at_e) : (uint32_t)kExpBias;
+              // a marked row's codes are zeros: with another scale it is out of the product
+              if (kMask && e == kExpNan && (int32_t)(pp->key0 + j * kTileKeys + tok) >= pp->climit) {
+                e = kExpBias;
+                *static_cast<volatile uint32_t*>(&bars.odd) = 1;
+              }
               to_bf16<4>(
                   e, live, [&](int c) { return raw + C::kRawK + vb * (kBlock * 64) + offset8v(tok % kBlock, c); },
                   [&](int c) { return dst + tok * 128 + ((c ^ (tok & 7u)) << 4); });
@@ -794,21 +948,28 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   if (warp == 9) tc_dealloc<C::kCtas>(bars.tmem, 512);
 }
 
-template <int D, int FMT>
-cudaError_t prepare_one() {
+template <int D, int FMT, bool kMask>
+cudaError_t prepare_form() {
   // setmaxnreg hands out what the launch was given: fewer registers than the split adds up to would wait for ever
   cudaFuncAttributes at{};
-  cudaError_t e = cudaFuncGetAttributes(&at, tiles_kernel<D, FMT>);
+  cudaError_t e = cudaFuncGetAttributes(&at, tiles_kernel<D, FMT, kMask>);
   if (e != cudaSuccess) return e;
   const int threads = Cfg<D, FMT>::kWarps * 32;
   if (at.numRegs * threads < 256 * Cfg<D, FMT>::kRegSoft + (threads - 256) * Cfg<D, FMT>::kRegRest)
     return cudaErrorInvalidKernelImage;
-  return cudaFuncSetAttribute(tiles_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, FMT>::kSmem);
+  return cudaFuncSetAttribute(tiles_kernel<D, FMT, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Cfg<D, FMT>::kSmem);
+}
+template <int D, int FMT>
+cudaError_t prepare_one() {
+  const cudaError_t e = prepare_form<D, FMT, false>();
+  return e != cudaSuccess ? e : prepare_form<D, FMT, true>();
 }
 template <int D, int FMT>
 cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   using C = Cfg<D, FMT>;
-  return launch(tiles_kernel<D, FMT>, p.tile_workers * C::kCtas, C::kWarps * 32, C::kSmem, C::kCtas, overlap, s, a, p);
+  return launch(p.mask_tiles ? tiles_kernel<D, FMT, true> : tiles_kernel<D, FMT, false>, p.tile_workers * C::kCtas,
+                C::kWarps * 32, C::kSmem, C::kCtas, overlap, s, a, p);
 }
 
 }  // namespace

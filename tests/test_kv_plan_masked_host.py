@@ -1,5 +1,5 @@
-"""The plan of a batch with masked spans: its pieces give every query all of such a span's keys, the tile kernel's only those
-before the own ones, and the row kernel is told where those begin."""
+"""The plan of a batch with masked spans: its pieces give every query all of such a span's keys, and both kernels are told where
+the own ones begin; the tile kernel takes those of a limited number of queries."""
 import os
 import random
 import subprocess
@@ -19,7 +19,9 @@ def plan(tmp_path_factory):
             ("const long lim = s->causal ?", "const bool masked = s->causal == kMasked;\n"
              "          CHECK(kind || p.split == (masked ? 1u : 0u));\n"
              "          if (masked && !kind) CHECK((long)p.climit == (long)s->length - (long)s->num_queries);\n"
-             "          if (masked && kind) CHECK(last <= (long)s->length - (long)s->num_queries);\n"
+             "          if (kind && p.climit == kNoLimit) CHECK(!masked || last <= (long)s->length - (long)s->num_queries);\n"
+             "          else if (kind) CHECK(masked && o.mask_tiles && s->num_queries <= kTileOwn && (long)p.climit == (long)s->length - (long)s->num_queries);\n"
+             "          else CHECK(!masked || o.mask_rows);\n"
              "          const long lim = masked ? (long)s->length : s->causal ?"),
             ("else CHECK((long)p.climit ==", "else if (!masked) CHECK((long)p.climit =="),
             (": s.causal ? std::min<long>", ": s.causal == 1 ? std::min<long>"),
@@ -44,6 +46,9 @@ def plan(tmp_path_factory):
 
 def _random(rng):
     shape, spans = host._random(rng)
+    if rng.random() < 0.2:  # more own tokens than the tile kernel takes
+        shape = (*shape[:5], 600)
+        spans = [(0, 600, 2000, 2), (10, 257, 257, 2), (300, 256, 900, 2)]
     return shape, [(a, n, max(length, n), 2) if rng.random() < 0.6 else (a, n, length, c) for a, n, length, c in spans]
 
 
@@ -55,7 +60,7 @@ def test_every_key_once(plan):
 
 def test_forms(plan):
     got = plan([
-        # contexts by tiles, drafts by rows
+        # contexts and drafts by tiles
         ((152, 128, 0, 8, 8, 640), [(64 * i, 64, 4000 + 64 + i, 2) for i in range(10)]),
         # drafts on a shared prefix
         ((152, 128, 2, 8, 8, 310), [(0, 310, 16384, 0)] + [(31 * i, 31, 31 + i, 2) for i in range(10)]),
@@ -64,6 +69,6 @@ def test_forms(plan):
         # alone: written by the row kernel
         ((152, 64, 1, 1, 1, 16), [(0, 16, 16, 2)]),
     ])
-    assert got[0][0] and got[0][1] and got[1][0] and got[1][1]
+    assert not got[0][0] and got[0][1] and got[1][0] and got[1][1]
     assert got[2][3] > 0
     assert got[3] == (1, 0, 0, 0)
