@@ -133,7 +133,8 @@ PS_API ps_status ps_kv_move_workspace(ps_kv* kv, uint64_t n, uint64_t* bytes);
  * cache skips it and is reported by kv.  A block may be copied to many places.  Blocks of dst must be different, and where
  * from is kv, none of them may be another copy's source.  The paper has no counterpart.
  * Errors: PS_ERR_INVALID, PS_ERR_CUDA. */
-PS_API ps_status ps_kv_copy_blocks(ps_kv* kv, ps_kv* from, const int64_t* src, const int64_t* dst, uint64_t n, void* stream);
+PS_API ps_status ps_kv_copy_blocks(ps_kv* kv, ps_kv* from, const int64_t* src, const int64_t* dst, uint64_t n,
+                                   void* stream);
 
 /* Masks and positions of trees of drafted tokens, for ps_kv_attend_masked and ps_kv_write_rotated.  Tree b's nodes are
  * rows offsets[b] .. offsets[b + 1] - 1 of num_nodes (device array of num_trees + 1 int64, rising), or with offsets NULL

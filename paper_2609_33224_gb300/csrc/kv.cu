@@ -154,7 +154,8 @@ ps_status reported(ps_kv* kv) {
   if (e & pskv::kErrWait)
     return fail(kv, PS_ERR_TIMEOUT, "a bounded device-side wait of an earlier attention call gave up");
   if (e & pskv::kErrSlot) return fail(kv, PS_ERR_INVALID, "an earlier call named a slot or block outside the cache");
-  return fail(kv, PS_ERR_INVALID, "an earlier call's trees had a parent that is no node before its child, or wrong offsets");
+  return fail(kv, PS_ERR_INVALID,
+              "an earlier call's trees had a parent that is no node before its child, or wrong offsets");
 }
 
 size_t elem_size(int type) { return type == PS_KV_FP32 ? 4 : 2; }

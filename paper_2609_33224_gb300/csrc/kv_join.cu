@@ -129,11 +129,11 @@ __global__ void __launch_bounds__(256, 4) join_kernel(const AttnArgs a, const Pl
     a.lse[(uint64_t)query * a.kv_heads * a.group + head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// A warp takes an entry: rows of one query whose parts are alike, kParts of them at most.  A lane finds the place, maximum
-// and sum of a (row, part), 32 / kParts rows at once, and the rows' values are then loaded some rows together, with
-// nothing to wait for between them.  The same operations in the same order as above.  Bound by the bytes of the parts,
-// where the other form, a warp a row, is bound by the four loads that a row waits for, with as many rows in flight as
-// there are warps.
+// A warp takes an entry: rows of one query that have the same number of parts, at most kParts.  A lane finds the place,
+// maximum and sum of a (row, part), 32 / kParts rows at once, and the rows' values are then loaded some rows together,
+// with nothing to wait for between them.  The same operations in the same order as above.  Bound by the bytes of the
+// parts, where the other form, a warp a row, is bound by the four loads that a row waits for, with as many rows in flight
+// as there are warps.
 template <int D, bool FP16, int kParts>
 __global__ void __launch_bounds__(256, 4) join_entries_kernel(const AttnArgs a, const PlanDev p) {
   constexpr int kV = D / 32, kRows = 32 / kParts, kAtOnce = kRows < 4 ? kRows : 4;
@@ -221,7 +221,11 @@ template <int D, bool FP16>
 cudaError_t go(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   const uint32_t rows = p.njoin * p.join_stride;
   // A CTA a row where there are few: 64 rows of 64 parts 7 us less than a warp a row; 2048 rows of 38 parts 3 us more.
-  if (p.max_parts > 4 && rows <= 1024)
+  // With up to 8 parts a warp a row is as good from fewer rows on: 1024 rows of 8 parts 15.6 us with the attention before
+  // them, 17.2 by CTAs; 512 rows of 8 14.7 and 14.0.  (Only where masked spans are: the sums of a row's parts are in
+  // another order, and other batches keep theirs.)
+  const uint32_t wide = p.max_parts <= 8 && (p.mask_tiles || p.mask_rows) ? 512 : 1024;
+  if (p.max_parts > 4 && rows <= wide)
     return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, overlap, s, a, p);
   // A warp an entry where there are many rows of few parts: 24700 rows of 2 parts 10.4 us, 17.3 by a warp a row; 7700 rows
   // of 5 or more 18.5 and 11.5; 16400 of 8 the same.

@@ -33,9 +33,11 @@ __device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
 // A warp takes a token and a share of its rows (queries' heads, then keys' heads), D / 16 lanes a row.  Its lanes first
 // work out the token's cosines and sines, a pair of elements each, which every row then uses: the angle is
 // position * (turns per position), as 64-bit fractions of a turn, so the integer product wraps at whole turns and no
-// position is too far; its upper 32 bits, less the nearest quarter turn, go to sincospif.  A lane has two groups of 8 elements that its
-// pairs lie in: half a rotated part apart, or next to each other.
-// Bound by bytes: reads q, k and v and writes the rotated queries and the cache's rows, each once.
+// position is too far; its upper 32 bits, less the nearest quarter turn, go to sincospif.  A lane has two groups of 8
+// elements that its pairs lie in: half a rotated part apart, or next to each other.
+// Bound by bytes: reads q, k and v and writes the rotated queries and the cache's rows, each once.  65536 tokens of 64 and
+// 8 heads, 128 columns, bf16 to fp8, 2.55 GB: 405 us = 6.3 TB/s, 93% of the measured copy.  The next row loaded ahead,
+// three or two blocks an SM (402 to 486 us) or streaming stores (409) gave no more.
 template <int D, int FMT, int TYPE>
 __global__ void __launch_bounds__(256, TYPE == PS_KV_FP32 ? 3 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
   constexpr bool kFp8 = FMT == PS_KV_FP8;

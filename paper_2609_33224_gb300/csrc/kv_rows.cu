@@ -13,7 +13,8 @@
 // 1/8 or less filled here.  5 requests of 65536 to 131072 tokens, fp8, 8 heads, 128 columns, 1.05 GB: 166 us a pass,
 // the join included, = 6.3 TB/s, 93% of the measured copy; with 44 of the 152 SMs, where memory does not bind it, it is
 // bound by its instructions (ALU pipe 56%).  As a warp joins nothing with its CTA's other warps, a share's partial
-// results cost 4 * D + 8 bytes a row.
+// results cost 4 * D + 8 bytes a row.  Batches with masked spans have an instance of their own (kMask), in which a row's
+// bits say which of its span's own tokens it sees.
 #include <type_traits>
 
 #include "kv_internal.cuh"
@@ -117,11 +118,12 @@ __device__ __forceinline__ uint32_t mask16(const uint32_t* row, int32_t at, int3
   return __funnelshift_r(lo, hi, (uint32_t)at % 32) & 0xFFFFu;
 }
 
-// A worker's pieces from `pl` on.  kMask: some are of masked spans.  kApart (fp8): the form for queries or value scales whose magnitudes lie far apart,
-// with keys, values, queries and probabilities in bf16, whose exponents reach as far as a float's; the other form leaves
-// it a piece (kTooFar), with nothing of it written, and the pieces after it.  5 requests of 131072 tokens, 256 queries on
-// 32768: 257 and 357 us, 166 and 248 by the other form.  The two are separate instances: as branches of a block they
-// cost the common form registers (178 and 260 us).
+// A worker's pieces from `pl` on.  kMask: some are of masked spans.
+// kApart (fp8): the form for queries or value scales whose magnitudes lie far apart, with keys, values, queries and
+// probabilities in bf16, whose exponents reach as far as a float's; the other form leaves it a piece (kTooFar), with
+// nothing of it written, and the pieces after it.  5 requests of 131072 tokens, 256 queries on 32768: 257 and 357 us, 166
+// and 248 by the other form.  The two are separate instances: as branches of a block they cost the common form registers
+// (178 and 260 us).
 template <int D, int FMT, bool kApart, bool kMask>
 __device__ __forceinline__ Step run_pieces(const AttnArgs& a, const PlanDev& p, const uint32_t ring, const uint32_t bar,
                                            Place& pl) {

@@ -5,8 +5,9 @@
 cache's format), ``write_rotated`` turns queries and keys by their positions on the way (``Rotary``), ``read`` gives back
 what the cache holds, ``attend`` computes attention of a batch that an ``AttentionPlan`` describes, a tree of drafted
 tokens among its forms (``tree_mask``), and ``move`` and ``copy_blocks`` copy what is held, token by token or in whole
-blocks.  All of them run on torch's current stream of the cache's device and return without waiting for it; what a kernel finds wrong raises ``PSError`` from the next call, or from ``check``.  They are
-operators of serving: no gradient goes through them, and their results are not part of autograd's graph.
+blocks.  All of them run on torch's current stream of the cache's device and return without waiting for it; what a kernel
+finds wrong raises ``PSError`` from the next call, or from ``check``.  They are operators of serving: no gradient goes
+through them, and their results are not part of autograd's graph.
 """
 from __future__ import annotations
 
@@ -262,7 +263,7 @@ class KVCache:
         h, n = self._open(), self._pairs(src, dst)
         stream = _stream(self.device)
         nb, ws = 0, None
-        if n > 1024:  # fewer need none
+        if n > 256:  # fewer need none
             c = ctypes.c_uint64()
             self._check(self._lib.ps_kv_move_workspace(h, n, ctypes.byref(c)))
             nb = c.value
@@ -293,7 +294,8 @@ class KVCache:
         h = self._open()
         if parents.dtype != torch.int32 or parents.get_device() != self.device or not parents.is_contiguous() or \
                 parents.dim() != (2 if offsets is None else 1):
-            raise ValueError(f"parents must be contiguous int32 on cuda:{self.device}, [trees, nodes] or a vector with offsets")
+            raise ValueError(f"parents must be contiguous int32 on cuda:{self.device}, [trees, nodes] or a vector with "
+                             "offsets")
         if offsets is None:
             trees, most = parents.shape
             new = torch.empty  # every row is a node's
@@ -343,8 +345,8 @@ class KVCache:
                 raise ValueError("the plan has masked spans: attend needs a mask")
             if mask.dtype != torch.int32 or mask.get_device() != self.device or mask.dim() != 2 or mask.shape[0] != n or \
                     32 * mask.shape[1] < plan.masked or (mask.shape[1] > 1 and mask.stride(1) != 1):
-                raise ValueError(f"mask must be int32 of shape [{n}, at least {-(-plan.masked // 32)}] on cuda:{self.device}, "
-                                 "a row's words next to each other")
+                raise ValueError(f"mask must be int32 of shape [{n}, at least {-(-plan.masked // 32)}] on "
+                                 f"cuda:{self.device}, a row's words next to each other")
         self._rows(0, q, "q", n, heads)
         out = self._out(_ROWS.size, out, "out", n, heads, None if out is not None else q.dtype)
         if lse is not None and (lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or
@@ -420,8 +422,9 @@ class AttentionPlan:
         b = np.ascontiguousarray(b)
         if not 0 <= int(num_queries) < 1 << 32:
             raise ValueError("num_queries must be in 0..2^32-1")
-        s = (L.ps_kv_plan_set_masked if masked else L.ps_kv_plan_set)(
-            h, int(num_queries), spans.ctypes.data if spans.size else None, spans.size, b.ctypes.data if b.size else None, b.size)
+        call = L.ps_kv_plan_set_masked if masked else L.ps_kv_plan_set
+        s = call(h, int(num_queries), spans.ctypes.data if spans.size else None, spans.size,
+                 b.ctypes.data if b.size else None, b.size)
         if s != PS_ERR_STATE:  # a plan that a CUDA graph holds stays as it is
             self.num_queries = self.workspace_bytes = self.masked = 0
         self.cache._check(s)

@@ -248,6 +248,29 @@ def test_many_rows_and_long_contexts(kv, fmt, D):  # noqa: F811
     d.cache.close()
 
 
+@pytest.mark.parametrize("fmt,Hkv,g,D", [("bf16", 1, 8, 128), ("fp8", 2, 2, 128), ("fp16", 1, 4, 64)])
+@pytest.mark.parametrize("n", [256, 257, 600])
+def test_large_drafts(kv, fmt, Hkv, g, D, n):  # noqa: F811
+    """As many own tokens as the tile kernel takes, and more, over several of its steps."""
+    for own in (0, 777):
+        T, spans, sees = batch([(own, n), (1500, 3)], kind="mask" if own else "any", seed=n)
+        d = Drafts(kv, fmt, Hkv, g, D, spans, T, sees, seed=n + own)
+        d.check(*d.run())
+        d.cache.close()
+
+
+@pytest.mark.parametrize("fmt,D", [("bf16", 128), ("fp8", 128), ("fp16", 64)])
+@pytest.mark.parametrize("shared,own", [(600, 40), (9000, 700)])
+def test_many_rows_to_join(kv, fmt, D, shared, own):  # noqa: F811
+    """More than 16384 rows with a few parts each; some queries see nothing at all."""
+    T, spans, sees = batch([(own, 29)] * 9 + [(0, 3)], kind="any", seed=12)
+    T2 = T + 2
+    spans = [(0, T - 3, shared, 0)] + spans
+    d = Drafts(kv, fmt, 8, 8, D, spans, T2, sees[:-3] + [set(), {0}, set()] + [set()] * 2, seed=13)
+    d.check(*d.run())
+    d.cache.close()
+
+
 def test_mixed_with_causal_spans(kv):  # noqa: F811
     """A batch of prefills, single tokens and drafts."""
     T, spans, sees = batch([(70, 20), (9, 40)], kind="any", seed=4)
