@@ -65,9 +65,10 @@ struct Row {
   }
 };
 
-// One row's 16 elements per lane (D / 16 lanes a row): the row's scale exponent, and this lane's codes.
+// One row's 16 elements per lane (D / 16 lanes a row): the row's scale exponent, and this lane's codes; at_border: whether
+// the row's maximum is within 2^-19 of where the exponent changes.
 template <int D>
-__device__ __forceinline__ uint4 quantise(const float (&x)[16], uint32_t* exp_code) {
+__device__ __forceinline__ uint4 quantise(const float (&x)[16], uint32_t* exp_code, bool* at_border = nullptr) {
   float amax = 0.0f;
   bool nan = false;
 #pragma unroll
@@ -84,6 +85,7 @@ __device__ __forceinline__ uint4 quantise(const float (&x)[16], uint32_t* exp_co
   // the smallest e with amax <= 1.75 * 2^(e + 8), from the float's exponent and mantissa fields; a
   // subnormal's fields give an e below the range, as they should
   const uint32_t b = __float_as_uint(amax);
+  if (at_border) *at_border = (b & 0x7FFFFFu) - (0x600000u - 16) <= 32;
   int e = (int)(b >> 23) - kExpBias - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   e = min(max(e, kExpMin), kExpMax);
   const float inv = __uint_as_float((uint32_t)(kExpBias - e) << 23);

@@ -242,3 +242,40 @@ def test_refusals(kv):
         with pytest.raises(P.PSError, match="overlap"):
             c.write_rotated(k, v, s, s, r, q=q, out=torch.empty(5, 1, 64, device="cuda", dtype=torch.bfloat16).expand(5, 4, 64))
         c.check()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp16", "fp8"])
+@pytest.mark.parametrize("interleaved,magnitude", [(False, 1.0), (True, 1.0), (False, 1.375)])
+def test_keys_are_rounded_once(kv, fmt, interleaved, magnitude):
+    """What the cache holds is the exact key's rounding, but where that lies within 2^-22 of what is mixed from a border: sine
+    and cosine are off by 2^-25 (with the magnitude 2^-24), a product and the sum of it and the other by as much again.
+    An fp8 row's scale is the exact row's, but where its maximum lies within 2^-26 of a border."""
+    T, H, D = 20000, 4, 128
+    _, k, v = _data(T, 1, H, D, "fp32" if fmt == "fp16" else "bf16", 11)
+    rotary = kv.Rotary(D, interleaved=interleaved, magnitude=magnitude)
+    positions = torch.randint(0, 1 << 17, (T,), device="cuda")
+    if fmt == "fp8":  # rows whose largest element, unturned, lies at a border of the scales or just beside it
+        positions[::2] = 0
+        k = k.float()
+        k[::2] *= (448.0 / magnitude / k[::2].abs().amax(-1, keepdim=True)) * (1 + torch.randint(-3, 4, (T // 2, H, 1), device="cuda") * 2.0 ** -23)
+        v = v.float()
+    slots = torch.randperm(T + 8, device="cuda")[:T].contiguous()
+    with kv.KVCache(T // 16 + 1, H, D, fmt=fmt) as c:
+        c.write_rotated(k, v, slots, positions, rotary)
+        got = c.read(slots, dtype=torch.float32)[0].double()
+        c.check()
+    want, mag = turned(k, positions, rotary)
+    if fmt == "fp8":
+        top = want.abs().amax(-1, keepdim=True)
+        e, least = (torch.ceil(torch.log2(x / 448.0)) for x in (top * (1 + 2.0 ** -26), top * (1 - 2.0 ** -26)))
+        same = (e == least).expand_as(want)
+        unit = torch.exp2(e)
+        step = lambda x: unit * torch.exp2(torch.floor(torch.log2((x / unit).abs().clamp(min=2.0 ** -6))) - 3)  # noqa: E731
+    else:
+        p, smallest = (8, -126) if fmt == "bf16" else (11, -14)  # significant bits, the smallest normal exponent
+        same = torch.ones_like(want, dtype=torch.bool)
+        step = lambda x: torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=2.0 ** smallest))) - (p - 1))  # noqa: E731
+    low, high = (torch.round(x / step(x)) * step(x) for x in (want - mag * 2.0 ** -22, want + mag * 2.0 ** -22))
+    clear = same & (low == high)
+    assert clear.double().mean() > (0.5 if fmt == "fp8" else 0.99)
+    assert torch.equal(got[clear], low[clear])
