@@ -151,8 +151,8 @@ PS_API ps_status ps_kv_tree_mask(ps_kv* kv, const int32_t* parents, uint64_t num
                                  uint32_t words, int64_t* positions, void* stream);
 
 /* Waits for the stream and returns what the kernels reported since the last report: PS_OK,
- * PS_ERR_INVALID (a slot outside the cache) or PS_ERR_TIMEOUT (a bounded wait of the attention gave up;
- * that call's outputs are not valid).  Error reporting only: no counterpart in the paper. */
+ * PS_ERR_INVALID (a slot or block outside the cache, a wrong tree) or PS_ERR_TIMEOUT (a bounded wait of the attention
+ * gave up; that call's outputs are not valid).  Error reporting only: no counterpart in the paper. */
 PS_API ps_status ps_kv_check(ps_kv* kv, void* stream);
 
 /* A plan: the spans of a batch, laid out for the device.  It is made once and set again for every step

@@ -89,7 +89,6 @@ class Rotary:
         f.flags.writeable = False
         self.frequencies = f
         self._c = PsKvRotary(self.dims, self.interleaved, self.magnitude, (ctypes.c_double * 64)(*f))
-        self._at = ctypes.addressof(self._c)
 
     def _scaled(self, base, scaling, factor, original, low, high):
         if not (base > 0 and factor > 0):
@@ -251,8 +250,8 @@ class KVCache:
             out = self._out(3 * _ROWS.size, out, "out", n, heads, self.dtype)
         elif out is not None:
             raise ValueError("out without q")
-        s = self._lib.ps_kv_write_rotated(h, rotary._at, positions.data_ptr(), q_at, out_at, heads, self._arg0, self._arg1,
-                                          slots.data_ptr(), n, _stream(self.device))
+        s = self._lib.ps_kv_write_rotated(h, ctypes.addressof(rotary._c), positions.data_ptr(), q_at, out_at, heads,
+                                          self._arg0, self._arg1, slots.data_ptr(), n, _stream(self.device))
         if s:
             self._check(s)
         return out
@@ -432,7 +431,7 @@ class AttentionPlan:
         self.cache._check(L.ps_kv_plan_workspace(h, ctypes.byref(n)))
         self.num_queries, self.workspace_bytes = int(num_queries), n.value
         if masked:
-            self.masked = int(max(spans["num_queries"][spans["causal"] == 2], default=0))
+            self.masked = int(spans["num_queries"][spans["causal"] == 2].max(initial=0))
 
     def close(self):
         if getattr(self, "_h", None):

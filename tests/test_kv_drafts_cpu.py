@@ -148,3 +148,10 @@ def test_spans_of_drafts(kv):
         assert [own[first[i]] for i in (0, 1)] == want
     with pytest.raises(ValueError):
         kv.shared_spans(tables, [90, 92], [20, 3], masked=[True])
+
+
+def test_a_rotary_can_be_copied(kv):
+    import copy
+    r = copy.deepcopy(kv.Rotary(32, interleaved=True, magnitude=1.5, scaling="linear", factor=2.0))
+    assert (r._c.dims, r._c.interleaved, r._c.magnitude) == (32, 1, 1.5)
+    np.testing.assert_array_equal(list(r._c.frequency)[:16], r.frequencies)
