@@ -115,6 +115,30 @@ def test_wrong_trees_are_reported(cache):
             cache.tree_mask(**bad)
 
 
+def test_captured_masks(cache):
+    """A replay reads the parents' memory anew; on another stream, beside calls on this one."""
+    parents = torch.empty(6, 100, dtype=torch.int32, device="cuda")
+    start = torch.arange(6, device="cuda") * 1000
+    rng = random.Random(3)
+    trees = [torch.tensor([tree(rng, 100, k) for _ in range(6)], dtype=torch.int32).cuda() for k in ("any", "near", "early", "chain")]
+    want = [cache.tree_mask(t, start=start) for t in trees]
+    parents.copy_(trees[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mask, pos = cache.tree_mask(parents, start=start)
+    s = torch.cuda.Stream()
+    for i in (1, 0, 3, 2):
+        parents.copy_(trees[i])
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            graph.replay()
+        other = cache.tree_mask(trees[3 - i], start=start)
+        torch.cuda.synchronize()
+        assert torch.equal(mask, want[i][0]) and torch.equal(pos, want[i][1])
+        assert torch.equal(other[0], want[3 - i][0]) and torch.equal(other[1], want[3 - i][1])
+    cache.check()
+
+
 # ---- attention
 
 class Drafts:
@@ -335,6 +359,49 @@ def test_tokens_that_are_not_finite(kv, fmt, D, g, own):  # noqa: F811
         assert torch.isposinf(out[only][..., 9]).all() and torch.isfinite(out[only][..., torch.arange(D, device="cuda") != 9]).all()
         only = sees_one(39) & ~five & ~sees_one(12) & ~sees_one(9)
         assert torch.isneginf(out[only]).all()
+    d.cache.close()
+
+
+@pytest.mark.parametrize("n,own", [(200, 3000), (2500, 333)])
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+def test_a_chain_is_a_causal_span(kv, fmt, n, own):  # noqa: F811
+    """A tree that is a chain sees what a causal span of the same tokens sees."""
+    D = 64
+    sees = [set()] * n
+    d = Drafts(kv, fmt, 1, 2, D, [(0, n, own + n, 2)], n, sees, seed=15)
+    mask, pos = d.cache.tree_mask(torch.arange(-1, n - 1, dtype=torch.int32, device="cuda")[None])
+    assert torch.equal(pos, torch.arange(n, device="cuda"))
+    out, lse = d.run(mask=mask)
+    causal = kv.AttentionPlan(d.cache, d.Hq, n, 1, len(d.ids))
+    causal.set(n, [(0, n, own + n, 1, 0)], d.ids)
+    lse2 = torch.empty_like(lse)
+    want = d.cache.attend(d.q, causal, lse=lse2)
+    d.cache.check()
+    # either is off by its own rounding and its probabilities', 2^-8 of the largest value each; scores are off by
+    # (D + 3) 2^-24 of sum |q| |k|, which the same fp32 products and sums bound by 2^-14 here
+    vmax = ref.held(fmt, d.v)[d.slots_of[0]].abs().max()
+    assert (out.double() - want.double()).abs().max() <= 4 * 2.0 ** -8 * 1.05 * vmax
+    assert (lse - lse2).abs().max() <= 2.0 ** -12
+    d.cache.close()
+
+
+def test_one_plan_on_two_streams(kv):  # noqa: F811
+    T, spans, sees = batch([(900, 50), (2000, 64), (10, 9)], shared=300, kind="any", seed=21)
+    d = Drafts(kv, "fp8", 2, 8, 128, spans, T, sees, seed=22)
+    masks = [d.mask, torch.randint(-(1 << 31), 1 << 31, d.mask.shape, device="cuda").int()]
+    want = [d.cache.attend(d.q, d.plan, mask=m) for m in masks]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(d.cache.attend(d.q, d.plan, mask=masks[i]))
+    torch.cuda.synchronize()
+    d.cache.check()
+    for i in range(2):
+        for x in got[i]:
+            assert torch.equal(x, want[i])
     d.cache.close()
 
 
