@@ -43,7 +43,9 @@ struct alignas(16) Piece {
   uint32_t part_row;  // first row of the partial result, or kDirect: the output is written
   uint16_t nrows;
   uint16_t head;
-  uint32_t fold0, nfold;  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in
+  // row kernel, kDirect: the tile kernel's parts of these rows, to be joined in; tile kernel: fold0 1: it runs beside the
+  // next piece
+  uint32_t fold0, nfold;
   // row kernel: 1: masked; tile kernel (masked where climit is a limit): not 0: its even steps in tile 0, its odd ones in
   // tile 1, so many rows behind
   uint32_t split;
@@ -415,6 +417,10 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   }
   const int tile_sms = o.row_sms < pl.sms ? pl.sms - o.row_sms : pl.sms;
   const uint32_t row_workers = (uint32_t)(o.row_sms * kRowWarps);
+  // In a masked batch pieces of one tile of rows run two at a time, where a worker has two: 32 drafts of 16 nodes on 800 to
+  // 1000 tokens 63 us, 50 two at a time; one of 16 nodes after the other's end otherwise, its latencies in the open.
+  const uint32_t tile_workers = (uint32_t)std::max(1, tile_sms / tile_ctas_of((int)pl.D));
+  const bool may_split = !o.mask_tiles || o.tile_units.size() < 2 * (size_t)tile_workers;
   auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
@@ -422,7 +428,7 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
       // a tile piece that is split by steps has two parts
       uint32_t nparts = 0;
       for (uint32_t k = a; k < b; ++k) {
-        if (!rows && pl.D == 128 && p.nrows <= tile_rows_of(128) / 2 && pieces[k].nblocks >= kSplitSteps)
+        if (!rows && may_split && pl.D == 128 && p.nrows <= tile_rows_of(128) / 2 && pieces[k].nblocks >= kSplitSteps)
           pieces[k].split = units[i].tile_rows;
         nparts += !rows && pieces[k].split ? 2 : 1;
       }
@@ -445,9 +451,14 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   };
   std::vector<uint32_t> first;
   if (!o.tile_units.empty()) {
-    const uint32_t workers = (uint32_t)std::max(1, tile_sms / tile_ctas_of((int)pl.D));
-    share_out(o.tile_units, workers, 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
+    share_out(o.tile_units, tile_workers, 4, 2, kTileKeys / kBlock, &o.tile_pieces, &o.tile_off, &first);
     finish(o.tile_units, o.tile_pieces, first, false);
+    const auto one_tile = [&](const Piece& p) {
+      return !p.split && p.nrows <= tile_rows_of((int)pl.D) / 2;
+    };
+    for (size_t w = 0; o.mask_tiles && w + 1 < o.tile_off.size(); ++w)
+      for (uint32_t i = o.tile_off[w]; i + 1 < o.tile_off[w + 1]; ++i)
+        if (one_tile(o.tile_pieces[i]) && one_tile(o.tile_pieces[i + 1])) o.tile_pieces[i++].fold0 = 1;
   }
   if (!o.row_units.empty()) {
     share_out(o.row_units, row_workers, 2, 2, 1, &o.row_pieces, &o.row_off, &first);

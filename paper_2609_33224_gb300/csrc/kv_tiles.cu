@@ -262,6 +262,31 @@ __device__ __forceinline__ uint32_t first_masked(const Piece& p) {
   return p.climit >= (int32_t)p.key0 ? (uint32_t)(p.climit - (int32_t)p.key0) / kTileKeys : 0;
 }
 
+// What a role needs of a piece at every step.
+struct Steps {
+  uint32_t count, keys, masked0, key0;
+  int32_t climit;
+};
+template <bool kMask>
+__device__ __forceinline__ Steps steps_of(const Piece& p) {
+  return Steps{p.nblocks, p.end - p.key0, kMask ? first_masked(p) : 0xFFFFFFFFu, p.key0, p.climit};
+}
+// Piece pi and, if two, the one after it, which then runs beside it (kMask): each is of one tile of rows, the first is
+// tile 0, the second tile 1, and they take turns: step 0 of the first, step 0 of the second, step 1 of the first, and so
+// on, the longer one's last steps alone.
+struct Group {
+  Piece x, y;
+  bool two;
+};
+template <bool kMask>
+__device__ __forceinline__ Group group_of(const PlanDev& p, uint32_t pi) {
+  Group g;
+  g.x = p.tile_pieces[pi];
+  g.two = kMask && g.x.fold0;
+  if (g.two) g.y = p.tile_pieces[pi + 1];
+  return g;
+}
+
 // Which panels of 64 columns of token `tok`'s value row hold a value that is not finite (bits), by a whole warp.
 template <int D, int FMT>
 __device__ __forceinline__ uint32_t odd_panels(const uint8_t* rec, uint32_t tok, uint32_t lane) {
@@ -349,12 +374,18 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
     uint32_t steps = 0, done = 0;  // phases of s_full; of o_done
     bool alive = true;
-    for (uint32_t pi = first; alive && pi < last; ++pi) {
-      const Piece pc = p.tile_pieces[pi];
+    for (uint32_t pi = first, take; alive && pi < last; pi += take) {
+      // (16 bits: which piece is found before it is loaded, fp8: with it; the other way round a % longer, for registers)
+      Piece pc;
+      if (C::kFp8) pc = p.tile_pieces[pi];
+      const bool two = kMask && (C::kFp8 ? pc.fold0 : p.tile_pieces[pi].fold0);
+      take = two ? 2 : 1;
+      if (!C::kFp8 || (two && t)) pc = p.tile_pieces[pi + (two ? t : 0)];
       if (pi == first) wait_for_last();  // the plan is read before, queries and results' places after
       const uint32_t masked0 = kMask ? first_masked(pc) : 0;
-      if (!pc.split && t * C::kRows >= pc.nrows) continue;
-      const uint32_t in_tile = (pc.split ? 0 : t * C::kRows) + rank * 128 + r;
+      const uint32_t tile_row = pc.split || two ? 0 : t * C::kRows;
+      if (!pc.split && tile_row >= pc.nrows) continue;
+      const uint32_t in_tile = tile_row + rank * 128 + r;
       const uint32_t row = pc.row0 + in_tile;
       const bool valid = in_tile < pc.nrows;
       const uint32_t query = pc.query0 + row / a.group, head = pc.head * a.group + row % a.group;
@@ -527,7 +558,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       }
       const bool direct = pc.part_row == kDirect;
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      const uint64_t at = (uint64_t)pc.part_row + t * (pc.split ? pc.split : C::kRows) + rank * 128 + r;
+      const uint64_t at = (uint64_t)pc.part_row + (pc.split ? t * pc.split : tile_row) + rank * 128 + r;
       // The queries are used up: their shared memory takes the warp's 32 rows, half of their columns at a time, from
       // which whole rows are stored by neighbouring lanes.  A warp uses the place of its own queries alone, 4 KB in
       // each panel: the tile's other warps may be at this or already at their next piece's queries.
@@ -597,7 +628,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegRest));
     if (warp == 8) {
       // ================= copies: a step's keys, then its values (fp8: all at once) =================
-      uint32_t n = 0, ids = 0;  // slots (fp8: raw stages) filled
+      uint32_t n = 0;  // slots (fp8: raw stages) filled
       constexpr uint32_t kN = C::kFp8 ? (C::kRaws ? C::kRaws : 1) : C::kSlots;
       // The copies of this lane: 16-bit keys (2 KB panels of this CTA's blocks) and values (its panel of
       // every block), or fp8 keys, values and exponents.  blk: the block of the step; from: in its record.
@@ -635,34 +666,47 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       wait_for_last();
       let_next_start();  // the row kernel, which does not wait for what came before this one
       bool alive = true, begun = false;
-      for (uint32_t pi = first; alive && pi < last; ++pi) {
-        const Piece* pp = p.tile_pieces + pi;
-        const uint32_t steps = pp->nblocks, block = pp->block, head = pp->head, key0 = pp->key0, end = pp->end;
-        const uint32_t nb = (end - key0 + kBlock - 1) / kBlock;  // blocks from here to the span's end
-        for (uint32_t j = 0; alive && j < steps; ++j) {
-          if ((j & 3u) == 0) ids = p.blocks[block + min(j * 8 + lane, nb - 1)];
-          const uint32_t live = min(nb - j * 8, 8u);
+      for (uint32_t pi = first, take; alive && pi < last; pi += take) {
+        const Group gp = group_of<kMask>(p, pi);
+        take = gp.two ? 2 : 1;
+        uint32_t steps[2] = {0, 0}, block[2], head[2], nb[2], ids[2];
 #pragma unroll
-          for (uint32_t part = 0; part < (C::kFp8 ? 1u : 2u); ++part, ++n) {
-            const uint32_t at = n % kN;
-            const uint32_t fb = C::kFp8 ? smem_u32(&bars.raw_full[at % 4]) : full(at);
-            const uint32_t eb = C::kFp8 ? smem_u32(&bars.raw_empty[at % 4]) : empty(at);
-            if (n >= kN) {
-              if (!begun) wait_worker<C::kCtas>();
-              begun = true;
-              if (!mbar_wait_warp(eb, (n / kN - 1) & 1)) {
-                alive = false;
-                break;
+        for (uint32_t t = 0; t < (kMask ? 2u : 1u); ++t) {
+          if (t && !gp.two) continue;
+          const Piece& pp = t ? gp.y : gp.x;
+          steps[t] = pp.nblocks;
+          block[t] = pp.block;
+          head[t] = pp.head;
+          nb[t] = (pp.end - pp.key0 + kBlock - 1) / kBlock;  // blocks from here to the span's end
+        }
+        for (uint32_t j = 0; alive && j < max(steps[0], steps[1]); ++j) {
+#pragma unroll
+          for (uint32_t t = 0; t < (kMask ? 2u : 1u); ++t) {
+            if (!alive || j >= steps[t]) continue;
+            if ((j & 3u) == 0) ids[t] = p.blocks[block[t] + min(j * 8 + lane, nb[t] - 1)];
+            const uint32_t live = min(nb[t] - j * 8, 8u);
+#pragma unroll
+            for (uint32_t part = 0; part < (C::kFp8 ? 1u : 2u); ++part, ++n) {
+              const uint32_t at = n % kN;
+              const uint32_t fb = C::kFp8 ? smem_u32(&bars.raw_full[at % 4]) : full(at);
+              const uint32_t eb = C::kFp8 ? smem_u32(&bars.raw_empty[at % 4]) : empty(at);
+              if (n >= kN) {
+                if (!begun) wait_worker<C::kCtas>();
+                begun = true;
+                if (!mbar_wait_warp(eb, (n / kN - 1) & 1)) {
+                  alive = false;
+                  break;
+                }
               }
+              const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids[t], (j & 3u) * 8 + blk[part]);
+              const uint32_t mine = blk[part] < live ? bytes[part] : 0u;
+              const uint32_t sum = __reduce_add_sync(0xFFFFFFFFu, mine);
+              if (lane == 0) mbar_expect(fb, sum);
+              __syncwarp();
+              if (mine)
+                bulk_load((C::kFp8 ? raw_ring + at * C::kRaw : ring + at * C::kSlot) + to[part],
+                          a.pool + ((uint64_t)id * a.kv_heads + head[t]) * C::kRec + from[part], mine, fb);
             }
-            const uint32_t id = __shfl_sync(0xFFFFFFFFu, ids, (j & 3u) * 8 + blk[part]);
-            const uint32_t mine = blk[part] < live ? bytes[part] : 0u;
-            const uint32_t sum = __reduce_add_sync(0xFFFFFFFFu, mine);
-            if (lane == 0) mbar_expect(fb, sum);
-            __syncwarp();
-            if (mine)
-              bulk_load((C::kFp8 ? raw_ring + at * C::kRaw : ring + at * C::kSlot) + to[part],
-                        a.pool + ((uint64_t)id * a.kv_heads + head) * C::kRec + from[part], mine, fb);
           }
         }
       }
@@ -697,7 +741,55 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
                               acc || k > 0);
       };
       for (uint32_t pi = first; alive && pi < last; ++pi) {
-        const Piece* pp = p.tile_pieces + pi;
+        const Group gp = group_of<kMask>(p, pi);
+        const Piece* pp = &gp.x;
+        if (gp.two) {
+          const Steps x = steps_of<kMask>(gp.x), y = steps_of<kMask>(gp.y);
+          const uint32_t n0 = n, both = min(x.count, y.count);
+          // where step j of tile t has its keys; its values come next
+          auto place = [&](uint32_t t, uint32_t j) { return n0 + 2 * (j < both ? 2 * j + t : both + j); };
+          auto here = [&](uint32_t i) { return wait(full(i % C::kSlots), (i / C::kSlots) & 1u); };
+          auto begin = [&](uint32_t t, uint32_t j) {  // its scores
+            const uint32_t i = place(t, j);
+            if (!here(i)) return false;
+            scores(t, i % C::kSlots);
+            tc_commit<C::kCtas>(smem_u32(&bars.s_full[t]));
+            tc_commit<C::kCtas>(empty(i % C::kSlots));
+            return true;
+          };
+          for (uint32_t t = 0; t < 2; ++t) {
+            if (!wait(smem_u32(&bars.q_ready[t]), q_seen[t] & 1)) break;
+            ++q_seen[t];
+            tc_fence_after();
+            if (!begin(t, 0)) break;
+          }
+          for (uint32_t j = 0; alive && j < max(x.count, y.count); ++j)
+            for (uint32_t t = 0; alive && t < 2; ++t) {
+              const Steps& z = t ? y : x;
+              if (j >= z.count) continue;
+              const uint32_t i = place(t, j) + 1;
+              if (!here(i)) break;
+              if (!C::kFp8 && (z.keys < (j + 1) * kTileKeys || j >= z.masked0)) {
+                mbar_arrive(smem_u32(&bars.tail_here));
+                if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
+              }
+              for (int half = 0; half < 2; ++half) {
+                if (!wait(smem_u32(&bars.p_ready[t][half]), p_seen[t] & 1)) break;
+                tc_fence_after();
+                values(t, i % C::kSlots, half, half > 0 || j > 0);
+              }
+              if (!alive) break;
+              ++p_seen[t];
+              if (j + 1 == z.count)
+                tc_commit<C::kCtas>(smem_u32(&bars.o_done[t]));
+              else if (!begin(t, j + 1))
+                break;
+              tc_commit<C::kCtas>(empty(i % C::kSlots));
+            }
+          n = n0 + 2 * (x.count + y.count);
+          ++pi;
+          continue;
+        }
         const uint32_t steps = pp->nblocks, keys = pp->end - pp->key0;
         const uint32_t tiles = pp->nrows > C::kRows ? 2 : 1;
         const uint32_t masked0 = kMask ? first_masked(*pp) : 0;
@@ -764,20 +856,25 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       // ================= the pair's second CTA: tells the first what has arrived here =================
       uint32_t n = 0, tails = 0;
       bool alive = true;
-      for (uint32_t pi = first; alive && pi < last; ++pi) {
-        const Piece* pp = p.tile_pieces + pi;
-        const uint32_t slots = 2 * pp->nblocks;
-        const bool partial = pp->end - pp->key0 < pp->nblocks * kTileKeys;
-        const uint32_t masked0 = kMask ? first_masked(*pp) : 0;
-        for (uint32_t i = 0; alive && i < slots; ++i, ++n) {
-          const uint32_t at = n % C::kSlots;
-          alive = mbar_wait(full(at), (n / C::kSlots) & 1);
-          if (alive && ((partial && i == slots - 1) || (kMask && i % 2 == 1 && i / 2 >= masked0))) {
-            mbar_arrive(smem_u32(&bars.tail_here));
-            alive = mbar_wait(smem_u32(&bars.tail_done), tails++ & 1);
+      for (uint32_t pi = first, take; alive && pi < last; pi += take) {
+        const Group gp = group_of<kMask>(p, pi);
+        take = gp.two ? 2 : 1;
+        const Steps x = steps_of<kMask>(gp.x), y = gp.two ? steps_of<kMask>(gp.y) : Steps{0, 0, 0, 0, 0};
+        for (uint32_t j = 0; alive && j < max(x.count, y.count); ++j)
+          for (uint32_t t = 0; alive && t < take; ++t) {
+            const Steps& z = t ? y : x;
+            if (j >= z.count) continue;
+            const bool tail = z.keys < (j + 1) * kTileKeys || j >= z.masked0;
+            for (uint32_t part = 0; alive && part < 2; ++part, ++n) {
+              const uint32_t at = n % C::kSlots;
+              alive = mbar_wait(full(at), (n / C::kSlots) & 1);
+              if (alive && part && tail) {
+                mbar_arrive(smem_u32(&bars.tail_here));
+                alive = mbar_wait(smem_u32(&bars.tail_done), tails++ & 1);
+              }
+              if (alive) arrive_first<C::kCtas>(full(at));
+            }
           }
-          if (alive) arrive_first<C::kCtas>(full(at));
-        }
       }
       if (!alive) {
         atomicOr_system(a.err, kErrWait);
@@ -813,23 +910,27 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       // A token that a row does not see has a probability of 0 there, but 0 times an infinity or a NaN is not: an own
       // token's values (here: this CTA's panel of them) are taken out of the product where one of them is not finite, and
       // rows that see the token add them at the piece's end.
-      uint32_t n = 0, tails = 0;
-      bool alive = true;
-      for (uint32_t pi = first; alive && pi < last; ++pi) {
-        const Piece* pp = p.tile_pieces + pi;
-        const uint32_t n0 = n, steps = pp->nblocks, key0 = pp->key0, end = pp->end, masked0 = first_masked(*pp);
-        const uint32_t own = masked0 < steps ? (uint32_t)pp->climit : end;
-        n += 2 * steps;
-        for (uint32_t j = min(masked0, end - key0 < steps * kTileKeys ? steps - 1 : steps); j < steps; ++j) {
+      uint32_t items = 0, tails = 0;  // steps so far
+      bool alive = true, more = true;
+      for (uint32_t pi = first, take; alive && more && pi < last; pi += take) {
+        const Group gp = group_of<kMask>(p, pi);
+        take = gp.two ? 2 : 1;
+        const Steps x = steps_of<kMask>(gp.x), y = gp.two ? steps_of<kMask>(gp.y) : Steps{0, 0, 0, 0, 0};
+        for (uint32_t j = 0, t = 0; alive && more && j < max(x.count, y.count); t + 1 < take ? ++t : (t = 0, ++j)) {
+          const Steps& z = t ? y : x;
+          if (j >= z.count) continue;
+          const uint32_t item = items++, key0 = z.key0, end = z.key0 + z.keys;
+          if (j < z.masked0 && z.keys >= (j + 1) * kTileKeys) continue;
+          const uint32_t own = z.masked0 < z.count ? (uint32_t)z.climit : end;
           if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars.tail_here), tails++ & 1, 60000000000ull))) {
             alive = false;
             break;
           }
           if (*static_cast<volatile uint32_t*>(&bars.gave_up)) {  // no step comes any more
-            pi = last;
+            more = false;
             break;
           }
-          const uint32_t v = ring + (n0 + 2 * j + 1) % C::kSlots * C::kSlot;
+          const uint32_t v = ring + (2 * item + 1) % C::kSlots * C::kSlot;
           bool any = false;
 #pragma unroll 1
           for (uint32_t i = lane; i < kTileKeys; i += 32) {
@@ -873,10 +974,14 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       constexpr uint32_t kOwn = C::kKeys / kBlock;
       uint32_t n = 0, raws = 0;
       bool alive = true;
-      for (uint32_t pi = first; alive && pi < last; ++pi) {
-        const Piece* pp = p.tile_pieces + pi;
-        const uint32_t steps = pp->nblocks, keys = pp->end - pp->key0;
-        for (uint32_t j = 0; alive && j < steps; ++j, ++raws) {
+      for (uint32_t pi = first, take; alive && pi < last; pi += take) {
+        const Group gp = group_of<kMask>(p, pi);
+        take = gp.two ? 2 : 1;
+        const Steps x = steps_of<kMask>(gp.x), y = gp.two ? steps_of<kMask>(gp.y) : Steps{0, 0, 0, 0, 0};
+        for (uint32_t j = 0, t = 0; alive && j < max(x.count, y.count); t + 1 < take ? ++t : (t = 0, ++j)) {
+          const Steps& z = kMask && t ? y : x;
+          if (kMask && j >= z.count) continue;
+          const uint32_t keys = z.keys;
           const uint32_t rs = raws % C::kRaws;
           if (!mbar_wait_warp(smem_u32(&bars.raw_full[rs]), (raws / C::kRaws) & 1)) {
             alive = false;
@@ -906,7 +1011,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
               const uint32_t at_e = exps + vb * 32 + kBlock + exp_place(tok % kBlock);
               uint32_t e = live ? lds8(at_e) : (uint32_t)kExpBias;
               // a marked row's codes are zeros: with another scale it is out of the product
-              if (kMask && e == kExpNan && (int32_t)(pp->key0 + j * kTileKeys + tok) >= pp->climit) {
+              if (kMask && e == kExpNan && (int32_t)(z.key0 + j * kTileKeys + tok) >= z.climit) {
                 e = kExpBias;
                 *static_cast<volatile uint32_t*>(&bars.odd) = 1;
               }
@@ -919,6 +1024,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
             if (lane == 0) arrive_first<C::kCtas>(full(at));
           }
           if (alive && lane == 0) mbar_arrive(smem_u32(&bars.raw_empty[rs]));
+          ++raws;
         }
       }
       if (!alive && tok == 0) atomicOr_system(a.err, kErrWait);

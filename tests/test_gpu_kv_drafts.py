@@ -295,6 +295,31 @@ def test_many_rows_to_join(kv, fmt, D, shared, own):  # noqa: F811
     d.cache.close()
 
 
+@pytest.mark.parametrize("fmt,D,g", [("bf16", 128, 16), ("fp8", 128, 16), ("fp16", 128, 8), ("fp16", 64, 8), ("fp8", 64, 8)])
+def test_many_small_drafts(kv, fmt, D, g):  # noqa: F811
+    """Several pieces of one tile of rows a worker of the tile kernel, of uneven lengths, two at a time; then with values of
+    drafted tokens that are not finite, which reach the queries that see them and no other."""
+    rng = random.Random(6)
+    T, spans, sees = batch([(rng.choice([130, 300, 700, 1000]) + rng.randrange(40), rng.randrange(8, 16)) for _ in range(30)],
+                           kind="any", seed=14)
+    d = Drafts(kv, fmt, 8, g, D, spans, T, sees, seed=16)
+    out, lse = d.run()
+    d.check(out, lse)
+    for _ in range(5):
+        assert torch.equal(d.run()[0], out)
+    hit = torch.zeros(T, dtype=torch.bool, device="cuda")
+    for (f, n, length, kind, _), sl in zip(d.spans, d.slots_of):
+        for j in rng.sample(range(n), 2):
+            d.v[sl[length - n + j], :, rng.randrange(D)] = math.nan
+            hit |= torch.tensor([f <= t < f + n and j in sees[t] for t in range(T)], device="cuda")
+    d.write()
+    bad, _ = d.run()
+    assert torch.isnan(bad).any(-1).all(-1)[hit].all()
+    want, _, tol, _, _ = d.expected()
+    assert ((bad.double() - want).abs() <= tol)[~hit].all()
+    d.cache.close()
+
+
 def test_mixed_with_causal_spans(kv):  # noqa: F811
     """A batch of prefills, single tokens and drafts."""
     T, spans, sees = batch([(70, 20), (9, 40)], kind="any", seed=4)

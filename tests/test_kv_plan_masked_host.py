@@ -26,7 +26,16 @@ def plan(tmp_path_factory):
             ("else CHECK((long)p.climit ==", "else if (!masked) CHECK((long)p.climit =="),
             (": s.causal ? std::min<long>", ": s.causal == 1 ? std::min<long>"),
             ("x < (p.split ? 2u : 1u)", "x < (kind && p.split ? 2u : 1u)"),
-            ("if (p.split) CHECK(kind &&", "if (kind && p.split) CHECK(kind &&")):
+            ("if (p.split) CHECK(kind &&", "if (kind && p.split) CHECK(kind &&"),
+            # pieces side by side are neighbours of one worker, of one tile of rows each, and no piece is in two pairs
+            ("const unsigned step = kind ? kTileKeys : kBlock;", "const unsigned step = kind ? kTileKeys : kBlock;\n"
+             "        if (kind && p.fold0) {\n"
+             "          const size_t at = &p - pieces.data(), w = std::upper_bound(off.begin(), off.end(), at) - off.begin();\n"
+             "          CHECK(o.mask_tiles && at + 1 < off[w] && !pieces[at + 1].fold0 && p.fold0 == 1);\n"
+             "          for (size_t x = at; x < at + 2; ++x) CHECK(!pieces[x].split && (int)pieces[x].nrows <= tile_rows_of(D) / 2);\n"
+             "          ++pairs;\n"
+             "        }"),
+            ("const unsigned workers = kind ?", "static unsigned pairs = 0;\n      const unsigned workers = kind ?")):
         assert text.count(old) == 1, old
         text = text.replace(old, new)
     src.write_text(text)
@@ -68,7 +77,10 @@ def test_forms(plan):
         ((4, 128, 0, 2, 8, 300), [(0, 300, 500, 0)] + [(i * 30, 30, 60, 2) for i in range(10)]),
         # alone: written by the row kernel
         ((152, 64, 1, 1, 1, 16), [(0, 16, 16, 2)]),
+        # many of one tile
+        ((152, 128, 0, 8, 8, 512), [(16 * i, 16, 916 + i, 2) for i in range(32)]),
     ])
+    assert not got[4][0] and got[4][1]
     assert not got[0][0] and got[0][1] and got[1][0] and got[1][1]
     assert got[2][3] > 0
     assert got[3] == (1, 0, 0, 0)
