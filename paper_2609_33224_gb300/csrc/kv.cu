@@ -347,6 +347,7 @@ ps_status plan_set(ps_kv_plan* pl, uint32_t T, const ps_kv_span* spans, uint32_t
   d.join_parts = o.join_parts;
   d.mask_rows = o.mask_rows;
   d.mask_tiles = o.mask_tiles;
+  d.pairs = o.pairs;
   d.blocks = reinterpret_cast<const uint32_t*>(b.dev + bl);
   pl->dev = d;
   pl->cur ^= 1;

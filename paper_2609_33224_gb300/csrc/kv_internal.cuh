@@ -62,6 +62,7 @@ struct PlanDev {
   uint32_t max_parts;   // of a span's rows
   uint32_t join_parts;  // of an entry, at most
   uint32_t mask_rows, mask_tiles;  // whether a kernel has pieces with own tokens of masked spans
+  uint32_t pairs;                  // tile pieces that run beside the next one
   const uint32_t* blocks;
 };
 

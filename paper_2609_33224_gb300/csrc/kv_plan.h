@@ -119,8 +119,8 @@ inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool 
 }
 
 // The same for all keys of a masked span.  By rows they cost about twice as much as a plain span's, in pieces that end with
-// masked blocks (32 drafts of 32 nodes on 300 to 500 tokens, 4 query heads a key/value head: 44 us by tiles, 51 by rows; 16
-// of 8 nodes on 1500 to 2000 45 and 53; 60 of 4 nodes on 2000 to 3000, fp8, 187 and 127).  Where the rows have a prefix
+// masked blocks (32 drafts of 32 nodes on 300 to 500 tokens, 4 query heads a key/value head: 34 us by tiles, 51 by rows; 16
+// of 8 nodes on 1500 to 2000 38 and 53; 60 of 4 nodes on 2000 to 3000, fp8, 187 and 127).  Where the rows have a prefix
 // too, the tile kernel's results are to be joined with the prefix's, which the row kernel can do as it goes: 32 drafts
 // of 48 nodes on 30 tokens or less and 8000 shared ones 343 by tiles, 292 by rows; 60 of 8 to 12 nodes on 50 to 300 and
 // 4000, fp8, 117 and 110; 60 of up to 31 on up to 700 and 16384, fp8, 441 with all of them that the first rule would
@@ -196,6 +196,7 @@ struct Layout {
   uint32_t join_stride = 0;  // the largest entry's count
   uint32_t join_parts = 0;   // and number of parts
   bool mask_rows = false, mask_tiles = false;  // pieces with own tokens of masked spans
+  uint32_t pairs = 0;  // tile pieces that run beside the next one
   int row_sms = 0;  // SMs of the row kernel; fewer than all: beside the tile kernel
 };
 
@@ -417,10 +418,11 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   }
   const int tile_sms = o.row_sms < pl.sms ? pl.sms - o.row_sms : pl.sms;
   const uint32_t row_workers = (uint32_t)(o.row_sms * kRowWarps);
-  // In a masked batch pieces of one tile of rows run two at a time, where a worker has two: 32 drafts of 16 nodes on 800 to
-  // 1000 tokens 63 us, 50 two at a time; one of 16 nodes after the other's end otherwise, its latencies in the open.
+  // In a masked batch pieces of one tile of rows run two at a time, where there are enough of them, instead of each as two
+  // by parity, which leaves two results: 96 units for 76 workers (12 drafts of 16 nodes on up to 3000 tokens) 47.7 us and
+  // 50.9, 256 units on up to 1000 48.7 and 59.7 (62.8 one after the other); with 64 units on up to 8000 77.6 and 70.9.
   const uint32_t tile_workers = (uint32_t)std::max(1, tile_sms / tile_ctas_of((int)pl.D));
-  const bool may_split = !o.mask_tiles || o.tile_units.size() < 2 * (size_t)tile_workers;
+  const bool may_split = !o.mask_tiles || o.tile_units.size() < tile_workers;
   auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {
     for (size_t i = 0; i < units.size(); ++i) {
       const uint32_t a = first[i], b = i + 1 < units.size() ? first[i + 1] : (uint32_t)pieces.size();
@@ -458,7 +460,10 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
     };
     for (size_t w = 0; o.mask_tiles && w + 1 < o.tile_off.size(); ++w)
       for (uint32_t i = o.tile_off[w]; i + 1 < o.tile_off[w + 1]; ++i)
-        if (one_tile(o.tile_pieces[i]) && one_tile(o.tile_pieces[i + 1])) o.tile_pieces[i++].fold0 = 1;
+        if (one_tile(o.tile_pieces[i]) && one_tile(o.tile_pieces[i + 1])) {
+          o.tile_pieces[i++].fold0 = 1;
+          ++o.pairs;
+        }
   }
   if (!o.row_units.empty()) {
     share_out(o.row_units, row_workers, 2, 2, 1, &o.row_pieces, &o.row_off, &first);

@@ -21,11 +21,13 @@
 //
 // Keys here are seen by all rows: the plan gives the ends of causal spans to the row kernel.  Only a span's
 // last step can be partial; its scores past the end are masked, and its value rows past the end zeroed.
-// Masked spans, whose own tokens a row sees by its bits, are taken whole, in an instance of the kernel of their own (kMask):
+// Masked spans, whose own tokens a row sees by its bits, are taken whole, in instances of the kernel of their own (kMask):
 // their last steps' scores are masked by four words a row, and own tokens' value rows that are not finite are zeroed too,
 // as 0 times an infinity is no zero, and added at the end for the rows that see them.  32 trees of 40 to 64 nodes on 3000
 // to 5000 tokens, 64 query and 8 key/value heads, 219 GFLOP: 188 us (1.17 PFLOP/s; a tile's 256 rows are 80% filled), 245
-// with the drafted tokens by the row kernel and joined.
+// with the drafted tokens by the row kernel and joined.  There, pieces of one tile of rows run two at a time, the second as
+// tile 1, so that one's softmax, start and end lie beside the other's steps: 32 trees of 16 nodes on 800 to 1000 tokens 49
+// us, 63 one after the other.
 //
 // Bound by the tensor cores for full tiles: 4 * D multiply-adds a row and key, and, near that, the
 // exponentials: one per row and key.  Work is cut into equal shares per worker; each walks its pieces.
@@ -271,18 +273,18 @@ template <bool kMask>
 __device__ __forceinline__ Steps steps_of(const Piece& p) {
   return Steps{p.nblocks, p.end - p.key0, kMask ? first_masked(p) : 0xFFFFFFFFu, p.key0, p.climit};
 }
-// Piece pi and, if two, the one after it, which then runs beside it (kMask): each is of one tile of rows, the first is
+// Piece pi and, if two, the one after it, which then runs beside it (kInPairs): each is of one tile of rows, the first is
 // tile 0, the second tile 1, and they take turns: step 0 of the first, step 0 of the second, step 1 of the first, and so
 // on, the longer one's last steps alone.
 struct Group {
   Piece x, y;
   bool two;
 };
-template <bool kMask>
+template <bool kPairs>
 __device__ __forceinline__ Group group_of(const PlanDev& p, uint32_t pi) {
   Group g;
   g.x = p.tile_pieces[pi];
-  g.two = kMask && g.x.fold0;
+  g.two = kPairs && g.x.fold0;
   if (g.two) g.y = p.tile_pieces[pi + 1];
   return g;
 }
@@ -314,9 +316,13 @@ __device__ __forceinline__ void set_in_both(uint32_t addr) {
   }
 }
 
-template <int D, int FMT, bool kMask>
+// What spans an instance of the kernel is for: it has what they need, and no more.
+enum Form { kPlain, kDrafts, kInPairs };  // kInPairs: drafts, some pieces two at a time
+
+template <int D, int FMT, int FORM>
 __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(const AttnArgs a, const PlanDev p) {
   using C = Cfg<D, FMT>;
+  constexpr bool kMask = FORM != kPlain, kPairs = FORM == kInPairs;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) Bars bars;
   const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
@@ -378,7 +384,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       // (16 bits: which piece is found before it is loaded, fp8: with it; the other way round a % longer, for registers)
       Piece pc;
       if (C::kFp8) pc = p.tile_pieces[pi];
-      const bool two = kMask && (C::kFp8 ? pc.fold0 : p.tile_pieces[pi].fold0);
+      const bool two = kPairs && (C::kFp8 ? pc.fold0 : p.tile_pieces[pi].fold0);
       take = two ? 2 : 1;
       if (!C::kFp8 || (two && t)) pc = p.tile_pieces[pi + (two ? t : 0)];
       if (pi == first) wait_for_last();  // the plan is read before, queries and results' places after
@@ -667,11 +673,11 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       let_next_start();  // the row kernel, which does not wait for what came before this one
       bool alive = true, begun = false;
       for (uint32_t pi = first, take; alive && pi < last; pi += take) {
-        const Group gp = group_of<kMask>(p, pi);
+        const Group gp = group_of<kPairs>(p, pi);
         take = gp.two ? 2 : 1;
         uint32_t steps[2] = {0, 0}, block[2], head[2], nb[2], ids[2];
 #pragma unroll
-        for (uint32_t t = 0; t < (kMask ? 2u : 1u); ++t) {
+        for (uint32_t t = 0; t < (kPairs ? 2u : 1u); ++t) {
           if (t && !gp.two) continue;
           const Piece& pp = t ? gp.y : gp.x;
           steps[t] = pp.nblocks;
@@ -681,7 +687,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         }
         for (uint32_t j = 0; alive && j < max(steps[0], steps[1]); ++j) {
 #pragma unroll
-          for (uint32_t t = 0; t < (kMask ? 2u : 1u); ++t) {
+          for (uint32_t t = 0; t < (kPairs ? 2u : 1u); ++t) {
             if (!alive || j >= steps[t]) continue;
             if ((j & 3u) == 0) ids[t] = p.blocks[block[t] + min(j * 8 + lane, nb[t] - 1)];
             const uint32_t live = min(nb[t] - j * 8, 8u);
@@ -741,7 +747,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
                               acc || k > 0);
       };
       for (uint32_t pi = first; alive && pi < last; ++pi) {
-        const Group gp = group_of<kMask>(p, pi);
+        const Group gp = group_of<kPairs>(p, pi);
         const Piece* pp = &gp.x;
         if (gp.two) {
           const Steps x = steps_of<kMask>(gp.x), y = steps_of<kMask>(gp.y);
@@ -857,7 +863,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       uint32_t n = 0, tails = 0;
       bool alive = true;
       for (uint32_t pi = first, take; alive && pi < last; pi += take) {
-        const Group gp = group_of<kMask>(p, pi);
+        const Group gp = group_of<kPairs>(p, pi);
         take = gp.two ? 2 : 1;
         const Steps x = steps_of<kMask>(gp.x), y = gp.two ? steps_of<kMask>(gp.y) : Steps{0, 0, 0, 0, 0};
         for (uint32_t j = 0; alive && j < max(x.count, y.count); ++j)
@@ -913,7 +919,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       uint32_t items = 0, tails = 0;  // steps so far
       bool alive = true, more = true;
       for (uint32_t pi = first, take; alive && more && pi < last; pi += take) {
-        const Group gp = group_of<kMask>(p, pi);
+        const Group gp = group_of<kPairs>(p, pi);
         take = gp.two ? 2 : 1;
         const Steps x = steps_of<kMask>(gp.x), y = gp.two ? steps_of<kMask>(gp.y) : Steps{0, 0, 0, 0, 0};
         for (uint32_t j = 0, t = 0; alive && more && j < max(x.count, y.count); t + 1 < take ? ++t : (t = 0, ++j)) {
@@ -975,12 +981,12 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       uint32_t n = 0, raws = 0;
       bool alive = true;
       for (uint32_t pi = first, take; alive && pi < last; pi += take) {
-        const Group gp = group_of<kMask>(p, pi);
+        const Group gp = group_of<kPairs>(p, pi);
         take = gp.two ? 2 : 1;
         const Steps x = steps_of<kMask>(gp.x), y = gp.two ? steps_of<kMask>(gp.y) : Steps{0, 0, 0, 0, 0};
         for (uint32_t j = 0, t = 0; alive && j < max(x.count, y.count); t + 1 < take ? ++t : (t = 0, ++j)) {
-          const Steps& z = kMask && t ? y : x;
-          if (kMask && j >= z.count) continue;
+          const Steps& z = kPairs && t ? y : x;
+          if (kPairs && j >= z.count) continue;
           const uint32_t keys = z.keys;
           const uint32_t rs = raws % C::kRaws;
           if (!mbar_wait_warp(smem_u32(&bars.raw_full[rs]), (raws / C::kRaws) & 1)) {
@@ -1039,28 +1045,31 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
   if (warp == 9) tc_dealloc<C::kCtas>(bars.tmem, 512);
 }
 
-template <int D, int FMT, bool kMask>
+template <int D, int FMT, int FORM>
 cudaError_t prepare_form() {
   // setmaxnreg hands out what the launch was given: fewer registers than the split adds up to would wait for ever
   cudaFuncAttributes at{};
-  cudaError_t e = cudaFuncGetAttributes(&at, tiles_kernel<D, FMT, kMask>);
+  cudaError_t e = cudaFuncGetAttributes(&at, tiles_kernel<D, FMT, FORM>);
   if (e != cudaSuccess) return e;
   const int threads = Cfg<D, FMT>::kWarps * 32;
   if (at.numRegs * threads < 256 * Cfg<D, FMT>::kRegSoft + (threads - 256) * Cfg<D, FMT>::kRegRest)
     return cudaErrorInvalidKernelImage;
-  return cudaFuncSetAttribute(tiles_kernel<D, FMT, kMask>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(tiles_kernel<D, FMT, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               Cfg<D, FMT>::kSmem);
 }
 template <int D, int FMT>
 cudaError_t prepare_one() {
-  const cudaError_t e = prepare_form<D, FMT, false>();
-  return e != cudaSuccess ? e : prepare_form<D, FMT, true>();
+  cudaError_t e = prepare_form<D, FMT, kPlain>();
+  if (e == cudaSuccess) e = prepare_form<D, FMT, kDrafts>();
+  return e != cudaSuccess ? e : prepare_form<D, FMT, kInPairs>();
 }
 template <int D, int FMT>
 cudaError_t launch_one(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s) {
   using C = Cfg<D, FMT>;
-  return launch(p.mask_tiles ? tiles_kernel<D, FMT, true> : tiles_kernel<D, FMT, false>, p.tile_workers * C::kCtas,
-                C::kWarps * 32, C::kSmem, C::kCtas, overlap, s, a, p);
+  return launch(p.pairs        ? tiles_kernel<D, FMT, kInPairs>
+                : p.mask_tiles ? tiles_kernel<D, FMT, kDrafts>
+                               : tiles_kernel<D, FMT, kPlain>,
+                p.tile_workers * C::kCtas, C::kWarps * 32, C::kSmem, C::kCtas, overlap, s, a, p);
 }
 
 }  // namespace

@@ -35,7 +35,9 @@ def plan(tmp_path_factory):
              "          for (size_t x = at; x < at + 2; ++x) CHECK(!pieces[x].split && (int)pieces[x].nrows <= tile_rows_of(D) / 2);\n"
              "          ++pairs;\n"
              "        }"),
-            ("const unsigned workers = kind ?", "static unsigned pairs = 0;\n      const unsigned workers = kind ?")):
+            ("const unsigned workers = kind ?", "unsigned pairs = 0;\n      const unsigned workers = kind ?"),
+            ("        if (p.nfold) CHECK(next == p.nrows);\n      }\n", "        if (p.nfold) CHECK(next == p.nrows);\n      }\n"
+             "      CHECK(!kind || pairs == o.pairs);\n")):
         assert text.count(old) == 1, old
         text = text.replace(old, new)
     src.write_text(text)
