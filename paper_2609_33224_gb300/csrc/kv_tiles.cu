@@ -730,6 +730,10 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
       uint32_t p_seen[2] = {0, 0}, q_seen[2] = {0, 0}, tails = 0;
       bool alive = true;
       auto wait = [&](uint32_t bar, uint32_t parity) { return alive = alive && mbar_wait(bar, parity); };
+      auto looked_at = [&]() {  // the step's values, by the warp that zeroes some of them
+        mbar_arrive(smem_u32(&bars.tail_here));
+        return wait(smem_u32(&bars.tail_done), tails++ & 1);
+      };
       const uint64_t q_desc[2] = {operand(q_smem), operand(q_smem + C::kQ)};
       const uint64_t ring_desc = operand(ring);
       auto scores = [&](uint32_t t, uint32_t slot) {
@@ -775,10 +779,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
               if (j >= z.count) continue;
               const uint32_t i = place(t, j) + 1;
               if (!here(i)) break;
-              if (!C::kFp8 && (z.keys < (j + 1) * kTileKeys || j >= z.masked0)) {
-                mbar_arrive(smem_u32(&bars.tail_here));
-                if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
-              }
+              if (!C::kFp8 && (z.keys < (j + 1) * kTileKeys || j >= z.masked0) && !looked_at()) break;
               for (int half = 0; half < 2; ++half) {
                 if (!wait(smem_u32(&bars.p_ready[t][half]), p_seen[t] & 1)) break;
                 tc_fence_after();
@@ -834,10 +835,7 @@ __global__ void __launch_bounds__(Cfg<D, FMT>::kWarps * 32, 1) tiles_kernel(cons
         }
         for (uint32_t j = 0; alive && j < steps; ++j) {
           if (!here(2 * j + 1)) break;
-          if (!C::kFp8 && (keys - j * kTileKeys < (uint32_t)kTileKeys || (kMask && j >= masked0))) {
-            mbar_arrive(smem_u32(&bars.tail_here));
-            if (!wait(smem_u32(&bars.tail_done), tails++ & 1)) break;
-          }
+          if (!C::kFp8 && (keys - j * kTileKeys < (uint32_t)kTileKeys || (kMask && j >= masked0)) && !looked_at()) break;
           if (pp->split) {
             if (!turn(j & 1, j, 2)) break;
           } else {
