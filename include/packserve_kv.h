@@ -90,8 +90,9 @@ PS_API ps_status ps_kv_write(ps_kv* kv, const ps_kv_rows* k, const ps_kv_rows* v
 /* Rotary positions.  Of a head's elements the first dims (a multiple of 16, at most head_dim) are taken in dims / 2
  * pairs (a, b): elements i and i + dims / 2, or with `interleaved` 2 i and 2 i + 1.  At position p pair i turns by
  * p * frequency[i] radians: (a, b) becomes magnitude * (a cos - b sin, b cos + a sin); the other elements stay.  A
- * frequency is held as a 64-bit fraction of a turn, and its product with the position wraps at a whole turn, so that
- * angles are as exact at a position of millions as at 1: off by no more than p * (frequency[i] * 2^-52 + 2^-62). */
+ * frequency, of either sign, is held as a 64-bit fraction of a turn, and its product with the position wraps at a whole
+ * turn, so that nothing but the frequency's own rounding grows with the position: an angle is off by no more than
+ * |p| * (|frequency[i]| * 2^-52 + 2^-62). */
 typedef struct {
   uint32_t dims;
   uint32_t interleaved; /* 0 or 1 */
@@ -101,9 +102,10 @@ typedef struct {
 
 /* ps_kv_write of keys that are first rotated by positions[t] (device array of n int64, negative ones too), and the same
  * rotation of queries: row t of q (q_heads heads) goes to row t of q_out.  Rotation is in 32 bits, and what is stored is
- * rounded once; an fp8 row's scale is the exact row's, but where its maximum is within 2^-26 of a border.  q, k and v have one element type; q_out the type that ps_kv_attend takes.  q and q_out: both NULL (and
- * q_heads 0) for keys alone; q_out may be q itself, and must not overlap it or k or v otherwise.  Queries of tokens
- * whose slot is negative or outside the cache are rotated all the same.  The paper has no counterpart.
+ * rounded once; an fp8 row's scale is that of the row turned exactly by the angles as they are held, but where its maximum
+ * is within 2^-26 of a border.  q, k and v have one element type; q_out the type that ps_kv_attend takes.  q and q_out:
+ * both NULL (and q_heads 0) for keys alone; q_out may be q itself, and must not overlap it or k or v otherwise.  Queries
+ * of tokens whose slot is negative or outside the cache are rotated all the same.  The paper has no counterpart.
  * Errors: as ps_kv_write. */
 PS_API ps_status ps_kv_write_rotated(ps_kv* kv, const ps_kv_rotary* rotary, const int64_t* positions, const ps_kv_rows* q,
                                      const ps_kv_rows* q_out, uint32_t q_heads, const ps_kv_rows* k, const ps_kv_rows* v,

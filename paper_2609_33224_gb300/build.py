@@ -47,6 +47,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
                os.path.join(ROOT, "include", "packserve.h")]
     kv_headers = [os.path.join(CSRC, "kv_internal.cuh"), os.path.join(CSRC, "kv_plan.h"),
                   os.path.join(CSRC, "kv_ring.h"), os.path.join(CSRC, "kv_elem.cuh"),
+                  os.path.join(CSRC, "kv_turns.h"),
                   os.path.join(ROOT, "include", "packserve_kv.h"), headers[-1]]
     jobs = []
     for src in SOURCES:

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "kv_internal.cuh"
+#include "kv_turns.h"
 
 namespace {
 
@@ -470,15 +471,6 @@ const char* vector_error(const void* p, uint64_t n, const char* null, const char
   return n > 0 && reinterpret_cast<uintptr_t>(p) % align ? odd : nullptr;
 }
 
-// A frequency as turns per position, in 2^-64 of a turn.
-uint64_t turns_of(double frequency) {
-  double t = frequency / 6.283185307179586476925;
-  t -= std::floor(t);  // [0, 1], as exact as t
-  const double hi = std::floor(t * 0x1p32), lo = (t * 0x1p32 - hi) * 0x1p32;
-  // parts that round up to 2^32 carry, and a whole turn is none
-  return ((uint64_t)hi << 32) + (uint64_t)std::nearbyint(lo);
-}
-
 }  // namespace
 
 extern "C" {
@@ -605,7 +597,7 @@ ps_status ps_kv_write_rotated(ps_kv* kv, const ps_kv_rotary* ro, const int64_t* 
   a.dims = ro->dims;
   a.interleaved = ro->interleaved;
   a.magnitude = ro->magnitude;
-  for (uint32_t i = 0; i < ro->dims / 2; ++i) a.turns[i] = turns_of(ro->frequency[i]);
+  for (uint32_t i = 0; i < ro->dims / 2; ++i) a.turns[i] = pskv::turns_of(ro->frequency[i]);
   OnDevice on(kv->device);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   st = begin(kv, s);
