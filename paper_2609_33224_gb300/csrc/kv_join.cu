@@ -227,9 +227,7 @@ cudaError_t go(const AttnArgs& a, const PlanDev& p, bool overlap, cudaStream_t s
   const uint32_t wide = p.max_parts <= 8 && (p.mask_tiles || p.mask_rows) ? 512 : 1024;
   if (p.max_parts > 4 && rows <= wide)
     return launch(join_kernel<D, FP16, true>, rows, 256, 0, 1, overlap, s, a, p);
-  // A warp an entry where there are many rows of few parts: 24700 rows of 2 parts 10.4 us, 17.3 by a warp a row; 7700 rows
-  // of 5 or more 18.5 and 11.5; 16400 of 8 the same.
-  if (p.join_parts <= 8 && rows > 16384)
+  if (join_by_entries(p.njoin, p.join_stride, p.join_parts))
     return launch(p.join_parts <= 4 ? join_entries_kernel<D, FP16, 4> : join_entries_kernel<D, FP16, 8>, (p.njoin + 7) / 8,
                   256, 0, 1, overlap, s, a, p);
   return launch(join_kernel<D, FP16, false>, (rows + 7) / 8, 256, 0, 1, overlap, s, a, p);

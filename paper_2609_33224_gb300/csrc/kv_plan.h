@@ -203,6 +203,15 @@ struct Layout {
 // Rows of the join kernel's launch.
 inline uint64_t join_rows(const Layout& o) { return (uint64_t)o.join.size() * o.join_stride; }
 
+// Whether a warp of the join kernel takes an entry, its rows one after the other, some at once, instead of a row: where
+// there are many rows of few parts, several rows an entry, and entries enough to fill the GPU.  Whole calls, by entries
+// and by rows, us: 4096 entries of 8 rows, 4 parts 93.7 and 102.8, 16384 of 2 91.9 and 93.7, 3200 of 16, 5 parts 105.3 and
+// 111.0, 2048 of 16, 4 parts 82.1 and 83.1; but 1600 of 16, 6 parts 64.1 and 59.6, 1280 of 16, 5 parts 59.1 and 53.6, 32768
+// of 1 145 and 135.
+inline bool join_by_entries(uint32_t entries, uint32_t stride, uint32_t parts) {
+  return parts <= 8 && stride > 1 && entries >= 2048 && (uint64_t)entries * stride > 16384;
+}
+
 // A unit of the layer and group that come last.
 inline Unit unit(const ps_kv_span& s, uint32_t r0, uint32_t nr, uint32_t h, int64_t from, int64_t end, int step, int32_t climit,
           uint32_t tile_rows, const Layout& o) {
