@@ -204,8 +204,9 @@ PS_API ps_status ps_kv_attend(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, 
  * rows mask_stride words apart (4-byte aligned): bit j of query i's row (bit j % 32 of word j / 32) is set where i sees
  * token j of its masked span's own ones, the span's length - num_queries + j-th.  Bits past the span's queries and rows of
  * queries without a masked span are not looked at; 32 * mask_words is at least the queries of the longest masked span.
- * Any mask will do: a query need not see itself, nor anything.  The paper has no counterpart.
- * Errors: as ps_kv_attend, which refuses such a batch. */
+ * Any mask will do: a query need not see itself, nor anything.  A batch without masked spans takes no mask (NULL): one that
+ * is given would not be looked at, and is refused.  The paper has no counterpart.
+ * Errors: as ps_kv_attend, which refuses a batch with masked spans. */
 PS_API ps_status ps_kv_attend_masked(ps_kv* kv, ps_kv_plan* plan, const ps_kv_rows* q, const ps_kv_rows* out, float* lse,
                                      float scale, const uint32_t* mask, int64_t mask_stride, uint32_t mask_words,
                                      void* workspace, uint64_t workspace_bytes, void* stream);

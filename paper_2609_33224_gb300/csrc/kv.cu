@@ -399,6 +399,7 @@ ps_status attend(ps_kv* kv, ps_kv_plan* pl, const ps_kv_rows* q, const ps_kv_row
   if (!m && lse && reinterpret_cast<uintptr_t>(lse) % 4) m = "lse must start on a 4-byte boundary";
   if (!m && !std::isfinite(scale)) m = "scale must be finite";
   if (!m && pl->masked && !mask) m = "the batch has masked spans: it needs a mask";
+  if (!m && T && !pl->masked && mask) m = "the batch has no masked span: it takes no mask";
   if (!m && pl->masked && reinterpret_cast<uintptr_t>(mask) % 4) m = "the mask must start on a 4-byte boundary";
   if (!m && pl->masked > 32ull * mask_words) m = "the mask's rows are shorter than a masked span's queries";
   const uint64_t need = workspace_bytes(pl);

@@ -334,8 +334,8 @@ class KVCache:
 
         ``scale`` defaults to head_dim ** -0.5; ``lse``, a contiguous float32 [queries, q_heads] tensor, receives
         the logarithms of the softmax sums (-inf where a query sees no key; its output is zero).  ``mask``, int32
-        [queries, words] with rows of neighbouring words, is what a plan with masked spans needs: bit j % 32 of word j / 32
-        says whether the query sees token j of its masked span's own ones.
+        [queries, words] with rows of neighbouring words, is what a plan with masked spans needs, and no other takes: bit
+        j % 32 of word j / 32 says whether the query sees token j of its masked span's own ones.
         """
         h, p = self._open(), plan._open()
         n, heads = plan.num_queries, plan.q_heads
@@ -346,6 +346,8 @@ class KVCache:
                     32 * mask.shape[1] < plan.masked or (mask.shape[1] > 1 and mask.stride(1) != 1):
                 raise ValueError(f"mask must be int32 of shape [{n}, at least {-(-plan.masked // 32)}] on "
                                  f"cuda:{self.device}, a row's words next to each other")
+        elif mask is not None and n:
+            raise ValueError("the plan has no masked span: attend takes no mask")
         self._rows(0, q, "q", n, heads)
         out = self._out(_ROWS.size, out, "out", n, heads, None if out is not None else q.dtype)
         if lse is not None and (lse.dtype != torch.float32 or lse.device != q.device or not lse.is_contiguous() or
