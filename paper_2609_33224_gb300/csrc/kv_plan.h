@@ -119,12 +119,12 @@ inline double tile_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool 
 }
 
 // The same for all keys of a masked span.  By rows they cost about twice as much as a plain span's, in pieces that end with
-// masked blocks (32 drafts of 32 nodes on 300 to 500 tokens, 4 query heads a key/value head: 34 us by tiles, 51 by rows; 16
-// of 8 nodes on 1500 to 2000 38 and 53; 60 of 4 nodes on 2000 to 3000, fp8, 187 and 127).  Where the rows have a prefix
-// too, the tile kernel's results are to be joined with the prefix's, which the row kernel can do as it goes: 32 drafts
-// of 48 nodes on 30 tokens or less and 8000 shared ones 343 by tiles, 292 by rows; 60 of 8 to 12 nodes on 50 to 300 and
-// 4000, fp8, 117 and 110; 60 of up to 31 on up to 700 and 16384, fp8, 441 with all of them that the first rule would
-// give to tiles and 426 with this one.
+// masked blocks (all by tiles, and all by rows: 32 drafts of 32 nodes on 300 to 500 tokens, 4 query heads a key/value head,
+// 35 us and 52; 16 of 8 nodes on 1500 to 2000 38 and 50; 64 of 8 on 1800 to 2000 134 and 287; 60 of 4 on 2000 to 3000, fp8,
+// 184 and 128).  Where the rows have a prefix too, the tile kernel's results are to be joined with the prefix's, which the
+// row kernel can do as it goes: 32 drafts of 48 nodes on 30 tokens or less and 8000 shared ones 340 and 293; 60 of 8 to 12
+// nodes on 50 to 300 and 4000, fp8, 130 and 111; 60 of up to 31 on up to 700 and 16384, fp8, 438 and 490, and 421 by this
+// rule.  (Pieces of one tile of rows run in pairs in all of these.)
 constexpr double kMaskedRows = 2.0, kJoinRow = 0.25;
 inline double masked_saves(const PlanShape& kv, uint32_t rows, int64_t keys, bool prefix) {
   const double tile = step_ns(kv) * (double)((keys + kTileKeys - 1) / kTileKeys + kPieceSteps);
@@ -428,8 +428,8 @@ inline void lay_out(const PlanShape& pl, uint32_t T, const ps_kv_span* spans, ui
   const int tile_sms = o.row_sms < pl.sms ? pl.sms - o.row_sms : pl.sms;
   const uint32_t row_workers = (uint32_t)(o.row_sms * kRowWarps);
   // In a masked batch pieces of one tile of rows run two at a time, where there are enough of them, instead of each as two
-  // by parity, which leaves two results: 96 units for 76 workers (12 drafts of 16 nodes on up to 3000 tokens) 47.7 us and
-  // 50.9, 256 units on up to 1000 48.7 and 59.7 (62.8 one after the other); with 64 units on up to 8000 77.6 and 70.9.
+  // by parity, which leaves two results: 96 units for 76 workers (12 drafts of 16 nodes on up to 3000 tokens) 45.8 us and
+  // 47.4 (51.3 one after the other), 256 units on up to 1000 49.3 and 59.3 (63.4); with 64 units on up to 8000 77.6 and 66.0.
   const uint32_t tile_workers = (uint32_t)std::max(1, tile_sms / tile_ctas_of((int)pl.D));
   const bool may_split = !o.mask_tiles || o.tile_units.size() < tile_workers;
   auto finish = [&](std::vector<Unit>& units, std::vector<Piece>& pieces, std::vector<uint32_t>& first, bool rows) {

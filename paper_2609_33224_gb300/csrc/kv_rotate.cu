@@ -137,7 +137,8 @@ __device__ __noinline__ void store_exactly(const RotateArgs& a, uint64_t t, uint
 // whole row to another scale, so rows whose maximum is that near to a border (one in 10^5) are turned again, to 2^-28.
 // Bound by bytes: reads q, k and v and writes the rotated queries and the cache's rows, each once.  65536 tokens of 64 and
 // 8 heads, 128 columns, bf16 to fp8, 2.55 GB: 421 us = 6.1 TB/s, 89% of the measured copy; all keys turned to 2^-28 took
-// 456, none 410.  The next row loaded ahead, three or two blocks an SM or streaming stores gave nothing.
+// 456, none 410.  Four blocks an SM, whose 64 registers a thread spill 44 to 92 bytes, hide more latency than three (437)
+// or two (509).  The next row loaded ahead or streaming stores gave nothing.
 template <int D, int FMT, int TYPE>
 __global__ void __launch_bounds__(256, TYPE == PS_KV_FP32 ? 3 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
   constexpr bool kFp8 = FMT == PS_KV_FP8;

@@ -24,10 +24,10 @@
 // Masked spans, whose own tokens a row sees by its bits, are taken whole, in instances of the kernel of their own (kMask):
 // their last steps' scores are masked by four words a row, and own tokens' value rows that are not finite are zeroed too,
 // as 0 times an infinity is no zero, and added at the end for the rows that see them.  32 trees of 40 to 64 nodes on 3000
-// to 5000 tokens, 64 query and 8 key/value heads, 219 GFLOP: 188 us (1.17 PFLOP/s; a tile's 256 rows are 80% filled), 245
-// with the drafted tokens by the row kernel and joined.  There, pieces of one tile of rows run two at a time, the second as
-// tile 1, so that one's softmax, start and end lie beside the other's steps: 32 trees of 16 nodes on 800 to 1000 tokens 49
-// us, 63 one after the other.
+// to 5000 tokens, 64 query and 8 key/value heads, 219 GFLOP: a call takes 189 us (1.16 PFLOP/s; a tile's 256 rows are 80%
+// filled), of which this kernel alone 181, 245 with the drafted tokens by the row kernel and joined.  There, pieces of one
+// tile of rows run two at a time, the second as tile 1, so that one's softmax, start and end lie beside the other's steps:
+// 32 trees of 16 nodes on 800 to 1000 tokens 49 us, 63 one after the other.
 //
 // Bound by the tensor cores for full tiles: 4 * D multiply-adds a row and key, and, near that, the
 // exponentials: one per row and key.  Work is cut into equal shares per worker; each walks its pieces.
